@@ -430,6 +430,168 @@ int pp_sweep_spills(int32_t n, const int32_t *parent, int32_t *nbatches, int32_t
 int pp_backtrack_table(int32_t n, const int32_t *parent, uint32_t *table,
                        int64_t *rows);
 
+/* ------------------------------------------------------------------------
+ * The prefix cache of one worker: what runs below a plan.
+ *
+ * A worker keeps keys and values in pages of `page_size` tokens.  The chunks
+ * of its target row lie in slots 0..n_slots-1; slot s owns the pages
+ * s * (chunk_tokens / page_size) onwards, and every further page belongs to
+ * one request at a time.  A batch step is
+ *   pp_block_tables     prefixes found in the tree, pages handed out, the
+ *                       place of every new token
+ *   pp_kv_write         the new keys and values into their places (per layer)
+ *   pp_paged_attention  the new tokens' attention over their requests' pages
+ *                       (per layer), single tokens included
+ * and pp_prefix_table (per tree) and pp_cache_slots (per plan) lay out on
+ * the host what it looks things up in.
+ *
+ * The three enqueue their work on `hip_stream` and return; nothing is
+ * allocated and nothing is waited for, so they can be captured into a graph.
+ * What the host can see is checked before anything is enqueued (PP_E_ARG,
+ * PP_E_UNSUPPORTED); contents of device arrays are not read by the host:
+ * node, slot, page and token numbers out of range are treated as absent
+ * where the text says so, and in no case lead out of the arrays given.
+ * Row starts of queries, keys, values, outputs and pages are 16-byte
+ * aligned: their pointers, and their strides times the element size.
+ * ------------------------------------------------------------------------ */
+
+/* Element types of rows and pages.  PP_E4M3 is the 8-bit float of 4 exponent
+ * and 3 mantissa bits without infinities (largest value 448). */
+enum { PP_BF16 = 1, PP_F16 = 2, PP_E4M3 = 3 };
+
+/* Host only: the tree as pp_block_tables reads it.  table [n][16]: entries
+ * 0..14 of line v are v, its parent and so on (-1 past a root), entry 15 is
+ * v's depth (0 for a root).  One 64-byte line answers 14 levels, so a path
+ * of d chunks takes d / 14 dependent reads. */
+int pp_prefix_table(int32_t n, const int32_t *parent, int32_t *table);
+
+/* Host only: slots for a target row.  target [n]: a worker's row (nonzero =
+ * resident); held [n] or NULL: the slots so far (-1 = none).  A chunk that
+ * is held and still targeted keeps its slot; the others of the target take
+ * the free slots in increasing order, chunks in increasing id; every other
+ * chunk gets -1.  slot [n] out (may be `held` itself); n_new out, may be
+ * NULL: chunks without a slot so far, whose pages have to be filled.
+ * PP_E_RANGE if the target has more than n_slots chunks, or held names a
+ * slot out of range or twice. */
+int pp_cache_slots(int32_t n, const uint8_t *target, const int32_t *held,
+                   int32_t n_slots, int32_t *slot, int32_t *n_new);
+
+/* Block tables and slot maps of a batch, on the GPU.  All pointers are
+ * device pointers.
+ * Request r stands at `length[r]` tokens once all of them are computed.
+ *   cached[r] < 0: it begins in this step.  Its prefix is the path from a
+ *     root to chunk leaf[r] (out of range: none); the chunks on the path up
+ *     to the first one without a slot in 0..n_slots-1 are found, as long as
+ *     they end before the last token (one token at least is computed):
+ *     start = chunk_tokens * min(found, (length - 1) / chunk_tokens).
+ *   cached[r] >= 0: it goes on: start = min(cached[r], length[r]), and its
+ *     row holds the pages of those tokens.
+ * end = min(length, start + max_new) (max_new = 0: length).
+ * Row r of block_table gets the found chunks' pages, and from block
+ * ceil(start / page_size) to before ceil(end / page_size) pages off
+ * free_pages, which requests take in order of r; other entries stay as they
+ * are.  The new tokens of all requests, in order, are numbered from 0:
+ * request r has query_start[r] .. query_start[r + 1] - 1, of which number i
+ * stands at position[i] and its keys and values belong in slot_map[i] =
+ * page * page_size + position % page_size.  Numbers from the batch's tokens
+ * up to max_tokens get slot -1 and position 0.
+ * taken[0] = pages needed; above n_free, the requests that came too late
+ * have -1 in block_table and slot_map.  Blocks at or past max_blocks are not
+ * written, and their tokens get slot -1; so do page numbers below 0 in a
+ * row.  Tokens at or past max_tokens are counted in query_start and written
+ * nowhere.  Negative lengths act as 0. */
+typedef struct {
+    int32_t requests;          /* >= 0, at most 65,536 */
+    int32_t n;                 /* chunks in the tree, >= 0 */
+    int32_t n_slots;
+    int32_t n_free;
+    int32_t max_blocks;        /* entries a row of block_table holds */
+    int32_t max_tokens;        /* entries of slot_map and position */
+    int32_t page_size;         /* a power of two, 16 .. 1,024 */
+    int32_t chunk_tokens;      /* a multiple of page_size */
+    int32_t max_new;
+    int64_t row_stride;        /* entries from a row of block_table to the next */
+    const int32_t *leaf, *length, *cached;      /* [requests] */
+    const int32_t *prefix_table;                /* [n][16], 16-byte aligned */
+    const int32_t *slot;                        /* [n] */
+    const int32_t *free_pages;                  /* [n_free] */
+    int32_t *block_table;                       /* [requests][max_blocks] */
+    int32_t *query_start;                       /* out [requests + 1] */
+    int32_t *start, *end;                       /* out [requests] */
+    int64_t *slot_map;                          /* out [max_tokens] */
+    int32_t *position;                          /* out [max_tokens] */
+    int32_t *taken;                             /* out [1] */
+} pp_block_args;
+int pp_block_tables(const pp_block_args *args, void *hip_stream);
+
+/* One layer's pages: element (page, head, token, i) of k and of v lies at
+ * page * page_stride + head * head_stride + token * token_stride + i
+ * elements (any order of the three).  PP_E4M3 pages hold value / scale of
+ * their head, k_scale and v_scale [heads] (device; NULL = 1); other types
+ * have no scales. */
+typedef struct {
+    void *k, *v;
+    const float *k_scale, *v_scale;
+    int32_t dtype;
+    int32_t n_pages, page_size;    /* page_size a power of two, 16 .. 1,024 */
+    int32_t heads;
+    int32_t dim;                   /* 64, 128 or 256 */
+    int64_t page_stride, head_stride, token_stride;
+} pp_kv_pages;
+
+/* Writes rows k, v [tokens][heads][dim] (PP_BF16 or PP_F16) into the places
+ * slot_map names; a place below 0 or past the pages is skipped, and one named
+ * twice gets either row.  Pages of the rows' own type take them as they are;
+ * PP_E4M3 pages take row / scale rounded to nearest even, values past +-448
+ * (infinities too) as +-448, NaN as NaN.  Strides in elements. */
+int pp_kv_write(const pp_kv_pages *pages, int32_t tokens, int32_t dtype,
+                const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                const int64_t *slot_map, void *hip_stream);
+
+/* Attention of a batch's new tokens over their requests' pages.
+ * Request r has length[r] tokens in its pages, the last of which are its
+ * query_start[r + 1] - query_start[r] new ones, so new token i of u stands
+ * at p = length - u + i and sees the keys j <= p of its request, with
+ * window > 0 the last `window` of them (j > p - window):
+ *   s_j = scale * <q, K_j>,  out = sum_j e^(s_j) V_j / sum_j e^(s_j),
+ *   lse = log sum_j e^(s_j).
+ * A row that sees no key (p < 0), or only keys of s_j = -infinity, has
+ * out = 0 and lse = -infinity.  Query head g reads key head
+ * g / (q_heads / heads).  What a row does not see does not touch it, whatever
+ * it holds (NaN and infinities too).  Page numbers below 0 act as 0, above
+ * the last as the last; tokens past a row of the block table do not exist.
+ * Scores, sums and the accumulation are held in 32 bits; weights are rounded
+ * to the queries' type for the product with V.
+ * max_new and max_len bound every request's new tokens and length; new
+ * tokens past max_new may be left unwritten.  `workspace` is device memory
+ * of pp_attention_workspace bytes at least (256-byte aligned); the call
+ * writes it before it reads it, so its contents need not be kept. */
+typedef struct {
+    int32_t requests;              /* >= 0, at most 65,536 */
+    int32_t tokens;                /* rows of q and out */
+    int32_t q_heads;               /* a multiple of the pages' heads */
+    int32_t dtype;                 /* of q and out: PP_BF16 or PP_F16 */
+    int32_t max_new, max_len;
+    int32_t max_blocks;
+    int32_t window;                /* 0 = none */
+    float scale;
+    int64_t q_token_stride, q_head_stride;      /* elements */
+    int64_t out_token_stride, out_head_stride;
+    int64_t row_stride;            /* of block_table */
+    const void *q;                 /* [tokens][q_heads][dim] */
+    void *out;                     /* [tokens][q_heads][dim] */
+    float *lse;                    /* [tokens][q_heads], or NULL */
+    const int32_t *query_start;    /* [requests + 1] */
+    const int32_t *length;         /* [requests] */
+    const int32_t *block_table;    /* [requests][max_blocks] */
+    void *workspace;
+    int64_t workspace_bytes;
+} pp_attention_args;
+int64_t pp_attention_workspace(const pp_kv_pages *pages, const pp_attention_args *args);
+int pp_paged_attention(const pp_kv_pages *pages, const pp_attention_args *args,
+                       void *hip_stream);
+
 /* Description of the last error on the calling thread; valid until the
  * next pp_* call on that thread. */
 const char *pp_last_error(void);

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libprefixplace.so")
 
 PP_OK, PP_E_ARG, PP_E_TREE, PP_E_RANGE, PP_E_OVERFLOW = 0, -1, -2, -3, -4
 PP_E_NOMEM, PP_E_DEVICE, PP_E_UNSUPPORTED = -5, -6, -7
+PP_BF16, PP_F16, PP_E4M3 = 1, 2, 3
 PP_F_VALIDATE_ONLY, PP_F_NO_REFINE, PP_F_TIME_KERNELS, PP_F_SAFEGUARDS = 1, 2, 4, 8
 
 _P = ctypes.c_void_p
@@ -69,6 +70,39 @@ class pp_replan_info_f64(ctypes.Structure):
     _fields_ = [("adopt", ctypes.c_int32), ("incumbent_objective", ctypes.c_double),
                 ("proposal_objective", ctypes.c_double),
                 ("materialization_cost", ctypes.c_double)]
+
+
+class pp_block_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("requests", "n", "n_slots", "n_free", "max_blocks", "max_tokens",
+                 "page_size", "chunk_tokens", "max_new")] + \
+               [("row_stride", ctypes.c_int64)] + \
+               [(f, _P) for f in
+                ("leaf", "length", "cached", "prefix_table", "slot", "free_pages",
+                 "block_table", "query_start", "start", "end", "slot_map",
+                 "position", "taken")]
+
+
+class pp_kv_pages(ctypes.Structure):
+    _fields_ = [(f, _P) for f in ("k", "v", "k_scale", "v_scale")] + \
+               [(f, ctypes.c_int32) for f in
+                ("dtype", "n_pages", "page_size", "heads", "dim")] + \
+               [(f, ctypes.c_int64) for f in
+                ("page_stride", "head_stride", "token_stride")]
+
+
+class pp_attention_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("requests", "tokens", "q_heads", "dtype", "max_new", "max_len",
+                 "max_blocks", "window")] + \
+               [("scale", ctypes.c_float)] + \
+               [(f, ctypes.c_int64) for f in
+                ("q_token_stride", "q_head_stride", "out_token_stride",
+                 "out_head_stride", "row_stride")] + \
+               [(f, _P) for f in
+                ("q", "out", "lse", "query_start", "length", "block_table",
+                 "workspace")] + \
+               [("workspace_bytes", ctypes.c_int64)]
 
 
 class PPError(RuntimeError):
@@ -128,6 +162,16 @@ def lib() -> ctypes.CDLL:
         L.pp_plan_device.argtypes = [_P, i32, i32, _P, _P, _P, _P, _P, _P, _P,
                                      _P, _P, _P]
         L.pp_objective_device_noalloc.argtypes = [i32, i32, _P, _P, _P, _P, _P, _P]
+        L.pp_prefix_table.argtypes = [i32, _P, _P]
+        L.pp_cache_slots.argtypes = [i32, _P, _P, i32, _P, _P]
+        L.pp_block_tables.argtypes = [_P, _P]
+        L.pp_kv_write.argtypes = [_P, i32, i32, _P, i64, i64, _P, i64, i64, _P, _P]
+        L.pp_attention_workspace.argtypes = [_P, _P]
+        L.pp_attention_workspace.restype = i64
+        L.pp_paged_attention.argtypes = [_P, _P, _P]
+        for f in (L.pp_prefix_table, L.pp_cache_slots, L.pp_block_tables,
+                  L.pp_kv_write, L.pp_paged_attention):
+            f.restype = ctypes.c_int
         for f in (L.pp_plan, L.pp_replan, L.pp_replan_f64, L.pp_plan_f64,
                   L.pp_plan_f64_device,
                   L.pp_rooted_dp_f64, L.pp_rooted_dp, L.pp_marginal, L.pp_objective,
@@ -483,6 +527,189 @@ def pp_backtrack_table(parent):
     table = np.zeros((rows.value, 4), np.uint32)
     _check(lib().pp_backtrack_table(n, _p(parent), _p(table), ctypes.byref(rows)))
     return table
+
+
+# ------------------------------------------------------------ prefix cache ---
+
+def pp_prefix_table(parent):
+    """The tree as pp_block_tables reads it, int32 [n][16] (host only; see
+    include/prefixplace.h)."""
+    parent = _c(parent, np.int32)
+    n = parent.shape[0]
+    table = np.zeros((n, 16), np.int32)
+    _check(lib().pp_prefix_table(n, _p(parent), _p(table)))
+    return table
+
+
+def pp_cache_slots(target, n_slots, held=None):
+    """Slots for a worker's target row: (int32 [n], chunks new to the cache)
+    (host only; see include/prefixplace.h)."""
+    target = _c(target, np.uint8)
+    held = None if held is None else _c(held, np.int32)
+    n = target.shape[0]
+    if held is not None and held.shape[0] != n:
+        raise ValueError(f"held shape {held.shape} != {(n,)}")
+    slot = np.zeros(n, np.int32)
+    fresh = ctypes.c_int32(0)
+    _check(lib().pp_cache_slots(n, _p(target), None if held is None else _p(held),
+                                int(n_slots), _p(slot), ctypes.byref(fresh)))
+    return slot, fresh.value
+
+
+def _stream_of(torch, t, stream):
+    """The stream to enqueue on, where tensor `t` lies."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("tensors must lie on the current GPU")
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _ints(torch, t, what, *shape):
+    """Address of a contiguous int32 device tensor of that shape."""
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() \
+            or tuple(t.shape) != shape:
+        raise ValueError(f"{what}: want a contiguous int32 tensor of shape {shape} on the GPU")
+    return t.data_ptr()
+
+
+def pp_block_tables(leaf, length, cached, prefix_table, slot, free_pages, block_table,
+                    query_start, start, end, slot_map, position, taken, *, page_size,
+                    chunk_tokens, n_slots, max_new=0, stream=None):
+    """Block tables and slot maps of a batch on torch device tensors (see
+    include/prefixplace.h).  Inputs leaf, length, cached int32 [R],
+    prefix_table int32 [n][16], slot int32 [n], free_pages int32 [f]; the
+    rows of block_table int32 [R][blocks] are updated in place; outputs
+    query_start int32 [R + 1], start, end int32 [R], slot_map int64 [t],
+    position int32 [t], taken int32 [1]."""
+    import torch
+
+    st = _stream_of(torch, length, stream)
+    R, n, t = length.shape[0], slot.shape[0], slot_map.shape[0]
+    if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 \
+            or block_table.shape[0] != R or block_table.stride(1) != 1:
+        raise ValueError("block_table: want int32 rows, one a request, on the GPU")
+    if slot_map.dtype != torch.int64 or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError("slot_map: want a contiguous int64 tensor on the GPU")
+    a = pp_block_args(
+        R, n, int(n_slots), free_pages.shape[0], block_table.shape[1], t, int(page_size),
+        int(chunk_tokens), int(max_new), block_table.stride(0), _ints(torch, leaf, "leaf", R),
+        _ints(torch, length, "length", R), _ints(torch, cached, "cached", R),
+        _ints(torch, prefix_table, "prefix_table", n, 16), _ints(torch, slot, "slot", n),
+        _ints(torch, free_pages, "free_pages", free_pages.shape[0]), block_table.data_ptr(),
+        _ints(torch, query_start, "query_start", R + 1), _ints(torch, start, "start", R),
+        _ints(torch, end, "end", R), slot_map.data_ptr(), _ints(torch, position, "position", t),
+        _ints(torch, taken, "taken", 1))
+    _check(lib().pp_block_tables(ctypes.byref(a), st))
+
+
+_types = {}
+
+
+def _type(torch, t):
+    if not _types:
+        _types.update({torch.bfloat16: PP_BF16, torch.float16: PP_F16,
+                       torch.float8_e4m3fn: PP_E4M3})
+    try:
+        return _types[t.dtype]
+    except KeyError:
+        raise ValueError(f"no rows or pages of {t.dtype}") from None
+
+
+def _rows(t, what):
+    """(token stride, head stride) of device rows [tokens][heads][dim]."""
+    if t.dim() != 3 or not t.is_cuda or (t.stride(2) != 1 and t.shape[2] != 1):
+        raise ValueError(f"{what}: want [tokens][heads][dim] on the GPU, dim contiguous")
+    return t.stride(0), t.stride(1)
+
+
+def _pages(torch, k_cache, v_cache, k_scale, v_scale):
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape \
+            or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1 \
+            or k_cache.dtype != v_cache.dtype or not k_cache.is_cuda or not v_cache.is_cuda:
+        raise ValueError("pages: want two device tensors [pages][heads][page_size][dim] "
+                         "alike, dim contiguous")
+    P, H, ps, D = k_cache.shape
+    scales = []
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or not s.is_cuda or s.shape != (H,)
+                              or not s.is_contiguous()):
+            raise ValueError("scales: want float32 [heads] on the GPU")
+        scales.append(None if s is None else s.data_ptr())
+    sp, sh, st, _ = k_cache.stride()
+    return pp_kv_pages(k_cache.data_ptr(), v_cache.data_ptr(), scales[0], scales[1],
+                       _type(torch, k_cache), P, ps, H, D, sp, sh, st)
+
+
+def pp_kv_write(k, v, slot_map, k_cache, v_cache, *, k_scale=None, v_scale=None, stream=None):
+    """New rows k, v [tokens][heads][dim] into the places slot_map (int64
+    [tokens]) names, on torch device tensors (see include/prefixplace.h).
+    Pages are [pages][heads][page_size][dim] views in any memory order, of
+    the rows' type or float8_e4m3fn."""
+    import torch
+
+    st = _stream_of(torch, k, stream)
+    pages = _pages(torch, k_cache, v_cache, k_scale, v_scale)
+    (kt, kh), (vt, vh) = _rows(k, "k"), _rows(v, "v")
+    T = slot_map.shape[0]
+    if tuple(k.shape) != (T, pages.heads, pages.dim) or k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("shape mismatch")
+    if slot_map.dtype != torch.int64 or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError("slot_map: want a contiguous int64 tensor on the GPU")
+    _check(lib().pp_kv_write(ctypes.byref(pages), T, _type(torch, k), k.data_ptr(), kt, kh,
+                             v.data_ptr(), vt, vh, slot_map.data_ptr(), st))
+
+
+def _attention_args(torch, q, pages, block_table, query_start, length, out, lse, scale, max_new,
+                    max_len, window):
+    T, Hq, D = q.shape
+    R = length.shape[0]
+    (qt, qh), (ot, oh) = _rows(q, "q"), _rows(out, "out")
+    if D != pages.dim or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("shape mismatch")
+    if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 \
+            or block_table.shape[0] != R or block_table.stride(1) != 1:
+        raise ValueError("block_table: want int32 rows, one a request, on the GPU")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda
+                            or tuple(lse.shape) != (T, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse: want a contiguous float32 tensor [tokens][q_heads] on the GPU")
+    return pp_attention_args(
+        R, T, Hq, _type(torch, q), int(max_new), int(max_len), block_table.shape[1], int(window),
+        float(scale), qt, qh, ot, oh, block_table.stride(0), q.data_ptr(), out.data_ptr(),
+        None if lse is None else lse.data_ptr(), _ints(torch, query_start, "query_start", R + 1),
+        _ints(torch, length, "length", R), block_table.data_ptr(), None, 0)
+
+
+def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, out, lse=None, *,
+                       scale, max_new, max_len, window=0, k_scale=None, v_scale=None,
+                       workspace=None, stream=None):
+    """Attention of the batch's new tokens over their requests' pages, on
+    torch device tensors (see include/prefixplace.h): q and out
+    [tokens][q_heads][dim], pages as in pp_kv_write, block_table int32
+    [R][blocks], query_start int32 [R + 1], length int32 [R], lse float32
+    [tokens][q_heads] or None.  Without a `workspace` (a uint8 tensor that
+    the caller keeps) one is taken from torch's allocator for the call."""
+    import torch
+
+    st = _stream_of(torch, q, stream)
+    L = lib()
+    pages = _pages(torch, k_cache, v_cache, k_scale, v_scale)
+    a = _attention_args(torch, q, pages, block_table, query_start, length, out, lse, scale,
+                        max_new, max_len, window)
+    pr, ar = ctypes.byref(pages), ctypes.byref(a)
+    need = L.pp_attention_workspace(pr, ar)
+    if need < 0:
+        _check(need)
+    if need:
+        if workspace is None:
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            else:
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        elif not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace: want a contiguous tensor on the GPU")
+        a.workspace = workspace.data_ptr()
+        a.workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(L.pp_paged_attention(pr, ar, st))
 
 
 class Context:

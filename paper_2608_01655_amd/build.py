@@ -44,7 +44,8 @@ def build(verbose: bool = False) -> str:
     cc = hipcc()
     objs = []
     for src, device in (("pp_kernels.hip", True), ("pp_reduce.hip", True),
-                        ("pp_host.cpp", False)):
+                        ("pp_cache.hip", True), ("pp_attend.hip", True),
+                        ("pp_host.cpp", False), ("pp_serve.cpp", False)):
         obj = os.path.join(BUILD_DIR, src + ".o")
         cmd = [cc, f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS, "-c",
                os.path.join(CSRC, src), "-o", obj]

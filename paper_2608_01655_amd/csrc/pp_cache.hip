@@ -1,0 +1,272 @@
+// pp_cache.hip -- block tables, slot maps and page writes of the prefix
+// cache (gfx950).
+
+#include "pp_serve.h"
+
+namespace pp {
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kWalkWaves = 4;     // requests a block of k_walk looks up, one wave each
+constexpr int kPathLds = 128;     // chunks of a path kept in LDS between its two uses
+constexpr int kFillWaves = 16;    // requests a block of k_fill serves, one wave each
+
+struct Span {
+  int32_t start, end;
+};
+
+__device__ __forceinline__ int32_t ceil_div(int32_t a, int32_t shift) {
+  return (int32_t)(((int64_t)a + (1 << shift) - 1) >> shift);
+}
+
+__device__ __forceinline__ int32_t clamp_end(const pp_block_args& a, int32_t len, int32_t start) {
+  if (a.max_new == 0) return len;
+  const int64_t e = (int64_t)start + a.max_new;
+  return e < len ? (int32_t)e : len;
+}
+
+// Looks request r up and writes its row's found pages; one wave, all lanes
+// active.  slots: kPathLds words of LDS of this wave's own.
+//
+// Found chunks are the run of resident ones from the root down, and the path
+// is read from the leaf up: the run ends at the shallowest chunk without a
+// slot, known only at the root.  So the slots wait in LDS (deeper paths are
+// read twice) until then.
+__device__ Span walk(const pp_block_args& a, int32_t r, int lane, int32_t* slots) {
+  int32_t len = a.length[r];
+  if (len < 0) len = 0;
+  const int32_t cached = a.cached[r];
+  if (cached >= 0) {
+    const int32_t start = cached < len ? cached : len;
+    return {start, clamp_end(a, len, start)};
+  }
+  const int32_t leaf = a.leaf[r];
+  const int32_t most = len > 0 ? (len - 1) / a.chunk_tokens : 0;   // chunks before the last token
+  int32_t depth = -1, hit = 0;
+  if (leaf >= 0 && leaf < a.n && most > 0) {
+    depth = a.prefix_table[(int64_t)leaf * kLine + kLine - 1];
+    if (depth < 0 || depth >= a.n) depth = a.n - 1;
+    hit = depth + 1;
+  }
+  // position of lane j of the current line: at - j
+  int32_t v = leaf;
+  for (int32_t at = depth; at >= 0; at -= kHop) {
+    const int32_t id = lane < kLine ? a.prefix_table[(int64_t)v * kLine + lane] : -1;
+    const bool mine = lane < kHop && at - lane >= 0;
+    int32_t s = -1;
+    if (mine && id >= 0 && id < a.n) {
+      s = a.slot[id];
+      if (s >= a.n_slots) s = -1;
+    }
+    if (mine && at - lane < kPathLds) slots[at - lane] = s;
+    const uint64_t none = __ballot(mine && s < 0);
+    if (none) hit = at - (63 - __builtin_clzll(none));
+    v = __shfl(id, kHop);
+    if (v < 0 || v >= a.n) {
+      if (at >= kHop) hit = 0;   // the line does not reach its root
+      break;
+    }
+  }
+  const int32_t found = hit < most ? hit : most;
+  const int32_t per = a.chunk_tokens / a.page_size;
+  int32_t* row = a.block_table + (int64_t)r * a.row_stride;
+  const int32_t in_lds = found < kPathLds ? found : kPathLds;
+  const int64_t blocks = (int64_t)in_lds * per;
+  for (int64_t b = lane; b < blocks && b < a.max_blocks; b += kWave)
+    row[b] = slots[b / per] * per + (int32_t)(b % per);
+  v = leaf;
+  for (int32_t at = found > kPathLds ? depth : -1; at >= kPathLds; at -= kHop) {
+    const int32_t id = lane < kLine ? a.prefix_table[(int64_t)v * kLine + lane] : -1;
+    const bool mine = lane < kHop && at - lane >= kPathLds && at - lane < found;
+    if (mine && id >= 0 && id < a.n) {
+      const int32_t s = a.slot[id];
+      for (int64_t j = 0, b = (int64_t)(at - lane) * per; j < per && b + j < a.max_blocks; ++j)
+        row[b + j] = s * per + (int32_t)j;
+    }
+    v = __shfl(id, kHop);
+    if (v < 0 || v >= a.n) break;
+  }
+  const int32_t start = found * a.chunk_tokens;
+  return {start, clamp_end(a, len, start)};
+}
+
+__global__ void __launch_bounds__(kWave* kWalkWaves) k_walk(pp_block_args a) {
+  __shared__ int32_t slots[kWalkWaves][kPathLds];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int32_t r = blockIdx.x * kWalkWaves + wave;
+  if (r >= a.requests) return;
+  const Span s = walk(a, r, lane, slots[wave]);
+  if (lane == 0) {
+    a.start[r] = s.start;
+    a.end[r] = s.end;
+  }
+}
+
+// Sum of two values over the block's kFillWaves waves.
+__device__ __forceinline__ void block_sum(int64_t& x, int64_t& y, int64_t (*part)[2]) {
+  for (int o = kWave / 2; o; o >>= 1) {
+    x += __shfl_xor(x, o);
+    y += __shfl_xor(y, o);
+  }
+  const int wave = threadIdx.x / kWave;
+  if (threadIdx.x % kWave == 0) {
+    part[wave][0] = x;
+    part[wave][1] = y;
+  }
+  __syncthreads();
+  x = y = 0;
+  for (int w = 0; w < kFillWaves; ++w) {
+    x += part[w][0];
+    y += part[w][1];
+  }
+  __syncthreads();
+}
+
+// Every block sums the tokens and pages of all requests and of those before
+// its own (8 bytes a request out of L2), then each wave serves one request.
+__global__ void __launch_bounds__(kWave* kFillWaves) k_fill(pp_block_args a, int shift) {
+  __shared__ int64_t part[kFillWaves][2];
+  __shared__ int64_t mine[kFillWaves][2];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int32_t first = blockIdx.x * kFillWaves;
+  int64_t t0 = 0, p0 = 0, t1 = 0, p1 = 0;
+  for (int32_t i = threadIdx.x; i < a.requests; i += kWave * kFillWaves) {
+    const int32_t s = a.start[i], e = a.end[i];
+    const int64_t t = e - s, p = ceil_div(e, shift) - ceil_div(s, shift);
+    if (i < first) {
+      t0 += t;
+      p0 += p;
+    }
+    t1 += t;
+    p1 += p;
+  }
+  block_sum(t0, p0, part);
+  block_sum(t1, p1, part);
+  const int32_t r = first + wave;
+  int32_t start = 0, end = 0;
+  if (r < a.requests) {
+    start = a.start[r];
+    end = a.end[r];
+  }
+  const int32_t b0 = ceil_div(start, shift), b1 = ceil_div(end, shift);
+  if (lane == 0) {
+    mine[wave][0] = end - start;
+    mine[wave][1] = b1 - b0;
+  }
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) {
+    t0 += mine[w][0];
+    p0 += mine[w][1];
+  }
+  auto cap = [](int64_t x) { return (int32_t)(x < INT32_MAX ? x : INT32_MAX); };
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.query_start[0] = 0;
+    a.taken[0] = cap(p1);
+  }
+  // numbers that no token has
+  for (int64_t t = t1 + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < a.max_tokens;
+       t += (int64_t)gridDim.x * blockDim.x) {
+    a.slot_map[t] = -1;
+    a.position[t] = 0;
+  }
+  if (r >= a.requests) return;
+  if (lane == 0) a.query_start[r + 1] = cap(t0 + end - start);
+  int32_t* row = a.block_table + (int64_t)r * a.row_stride;
+  // the page of block b >= b0
+  auto fresh = [&](int32_t b) {
+    const int64_t i = p0 + b - b0;
+    return i < a.n_free ? a.free_pages[i] : -1;
+  };
+  for (int32_t b = b0 + lane; b < b1 && b < a.max_blocks; b += kWave) row[b] = fresh(b);
+  const int32_t mask = a.page_size - 1;
+  for (int64_t i = lane; i < end - start && t0 + i < a.max_tokens; i += kWave) {
+    const int32_t pos = start + (int32_t)i, b = pos >> shift;
+    int32_t page = -1;
+    if (b < a.max_blocks) page = b < b0 ? row[b] : fresh(b);
+    a.slot_map[t0 + i] = page < 0 ? -1 : ((int64_t)page << shift) + (pos & mask);
+    a.position[t0 + i] = pos;
+  }
+}
+
+// ------------------------------------------------------------ page writes ---
+
+typedef __attribute__((__vector_size__(16))) int i32x4;
+typedef __attribute__((__vector_size__(8))) int i32x2;
+
+__device__ __forceinline__ float widen(uint16_t x, bool f16) {
+  if (f16) return (float)__builtin_bit_cast(_Float16, x);
+  return __builtin_bit_cast(float, (uint32_t)x << 16);
+}
+
+// value / scale, held to the type's range; NaN stays NaN.
+__device__ __forceinline__ float shrink(float x, float scale) {
+  const float y = x / scale;
+  return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+}
+
+// Eight elements of a row a thread, of k and of v.  Bound by what it moves:
+// a row is read and written once, 16 bytes a lane.
+template <bool kNarrow>
+__global__ void __launch_bounds__(256) k_write(pp_kv_pages p, int32_t tokens, bool f16,
+                                               const uint16_t* k, int64_t kt, int64_t kh,
+                                               const uint16_t* v, int64_t vt, int64_t vh,
+                                               const int64_t* slot, int shift, int dim8,
+                                               int64_t total) {
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
+       i += (int64_t)gridDim.x * blockDim.x) {
+    const int32_t d = (int32_t)(i % dim8) * 8;
+    const int64_t th = i / dim8;
+    const int32_t h = (int32_t)(th % p.heads);
+    const int64_t t = th / p.heads;
+    const int64_t at = slot[t];
+    if (at < 0 || at >> shift >= p.n_pages) continue;
+    const int64_t to = (at >> shift) * p.page_stride + h * p.head_stride +
+                       (at & (p.page_size - 1)) * p.token_stride + d;
+    const i32x4 x = *(const i32x4*)(k + t * kt + h * kh + d);
+    const i32x4 y = *(const i32x4*)(v + t * vt + h * vh + d);
+    if constexpr (!kNarrow) {
+      *(i32x4*)((uint16_t*)p.k + to) = x;
+      *(i32x4*)((uint16_t*)p.v + to) = y;
+    } else {
+      auto pack = [&](i32x4 w, float s) {
+        float f[8];
+        for (int j = 0; j < 8; ++j) f[j] = shrink(widen((uint16_t)(w[j / 2] >> (16 * (j % 2))), f16), s);
+        i32x2 o;
+        for (int j = 0; j < 2; ++j) {
+          int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j], f[4 * j + 1], 0, false);
+          o[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j + 2], f[4 * j + 3], q, true);
+        }
+        return o;
+      };
+      *(i32x2*)((uint8_t*)p.k + to) = pack(x, p.k_scale ? p.k_scale[h] : 1.f);
+      *(i32x2*)((uint8_t*)p.v + to) = pack(y, p.v_scale ? p.v_scale[h] : 1.f);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_block_tables(const pp_block_args& a, hipStream_t st) {
+  const int shift = __builtin_ctz(a.page_size);
+  if (a.requests)
+    k_walk<<<(a.requests + kWalkWaves - 1) / kWalkWaves, kWave * kWalkWaves, 0, st>>>(a);
+  const int blocks = a.requests ? (a.requests + kFillWaves - 1) / kFillWaves : 1;
+  k_fill<<<blocks, kWave * kFillWaves, 0, st>>>(a, shift);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_write(const pp_kv_pages& p, int32_t tokens, int32_t dtype, const void* k,
+                           int64_t kt, int64_t kh, const void* v, int64_t vt, int64_t vh,
+                           const int64_t* slot, hipStream_t st) {
+  const int shift = __builtin_ctz(p.page_size), dim8 = p.dim / 8;
+  const int64_t total = (int64_t)tokens * p.heads * dim8;
+  const int64_t blocks = (total + 255) / 256;
+  const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+  auto kern = p.dtype == PP_E4M3 ? k_write<true> : k_write<false>;
+  kern<<<grid, 256, 0, st>>>(p, tokens, dtype == PP_F16, (const uint16_t*)k, kt, kh,
+                             (const uint16_t*)v, vt, vh, slot, shift, dim8, total);
+  return hipGetLastError();
+}
+
+}  // namespace pp

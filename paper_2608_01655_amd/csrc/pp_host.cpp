@@ -2397,6 +2397,8 @@ int guarded(F&& fn) {
 
 }  // namespace
 
+int pp::report(int code, const char* msg) { return fail_c(code, msg); }
+
 // ================================================================ C ABI ===
 
 extern "C" {

@@ -433,6 +433,10 @@ hipError_t launch_objective_noalloc(int32_t n, int32_t m, const int64_t* lam,
                                     const uint8_t* tgt, void* scr,
                                     NoAllocResult* out, hipStream_t st);
 
+// Sets this thread's error description (pp_last_error) and returns `code`;
+// allocates nothing.
+int report(int code, const char* msg);
+
 // Blocks of the DP sweep that can be resident at once for `cells` cells
 // per lane and `slots_lds` stack slots (0 if unsupported).
 int dp_resident_blocks(int cells, int32_t slots_lds, int device);
