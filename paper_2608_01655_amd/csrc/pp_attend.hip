@@ -1,4 +1,25 @@
 // pp_attend.hip -- attention of new tokens over paged keys and values (gfx950).
+//
+// out = sum_j w_j V_j / sum_j w_j, w_j = 2^(c s_j - c m), c = scale log2(e) k_scale, s = <q, K_j>,
+// in one pass over the keys with a running maximum m: where it grows by more than 8 in the exponent
+// (weights stay below 2^8), sums and accumulators are scaled down by 2^(c (m_old - m_new)).
+//
+// The query heads of a key head and the new tokens of a request are packed into rows (row =
+// token * G + head), so that a tile of keys is read once for all of them.  Both products are taken
+// transposed: S^T = K Q^T leaves a query in a lane's column and its keys in that lane's registers,
+// which is what the second product O^T = V^T P^T takes as its right operand, with the keys in the
+// registers' own order.  So weights never leave registers; the keys of V^T are put in the same
+// order by transposing LDS reads.
+//
+// Two kernels share this.  k_rows takes requests of few rows, which the reading of the pages
+// bounds: its waves split the keys and each streams its own through LDS with nothing but its own
+// counters to wait for.  k_tiles takes the others, which the matrix cores bound: four waves of 32 rows
+// share each tile of 64 keys.  Both split long requests over blocks, which leave normalised parts
+// and their log sums in the workspace for k_join.
+//
+// Weights are rounded to the queries' type for the second product (their error averages out over
+// the keys and is below that of rounding the output); scores, sums and accumulators are 32 bits.
+// 8-bit pages are widened to the queries' type after LDS, which is exact.
 
 #include "pp_serve.h"
 
@@ -6,63 +27,917 @@ namespace pp {
 
 namespace {
 
-constexpr int kWave = 64;
+typedef __attribute__((__vector_size__(4))) short s16x2;
+typedef __attribute__((__vector_size__(8))) short s16x4;
+typedef __attribute__((__vector_size__(16))) short s16x8;
+typedef __attribute__((__vector_size__(8))) int i32x2;
+typedef __attribute__((__vector_size__(16))) int i32x4;
+typedef __attribute__((__vector_size__(16))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(16))) float f32x4;
+typedef __attribute__((__vector_size__(64))) float f32x16;
+typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(16))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4))) _Float16 f16x2;
+typedef __attribute__((__vector_size__(16))) _Float16 f16x8;
 
-__device__ __forceinline__ float widen(const void* p, int64_t i, int32_t type) {
-  if (type == PP_F16) return (float)((const _Float16*)p)[i];
-  if (type == PP_BF16) return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)p)[i] << 16);
-  return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)p)[i], 0);
+#define LDS_PTR(T, a) ((__attribute__((address_space(3))) T*)(uintptr_t)(a))
+
+constexpr int kWave = 64;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLag = 8.f;   // growth of the maximum, in the exponent, that is let pass
+
+extern __shared__ __attribute__((aligned(1024))) char g_lds[];
+
+__device__ __forceinline__ uint32_t lds_base() {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)g_lds;
 }
 
-// One wave a (token, query head), key by key.
-__global__ void __launch_bounds__(kWave) k_attend_row(pp_kv_pages p, pp_attention_args a, int shift) {
-  const int lane = threadIdx.x;
-  const int32_t t = blockIdx.x / a.q_heads, g = blockIdx.x % a.q_heads;
-  int32_t r = 0;
-  while (r + 1 < a.requests && a.query_start[r + 1] <= t) ++r;
-  const int32_t first = a.query_start[r], u = a.query_start[r + 1] - first;
-  if (t < first || t >= first + u) return;
-  const int64_t room = (int64_t)a.max_blocks << shift;
-  const int32_t pos = a.length[r] - u + (t - first);
-  const int h = g / (a.q_heads / p.heads);
-  const int64_t from = a.window && pos >= a.window ? pos - a.window + 1 : 0;
-  const int64_t to = pos + 1 < room ? pos + 1 : room;
-  const float ks = p.k_scale ? p.k_scale[h] : 1.f, vs = p.v_scale ? p.v_scale[h] : 1.f;
-  float q[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0;
-  for (int j = 0; j < p.dim / kWave; ++j)
-    q[j] = widen(a.q, t * a.q_token_stride + g * a.q_head_stride + j * kWave + lane, a.dtype);
-  for (int64_t k = from; k < to; ++k) {
-    int32_t page = a.block_table[r * a.row_stride + (k >> shift)];
-    page = page < 0 ? 0 : page < p.n_pages ? page : p.n_pages - 1;
-    const int64_t at = page * p.page_stride + h * p.head_stride +
-                       (k & (p.page_size - 1)) * p.token_stride + lane;
-    float s = 0;
-    for (int j = 0; j < p.dim / kWave; ++j) s += q[j] * widen(p.k, at + j * kWave, p.dtype);
-    for (int x = kWave / 2; x; x >>= 1) s += __shfl_xor(s, x);
-    s *= a.scale * ks;
-    const float n = fmaxf(m, s);
-    if (n == -INFINITY && s == s) continue;
-    const float w = m == -INFINITY ? 0.f : expf(m - n), e = expf(s - n);
-    l = l * w + e;
-    for (int j = 0; j < p.dim / kWave; ++j) o[j] = o[j] * w + e * widen(p.v, at + j * kWave, p.dtype);
-    m = n;
+// 16 bytes a lane from base + off straight into LDS at `to` + 16 * lane; counted in vmcnt like any
+// load, and the compiler is not told: wait_loads() before the reads.  (It keeps nothing in m0.)
+__device__ __forceinline__ void load_lds(uint32_t to, uint32_t off, const char* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(to), "v"(off), "s"(base) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ void barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma32(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Two floats rounded to nearest into the rows' type.
+template <bool F16>
+__device__ __forceinline__ int pack2(float x, float y) {
+  if constexpr (F16) {
+    f16x2 v = {(_Float16)x, (_Float16)y};
+    return __builtin_bit_cast(int, v);
+  } else {
+    bf16x2 v = {(__bf16)x, (__bf16)y};
+    return __builtin_bit_cast(int, v);
   }
-  for (int j = 0; j < p.dim / kWave; ++j) {
-    const float x = l == 0 ? 0.f : o[j] / l * vs;
-    const int64_t i = t * a.out_token_stride + g * a.out_head_stride + j * kWave + lane;
-    if (a.dtype == PP_F16) ((_Float16*)a.out)[i] = (_Float16)x;
-    else ((__bf16*)a.out)[i] = (__bf16)x;
+}
+
+template <bool F16>
+__device__ __forceinline__ s16x8 pack8(const float* x) {
+  i32x4 v;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = pack2<F16>(x[2 * j], x[2 * j + 1]);
+  return __builtin_bit_cast(s16x8, v);
+}
+
+// Eight e4m3 values widened to the rows' type (exact).
+template <bool F16>
+__device__ __forceinline__ s16x8 widen8(i32x2 x) {
+  i32x4 v;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if constexpr (F16) {
+      v[2 * j] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[j], 1.f, false));
+      v[2 * j + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[j], 1.f, true));
+    } else {
+      v[2 * j] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], 1.f, false));
+      v[2 * j + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], 1.f, true));
+    }
   }
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + g] = l == 0 ? -INFINITY : m + logf(l);
+  return __builtin_bit_cast(s16x8, v);
+}
+
+// A tile that some row does not see whole gives those keys a weight of 0, and 0 times an infinity
+// or NaN would still be NaN.  There V goes into the product with such values as 0, and where one
+// turned up, a second product counts them for the rows that do see them: +infinities as 1,
+// -infinities as 128, NaN as 16,384 (a tile has at most 64 keys, so the counts stay apart).
+template <bool F16>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {   // bit 15 and bit 31 for the two halves
+  if constexpr (F16) return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+  return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+
+template <bool F16>
+__device__ __forceinline__ s16x8 only_finite(s16x8 v, uint32_t& odd) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t n = not_finite<F16>(x[j]);
+    odd |= n;
+    x[j] &= ~((n >> 15) * 0xffffu);
+  }
+  return __builtin_bit_cast(s16x8, x);
+}
+
+template <bool F16>
+__device__ __forceinline__ s16x8 marks(s16x8 v) {
+  s16x8 o;
+  const uint16_t top = F16 ? 0x7c00 : 0x7f80;
+  const short one = F16 ? 0x3c00 : 0x3f80, b = F16 ? 0x5800 : 0x4300, c = F16 ? 0x7400 : 0x4680;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint16_t u = (uint16_t)v[j];
+    o[j] = (u & top) != top ? 0 : (u & 0x7fff) != top ? c : (u >> 15) ? b : one;
+  }
+  return o;
+}
+
+// 1 where the low bits say so.
+template <bool F16>
+__device__ __forceinline__ s16x8 ones8(uint32_t bits) {
+  s16x8 o;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] = (bits >> j & 1) ? (short)(F16 ? 0x3c00 : 0x3f80) : (short)0;
+  return o;
+}
+
+__device__ __forceinline__ float counted(float acc, float n) {
+  const int k = (int)n;
+  if (k & 127) acc += INFINITY;
+  if ((k >> 7) & 127) acc -= INFINITY;
+  if (k >> 14) acc += __builtin_nanf("");
+  return acc;
+}
+
+template <int MASK>
+__device__ __forceinline__ float swap_max(float x) { return fmaxf(x, __shfl_xor(x, MASK)); }
+
+// ------------------------------------------------------------- requests ---
+
+// How a call is split: requests of at most `few` rows go to k_rows, the others to k_tiles; a
+// request's keys are cut every `cut` keys, into at most `parts` parts of which the last is open.
+struct Plan {
+  int32_t few, group;
+  int32_t cut_rows, parts_rows, cut_tiles, parts_tiles;
+  int32_t slots;                 // tiles of rows at most, for k_tiles' grid
+  float c;                       // |scale| log2(e)
+  int32_t negative, shift;
+  float* part;                   // [parts][tokens * q_heads][dim], then the log sums
+  float* part_lse;               // [parts][tokens * q_heads]
+};
+
+struct Request {
+  int32_t first, count;          // its tokens
+  int32_t start;                 // position of the first one
+  int32_t lo, hi;                // keys any of its rows sees, lo a multiple of 64
+};
+
+__device__ __forceinline__ Request request(const pp_attention_args& a, const Plan& pl, int32_t r) {
+  Request q;
+  int32_t b = a.query_start[r], e = a.query_start[r + 1];
+  b = b < 0 ? 0 : b < a.tokens ? b : a.tokens;
+  e = e < b ? b : e < a.tokens ? e : a.tokens;
+  const int32_t len = a.length[r] > 0 ? a.length[r] : 0;
+  const int64_t room = (int64_t)a.max_blocks << pl.shift;
+  q.first = b;
+  q.count = e - b;
+  q.start = len - q.count;
+  q.hi = len < room ? len : (int32_t)room;
+  q.lo = a.window && q.start >= a.window ? (q.start - a.window + 1) & ~63 : 0;
+  return q;
+}
+
+__device__ __forceinline__ int32_t parts_of(const Request& q, int32_t cut, int32_t most) {
+  if (q.hi <= q.lo) return 1;
+  const int32_t n = (int32_t)(((int64_t)q.hi - q.lo + cut - 1) / cut);
+  return n < most ? n : most;
+}
+
+__device__ __forceinline__ bool sees(int32_t pos, int32_t key, int32_t window) {
+  return key <= pos && (window == 0 || (uint32_t)(pos - key) < (uint32_t)window);
+}
+
+// The last r with f(r) <= x, f increasing, f(0) <= x; all lanes active.
+template <class F>
+__device__ __forceinline__ int32_t find_last(int32_t count, int32_t x, F f) {
+  int32_t n = 0;
+  for (int32_t base = 0; base < count; base += kWave) {
+    const int32_t r = base + (int32_t)(threadIdx.x % kWave);
+    const int32_t k = __popcll(__ballot(r < count && f(r) <= x));
+    n += k;
+    if (k < kWave) break;
+  }
+  return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// Page numbers of 64 consecutive tiles of keys, one a lane.
+__device__ __forceinline__ int32_t page_of(const pp_kv_pages& p, const pp_attention_args& a,
+                                           const Plan& pl, int32_t r, int64_t key) {
+  const int64_t b = key >> pl.shift;
+  int32_t page = b < a.max_blocks ? a.block_table[r * a.row_stride + b] : 0;
+  return page < 0 ? 0 : page < p.n_pages ? page : p.n_pages - 1;
+}
+
+// Four neighbouring values of a row of out.
+template <bool F16>
+__device__ __forceinline__ void store4(const pp_attention_args& a, int32_t t, int32_t g, int32_t d, f32x4 x) {
+  const i32x2 v = {pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3])};
+  *(i32x2*)((uint16_t*)a.out + t * a.out_token_stride + g * a.out_head_stride + d) = v;
+}
+
+// ---------------------------------------------------------------- k_rows ---
+
+// Swizzles: the 16-byte unit u of a row lies at u ^ f(row), so that the rows a read takes together
+// fall into different banks.
+template <int RB>
+struct RowsSwizzle {
+  static constexpr int kUnits = RB / 16;
+  static __device__ __forceinline__ int k(int row) { return row & (kUnits < 16 ? kUnits - 1 : 15); }
+  static __device__ __forceinline__ int v(int row, bool narrow) {
+    if (narrow) return kUnits >= 8 ? (row & 3) | ((row >> 2) & 4) : row & 3;
+    return kUnits >= 16 ? (row & 7) * 2 : (row & 3) * 2;
+  }
+};
+
+template <bool NARROW, int D, int RT>
+struct RowsShape {
+  static constexpr int kRB = D * (NARROW ? 1 : 2);          // bytes of a row
+  static constexpr int kStage = 2 * 32 * kRB;               // K and V of 32 keys
+  static constexpr int kNW = kStage > 16384 ? 2 : 4;        // waves
+  static constexpr int kNS = kStage > 8192 ? 2 : 4;         // stages of a wave's ring
+  static constexpr int kRing = kNW * kNS * kStage;
+  static constexpr int kRow = D + 4;                        // floats of a joined row
+  static constexpr int kJoin = kNW * 16 * RT * (kRow + 2) * 4;
+  static constexpr int kLds = kRing > kJoin ? kRing : kJoin;
+};
+
+// One request, key head and part a block: up to 16 RT rows, in tiles of 16.
+template <bool F16, bool NARROW, int D, int RT>
+__global__ void __launch_bounds__((kWave * RowsShape<NARROW, D, RT>::kNW))
+k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
+  using Sh = RowsShape<NARROW, D, RT>;
+  using Sw = RowsSwizzle<Sh::kRB>;
+  constexpr int RB = Sh::kRB, UPR = RB / 16, NW = Sh::kNW, NS = Sh::kNS;
+  constexpr int kLoads = 32 * RB / 1024;                    // loads a matrix and tile
+  constexpr int kRowsPerLoad = 1024 / RB;
+  constexpr int DB = D / 16, KS = D / 32;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h = blockIdx.x % p.heads;
+  const int part = (blockIdx.x / p.heads) % pl.parts_rows;
+  const int32_t r = blockIdx.x / p.heads / pl.parts_rows;
+  const Request q = request(a, pl, r);
+  const int G = pl.group;
+  const int64_t rows64 = (int64_t)q.count * G;
+  if (rows64 == 0 || rows64 > pl.few) return;
+  const int32_t rows = (int32_t)rows64;
+  const int32_t parts = parts_of(q, pl.cut_rows, pl.parts_rows);
+  if (part >= parts) return;
+  int64_t k0 = q.lo + (int64_t)part * pl.cut_rows;
+  int64_t k1 = part + 1 < parts ? k0 + pl.cut_rows : q.hi;
+  if (k1 > q.hi) k1 = q.hi;
+  const int32_t tiles = k1 > k0 ? (int32_t)((k1 - k0 + 31) / 32) : 0;
+  const int32_t each = (tiles + NW - 1) / NW;
+  const int32_t t0 = wave * each < tiles ? wave * each : tiles;
+  const int32_t nt = t0 + each < tiles ? each : tiles - t0;
+  const int32_t kbase = (int32_t)k0 + t0 * 32;
+
+  // this lane's row of each tile of rows: its token's position, or -1
+  int32_t pos[RT];
+  s16x8 qf[RT][KS];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int32_t row = rt * 16 + lane % 16;
+    const int32_t tok = row / G, g = h * G + row % G;
+    pos[rt] = row < rows ? q.start + tok : -1;
+    const uint16_t* src = (const uint16_t*)a.q + (q.first + (row < rows ? tok : 0)) * a.q_token_stride +
+                          (row < rows ? g : h * G) * a.q_head_stride + (lane / 16) * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      i32x4 x = *(const i32x4*)(src + ks * 32);
+      if (pl.negative) x ^= (int)0x80008000;
+      qf[rt][ks] = __builtin_bit_cast(s16x8, x);
+    }
+  }
+  const float c = pl.c * (NARROW && p.k_scale ? p.k_scale[h] : 1.f);
+
+  const int64_t es = NARROW ? 1 : 2;
+  const int64_t page_b = p.page_stride * es, tok_b = p.token_stride * es;
+  const char* kh = (const char*)p.k + h * p.head_stride * es;
+  const char* vh = (const char*)p.v + h * p.head_stride * es;
+  const uint32_t ring = lds_base() + wave * (NS * Sh::kStage);
+  // this lane's source in a group of 16 keys, load by load
+  constexpr int kPer16 = kLoads / 2;
+  uint32_t koff[kPer16], voff[2][kPer16];
+#pragma unroll
+  for (int i = 0; i < kPer16; ++i) {
+    const int row = i * kRowsPerLoad + lane / UPR;
+    koff[i] = (uint32_t)(row * tok_b) + ((lane % UPR) ^ Sw::k(row)) * 16;
+    voff[0][i] = (uint32_t)(row * tok_b) + ((lane % UPR) ^ Sw::v(row, NARROW)) * 16;
+    voff[1][i] = (uint32_t)(row * tok_b) + ((lane % UPR) ^ Sw::v(row + 16, NARROW)) * 16;
+  }
+  int32_t held = 0;
+  auto issue = [&](int32_t t) {
+    const uint32_t to = ring + (t % NS) * Sh::kStage;
+    if ((t & 31) == 0) held = page_of(p, a, pl, r, (int64_t)kbase + (t + lane / 2) * 32 + (lane & 1) * 16);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int64_t page = __builtin_amdgcn_readlane(held, (t & 31) * 2 + half);
+      const int64_t at = page * page_b + ((kbase + t * 32 + half * 16) & (p.page_size - 1)) * tok_b;
+#pragma unroll
+      for (int i = 0; i < kPer16; ++i)
+        load_lds(to + half * 16 * RB + i * 1024, koff[i], kh + at);
+#pragma unroll
+      for (int i = 0; i < kPer16; ++i)
+        load_lds(to + 32 * RB + half * 16 * RB + i * 1024, voff[half][i], vh + at);
+    }
+  };
+
+  f32x4 acc[RT][DB];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = -INFINITY;
+    l[rt] = 0;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[rt][d] = f32x4{0, 0, 0, 0};
+  }
+  // reads: K row lane % 16, its units lane / 16 + 4 ks; V four keys a 16-lane group, transposed
+  const int grp = lane / 16, i16 = lane % 16;
+  const uint32_t krow = i16 * RB;
+  const uint32_t kx = NARROW ? ((grp / 2) ^ Sw::k(i16)) * 16 + (grp % 2) * 8 : (grp ^ Sw::k(i16)) * 16;
+  const int vrow = NARROW ? ((i16 / 2) / 4) * 16 + 4 * grp + (i16 / 2) % 4 : 4 * grp + i16 / 4;
+  const uint32_t vat = vrow * RB;
+  const uint32_t vx = NARROW ? Sw::v(vrow, true) * 16 + (i16 % 2) * 8
+                             : (((i16 % 4) / 2) ^ Sw::v(vrow, false)) * 16 + (i16 % 2) * 8;
+  const int32_t pos_lo = q.start;   // the first row's; rows of -1 see nothing in any case
+  const int32_t pos_hi = q.start + q.count - 1;
+
+  for (int32_t t = 0; t < NS - 1 && t < nt; ++t) issue(t);
+  for (int32_t t = 0; t < nt; ++t) {
+    if (t + NS - 1 < nt) {
+      issue(t + NS - 1);
+      wait_loads<(NS - 1) * 2 * kLoads>();
+    } else if (NS > 3 && t + NS - 2 < nt) {
+      wait_loads<(NS > 2 ? NS - 2 : 0) * 2 * kLoads>();
+    } else if (NS > 2 && t + NS - 3 < nt) {
+      wait_loads<(NS > 3 ? NS - 3 : 0) * 2 * kLoads>();
+    } else {
+      wait_loads<0>();
+    }
+    const uint32_t kt = ring + (t % NS) * Sh::kStage, vt = kt + 32 * RB;
+    f32x4 s[RT][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt][kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s16x8 f;
+        if constexpr (NARROW)
+          f = widen8<F16>(*LDS_PTR(i32x2, kt + kb * 16 * RB + krow + (kx ^ (ks * 32))));
+        else
+          f = *LDS_PTR(s16x8, kt + kb * 16 * RB + krow + (kx ^ (ks * 64)));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][kb] = mfma16<F16>(f, qf[rt][ks], s[rt][kb]);
+      }
+    }
+    const int32_t key0 = kbase + t * 32 + 4 * grp;   // of s[.][0][0]; + 16 kb + i
+    const bool part_seen = kbase + t * 32 + 31 > pos_lo || kbase + t * 32 + 31 >= k1 ||
+                           (a.window && kbase + t * 32 <= (int64_t)pos_hi - a.window);
+    s16x8 pf[RT];
+    uint32_t seen[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float x[8], w[8];
+      seen[rt] = 0xff;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = s[rt][j / 4][j % 4];
+      if (part_seen) {
+        seen[rt] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int32_t key = key0 + (j / 4) * 16 + j % 4;
+          const bool ok = sees(pos[rt], key, a.window) && key < k1;
+          seen[rt] |= ok ? 1u << j : 0;
+          if (!ok) x[j] = -INFINITY;
+        }
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
+      mx = swap_max<16>(mx);
+      mx = swap_max<32>(mx);
+      const bool grow = mx > m[rt] && (m[rt] == -INFINITY || (mx - m[rt]) * c > kLag);
+      if (__any(grow)) {
+        const float n = fmaxf(m[rt], mx);
+        const float al = m[rt] == -INFINITY ? 0.f : exp2_((m[rt] - n) * c);
+        l[rt] *= al;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[rt][d] *= al;
+        m[rt] = n;
+      }
+      const float mc = m[rt] == -INFINITY ? 0.f : m[rt] * c;
+      float sum = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = exp2_(__builtin_fmaf(x[j], c, -mc));
+        if (part_seen && !(seen[rt] >> j & 1)) w[j] = 0;
+        sum += w[j];
+      }
+      l[rt] += sum;
+      pf[rt] = pack8<F16>(w);
+    }
+    auto v_frag = [&](int db) -> s16x8 {
+      if constexpr (NARROW) {
+        return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            LDS_PTR(i32x2, vt + vat + (vx ^ (db * 16))))));
+      } else {
+        const uint32_t at = vt + vat + (vx ^ (db * 32));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 16 * RB));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    };
+    if (!part_seen) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const s16x8 f = v_frag(db);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt][db] = mfma16<F16>(f, pf[rt], acc[rt][db]);
+      }
+    } else {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const s16x8 f = only_finite<F16>(v_frag(db), odd);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt][db] = mfma16<F16>(f, pf[rt], acc[rt][db]);
+      }
+      if (__any(odd != 0)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const s16x8 f = marks<F16>(v_frag(db));
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const f32x4 n = mfma16<F16>(f, ones8<F16>(seen[rt]), f32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[rt][db][i] = counted(acc[rt][db][i], n[i]);
+          }
+        }
+      }
+    }
+    wait_lds();   // this stage's reads are done before its next load is issued
+  }
+
+  // the waves' parts of the rows are joined in LDS
+  barrier();
+  constexpr int R16 = 16 * RT;
+  float* js = (float*)g_lds;                       // [NW][R16][kRow]
+  float* jm = js + NW * R16 * Sh::kRow;            // [NW][R16]
+  float* jl = jm + NW * R16;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float ls = l[rt] + __shfl_xor(l[rt], 16);
+    ls += __shfl_xor(ls, 32);
+    const int row = rt * 16 + i16;
+    if (grp == 0) {
+      jm[wave * R16 + row] = m[rt];
+      jl[wave * R16 + row] = ls;
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      *(f32x4*)&js[(wave * R16 + row) * Sh::kRow + db * 16 + grp * 4] = acc[rt][db];
+  }
+  __syncthreads();
+  const float vs = NARROW && p.v_scale ? p.v_scale[h] : 1.f;
+  for (int i = threadIdx.x; i < rows * (D / 4); i += NW * kWave) {
+    const int row = i / (D / 4), d = i % (D / 4) * 4;
+    float mm = -INFINITY, ll = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, jm[w * R16 + row]);
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float mw = jm[w * R16 + row], lw = jl[w * R16 + row];
+      if (lw == 0) continue;      // it saw nothing
+      const float f = mw == mm ? 1.f : exp2_((mw - mm) * c);
+      ll += f * lw;
+      o += f * *(const f32x4*)&js[(w * R16 + row) * Sh::kRow + d];
+    }
+    const float inv = ll == 0 ? 0.f : vs / ll;
+    o *= inv;
+    const float lse = ll == 0 ? -INFINITY : mm * c + __log2f(ll);
+    const int32_t tk = q.first + row / G, g = h * G + row % G;
+    if (parts == 1) {
+      store4<F16>(a, tk, g, d, o);
+      if (a.lse && d == 0) a.lse[(int64_t)tk * a.q_heads + g] = lse / kLog2e;
+    } else {
+      const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
+      *(f32x4*)&pl.part[at * D + d] = o;
+      if (d == 0) pl.part_lse[at] = lse;
+    }
+  }
+}
+
+// --------------------------------------------------------------- k_tiles ---
+
+template <int RB>
+struct TilesSwizzle {
+  static constexpr int kUnits = RB / 16;
+  static __device__ __forceinline__ int k(int row) { return row & (kUnits < 16 ? kUnits - 1 : 15); }
+  static __device__ __forceinline__ int v(int row, bool narrow) {
+    if (narrow) return kUnits >= 8 ? (row & 3) | ((row >> 1) & 4) : row & 3;
+    return kUnits >= 16 ? (row & 3) * 4 + (row & 2) : (row & 3) * 2;
+  }
+};
+
+template <bool NARROW, int D>
+constexpr int kTilesLds = 2 * 2 * 64 * D * (NARROW ? 1 : 2);
+
+// 128 rows of one request and key head, and one part of its keys, a block.
+template <bool F16, bool NARROW, int D>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2)
+k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
+  constexpr int RB = D * (NARROW ? 1 : 2), UPR = RB / 16;
+  using Sw = TilesSwizzle<RB>;
+  constexpr int kLoads = 16 * RB / 1024, kRowsPerLoad = 1024 / RB;
+  constexpr int DB = D / 32, KS = D / 16;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h = blockIdx.x % p.heads;
+  const int part = (blockIdx.x / p.heads) % pl.parts_tiles;
+  const int32_t slot = blockIdx.x / p.heads / pl.parts_tiles;
+  const int G = pl.group;
+  // request r's tiles start at slot floor(first token * G / 128) + r, which leaves it enough of them
+  auto base_of = [&](int32_t r) { return (int32_t)((int64_t)a.query_start[r] * G / 128) + r; };
+  const int32_t r = find_last(a.requests, slot, base_of);
+  if (r < 0 || base_of(r) > slot) return;
+  const Request q = request(a, pl, r);
+  const int64_t rows = (int64_t)q.count * G;
+  const int64_t row0 = (int64_t)(slot - base_of(r)) * 128;
+  if (rows <= pl.few || row0 >= rows) return;
+  const int32_t parts = parts_of(q, pl.cut_tiles, pl.parts_tiles);
+  if (part >= parts) return;
+
+  const int64_t row = row0 + wave * 32 + lane % 32;
+  const bool live = row < rows;
+  const int32_t tok = (int32_t)((live ? row : 0) / G), g = h * G + (int32_t)((live ? row : 0) % G);
+  const int32_t pos = live ? q.start + tok : -1;
+  const int half = lane / 32;
+
+  // keys of this part that the tile's rows see
+  const int32_t tok_lo = (int32_t)(row0 / G);
+  const int64_t last = row0 + 127 < rows ? row0 + 127 : rows - 1;
+  const int32_t pos_lo = q.start + tok_lo, pos_hi = q.start + (int32_t)(last / G);
+  int64_t k0 = q.lo + (int64_t)part * pl.cut_tiles;
+  int64_t k1 = part + 1 < parts ? k0 + pl.cut_tiles : q.hi;
+  if (k1 > (int64_t)pos_hi + 1) k1 = (int64_t)pos_hi + 1;
+  if (k1 > q.hi) k1 = q.hi;
+  if (a.window && (int64_t)pos_lo - a.window + 1 > k0) k0 = (pos_lo - a.window + 1) & ~63;
+  const int32_t nt = k1 > k0 ? (int32_t)((k1 - k0 + 63) / 64) : 0;
+  const int32_t kbase = (int32_t)k0;
+
+  s16x8 qf[KS];
+  {
+    const uint16_t* src = (const uint16_t*)a.q + (q.first + tok) * a.q_token_stride + g * a.q_head_stride + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      i32x4 x = *(const i32x4*)(src + ks * 16);
+      if (pl.negative) x ^= (int)0x80008000;
+      qf[ks] = __builtin_bit_cast(s16x8, x);
+    }
+  }
+  const float c = pl.c * (NARROW && p.k_scale ? p.k_scale[h] : 1.f);
+
+  const int64_t es = NARROW ? 1 : 2;
+  const int64_t page_b = p.page_stride * es, tok_b = p.token_stride * es;
+  const char* kh = (const char*)p.k + h * p.head_stride * es;
+  const char* vh = (const char*)p.v + h * p.head_stride * es;
+  constexpr uint32_t kTile = 64 * RB;
+  const uint32_t lds = lds_base();
+  uint32_t koff[kLoads], voff[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int rr = i * kRowsPerLoad + lane / UPR;          // + 16 wave: no swizzle reads that bit
+    koff[i] = (uint32_t)(rr * tok_b) + ((lane % UPR) ^ Sw::k(rr)) * 16;
+    voff[i] = (uint32_t)(rr * tok_b) + ((lane % UPR) ^ Sw::v(rr, NARROW)) * 16;
+  }
+  int32_t held = 0;
+  auto issue = [&](int32_t t) {   // wave w brings keys 16 w .. 16 w + 15 of the tile
+    const uint32_t to = lds + (t & 1) * 2 * kTile + wave * 16 * RB;
+    if ((t & 63) == 0) held = page_of(p, a, pl, r, (int64_t)kbase + (t + lane) * 64 + wave * 16);
+    const int64_t page = __builtin_amdgcn_readlane(held, t & 63);
+    const int64_t at = page * page_b + ((kbase + t * 64 + wave * 16) & (p.page_size - 1)) * tok_b;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_lds(to + i * 1024, koff[i], kh + at);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_lds(to + kTile + i * 1024, voff[i], vh + at);
+  };
+
+  f32x16 acc[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0;
+  float m = -INFINITY, l = 0;
+
+  const int l32 = lane % 32, i16 = lane % 16, dh = (lane / 16) % 2;
+  const uint32_t krow = l32 * RB;
+  const uint32_t kx = NARROW ? Sw::k(l32) * 16 + half * 8 : (half ^ Sw::k(l32)) * 16;
+  const int vrow = NARROW ? ((i16 / 2) / 4) * 8 + 4 * half + (i16 / 2) % 4 : 4 * half + i16 / 4;
+  const uint32_t vat = vrow * RB;
+  const uint32_t vx = NARROW ? (dh ^ Sw::v(vrow, true)) * 16 + (i16 % 2) * 8
+                             : ((dh * 2 + (i16 % 4) / 2) ^ Sw::v(vrow, false)) * 16 + (i16 % 2) * 8;
+
+  if (nt > 0) issue(0);
+  for (int32_t t = 0; t < nt; ++t) {
+    wait_loads<0>();
+    barrier();                    // every wave's keys are there, and the other buffer is read
+    if (t + 1 < nt) issue(t + 1);
+    const uint32_t kt = lds + (t & 1) * 2 * kTile, vt = kt + kTile;
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s16x8 f;
+        if constexpr (NARROW)
+          f = widen8<F16>(*LDS_PTR(i32x2, kt + kb * 32 * RB + krow + (kx ^ (ks * 16))));
+        else
+          f = *LDS_PTR(s16x8, kt + kb * 32 * RB + krow + (kx ^ (ks * 32)));
+        s[kb] = mfma32<F16>(f, qf[ks], s[kb]);
+      }
+    }
+    const int32_t tile0 = kbase + t * 64;
+    const bool part_seen = tile0 + 63 > pos_lo || tile0 + 63 >= k1 || (a.window && tile0 <= (int64_t)pos_hi - a.window);
+    uint32_t seen = ~0u;
+    if (part_seen) {
+      seen = 0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        const int32_t key = tile0 + (j / 16) * 32 + (j % 16 / 4) * 8 + 4 * half + j % 4;
+        const bool ok = sees(pos, key, a.window) && key < k1;
+        seen |= ok ? 1u << j : 0;
+        if (!ok) s[j / 16][j % 16] = -INFINITY;
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j / 16][j % 16]);
+    mx = swap_max<32>(mx);
+    const bool grow = mx > m && (m == -INFINITY || (mx - m) * c > kLag);
+    if (__any(grow)) {
+      const float n = fmaxf(m, mx);
+      const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) acc[d] *= al;
+      m = n;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+    s16x8 pf[4];
+    float sum = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = exp2_(__builtin_fmaf(s[k / 2][k % 2 * 8 + j], c, -mc));
+        if (part_seen && !(seen >> (k * 8 + j) & 1)) w[j] = 0;
+        sum += w[j];
+      }
+      pf[k] = pack8<F16>(w);
+    }
+    l += sum;
+    // keys 16 k + 8 (j / 4) + 4 half + j % 4 of the tile, as the weights' registers have them
+    auto v_frag = [&](int db, int k) -> s16x8 {
+      if constexpr (NARROW) {
+        return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            LDS_PTR(i32x2, vt + k * 16 * RB + vat + (vx ^ (db * 32))))));
+      } else {
+        const uint32_t at = vt + k * 16 * RB + vat + (vx ^ (db * 64));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 8 * RB));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    };
+    if (!part_seen) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[db] = mfma32<F16>(v_frag(db, k), pf[k], acc[db]);
+    } else {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[db] = mfma32<F16>(only_finite<F16>(v_frag(db, k), odd), pf[k], acc[db]);
+      if (__any(odd != 0)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          f32x16 n;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) n[i] = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            n = mfma32<F16>(marks<F16>(v_frag(db, k)), ones8<F16>(seen >> (k * 8)), n);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[db][i] = counted(acc[db][i], n[i]);
+        }
+      }
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  if (!live) return;
+  const float vs = NARROW && p.v_scale ? p.v_scale[h] : 1.f;
+  const float inv = l == 0 ? 0.f : vs / l;
+  const float lse = l == 0 ? -INFINITY : m * c + __log2f(l);
+  const int32_t tk = q.first + tok;
+  const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      f32x4 o = {acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]};
+      o = l == 0 ? f32x4{0, 0, 0, 0} : o * inv;
+      const int d = db * 32 + b * 8 + half * 4;
+      if (parts == 1) store4<F16>(a, tk, g, d, o);
+      else *(f32x4*)&pl.part[at * D + d] = o;
+    }
+  if (half == 0) {
+    if (parts > 1) pl.part_lse[at] = lse;
+    else if (a.lse) a.lse[(int64_t)tk * a.q_heads + g] = lse / kLog2e;
+  }
+}
+
+// ---------------------------------------------------------------- k_join ---
+
+// One wave a (token, query head) of a request in several parts.
+template <bool F16, int D>
+__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (at >= (int64_t)a.tokens * a.q_heads) return;
+  const int32_t t = (int32_t)(at / a.q_heads), g = (int32_t)(at % a.q_heads);
+  const int32_t r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
+  if (r < 0) return;
+  const Request q = request(a, pl, r);
+  if (t >= q.first + q.count) return;
+  const bool small = (int64_t)q.count * pl.group <= pl.few;
+  const int32_t parts = small ? parts_of(q, pl.cut_rows, pl.parts_rows) : parts_of(q, pl.cut_tiles, pl.parts_tiles);
+  if (parts == 1) return;
+  const int64_t step = (int64_t)a.tokens * a.q_heads;
+  float mm = -INFINITY;
+  for (int32_t i = lane; i < parts; i += kWave) mm = fmaxf(mm, pl.part_lse[i * step + at]);
+  for (int o = kWave / 2; o; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
+  constexpr int N = D / kWave;
+  float o[N] = {}, sum = 0;
+  for (int32_t i = 0; i < parts; ++i) {
+    const float x = pl.part_lse[i * step + at];
+    if (x == -INFINITY) continue;
+    const float w = x == mm ? 1.f : exp2_(x - mm);
+    sum += w;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] += w * pl.part[(i * step + at) * D + lane * N + j];
+  }
+  uint16_t* out = (uint16_t*)a.out + t * a.out_token_stride + g * a.out_head_stride + lane * N;
+  const float inv = sum == 0 ? 0.f : 1.f / sum;
+  if constexpr (N == 1) {
+    out[0] = (uint16_t)pack2<F16>(o[0] * inv, 0.f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) *(int*)(out + j) = pack2<F16>(o[j] * inv, o[j + 1] * inv);
+  }
+  if (a.lse && lane == 0) a.lse[at] = sum == 0 ? -INFINITY : (mm + __log2f(sum)) / kLog2e;
+}
+
+// -------------------------------------------------------------- dispatch ---
+
+constexpr int kFill = 1024;     // blocks a call is cut towards
+
+int32_t round_up(int64_t x, int32_t m) { return (int32_t)((x + m - 1) / m * m); }
+
+struct Choice {
+  int rt;                       // tiles of 16 rows in k_rows, 0 = not launched
+  bool tiles, join;
+};
+
+// Every rule here goes by sizes the host knows, so the workspace is known before the call.
+Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
+  Choice ch{};
+  pl.group = a.q_heads / p.heads;
+  pl.shift = __builtin_ctz(p.page_size);
+  const int most = p.dim == 256 ? 32 : 64;      // rows k_rows has registers for
+  const int64_t rows = (int64_t)a.max_new * pl.group;
+  auto tiles16 = [](int64_t n) { return n <= 16 ? 1 : n <= 32 ? 2 : 4; };
+  if (rows <= most) {
+    ch.rt = tiles16(rows);
+  } else {
+    ch.tiles = true;
+    // single tokens apart, unless every request has max_new tokens
+    if (pl.group <= most && (int64_t)a.requests * a.max_new != a.tokens) ch.rt = tiles16(pl.group);
+  }
+  pl.few = ch.rt * 16;
+  const int64_t keys = a.max_len > 1 ? a.max_len : 1;
+  auto cut = [&](int64_t blocks, int32_t unit, int32_t least, int32_t& size, int32_t& parts) {
+    int64_t want = (kFill + blocks - 1) / blocks;
+    int64_t c = (keys + want - 1) / want;
+    if (c < least) c = least;
+    size = round_up(c, unit);
+    parts = (int32_t)((keys + size - 1) / size);
+  };
+  pl.parts_rows = pl.parts_tiles = 1;
+  pl.cut_rows = pl.cut_tiles = round_up(keys, 128);
+  if (ch.rt) cut((int64_t)a.requests * p.heads, 128, 256, pl.cut_rows, pl.parts_rows);
+  pl.slots = (int32_t)((int64_t)a.tokens * pl.group / 128) + a.requests;
+  if (ch.tiles) cut((int64_t)a.tokens * pl.group / 128 * p.heads + 1, 64, 512, pl.cut_tiles, pl.parts_tiles);
+  ch.join = (ch.rt && pl.parts_rows > 1) || (ch.tiles && pl.parts_tiles > 1);
+  return ch;
+}
+
+int64_t part_floats(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl) {
+  const int64_t parts = pl.parts_rows > pl.parts_tiles ? pl.parts_rows : pl.parts_tiles;
+  return parts * a.tokens * a.q_heads;
+}
+
+template <class K>
+hipError_t allow_lds(K kern, int bytes) {
+  return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <bool F16, bool NARROW, int D, int RT>
+hipError_t go_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, hipStream_t st) {
+  constexpr int lds = RowsShape<NARROW, D, RT>::kLds;
+  static const hipError_t ok = allow_lds(&k_rows<F16, NARROW, D, RT>, lds);
+  if (ok != hipSuccess) return ok;
+  const int64_t grid = (int64_t)a.requests * pl.parts_rows * p.heads;
+  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  k_rows<F16, NARROW, D, RT><<<(unsigned)grid, kWave * RowsShape<NARROW, D, RT>::kNW, lds, st>>>(p, a, pl);
+  return hipGetLastError();
+}
+
+template <bool F16, bool NARROW, int D>
+hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, const Choice& ch, hipStream_t st) {
+  if (ch.tiles) {
+    constexpr int lds = kTilesLds<NARROW, D>;
+    static const hipError_t ok = allow_lds(&k_tiles<F16, NARROW, D>, lds);
+    if (ok != hipSuccess) return ok;
+    const int64_t grid = (int64_t)pl.slots * pl.parts_tiles * p.heads;
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    k_tiles<F16, NARROW, D><<<(unsigned)grid, 256, lds, st>>>(p, a, pl);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipError_t e = hipSuccess;
+  if (ch.rt == 1) e = go_rows<F16, NARROW, D, 1>(p, a, pl, st);
+  if (ch.rt == 2) e = go_rows<F16, NARROW, D, 2>(p, a, pl, st);
+  if constexpr (D < 256)
+    if (ch.rt == 4) e = go_rows<F16, NARROW, D, 4>(p, a, pl, st);
+  if (e != hipSuccess) return e;
+  if (ch.join) {
+    const int64_t rows = (int64_t)a.tokens * a.q_heads;
+    k_join<F16, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pl);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <bool F16, bool NARROW>
+hipError_t go_dim(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, const Choice& ch, hipStream_t st) {
+  if (p.dim == 64) return go<F16, NARROW, 64>(p, a, pl, ch, st);
+  if (p.dim == 128) return go<F16, NARROW, 128>(p, a, pl, ch, st);
+  return go<F16, NARROW, 256>(p, a, pl, ch, st);
 }
 
 }  // namespace
 
-int64_t attention_workspace(const pp_kv_pages&, const pp_attention_args&) { return 0; }
+int64_t attention_workspace(const pp_kv_pages& p, const pp_attention_args& a) {
+  Plan pl{};
+  const Choice ch = choose(p, a, pl);
+  return ch.join ? part_floats(p, a, pl) * (p.dim + 1) * 4 : 0;
+}
 
 hipError_t launch_attention(const pp_kv_pages& p, const pp_attention_args& a, hipStream_t st) {
-  k_attend_row<<<a.tokens * a.q_heads, kWave, 0, st>>>(p, a, __builtin_ctz(p.page_size));
-  return hipGetLastError();
+  Plan pl{};
+  const Choice ch = choose(p, a, pl);
+  pl.negative = a.scale < 0;
+  pl.c = (a.scale < 0 ? -a.scale : a.scale) * kLog2e;
+  pl.part = (float*)a.workspace;
+  pl.part_lse = pl.part + part_floats(p, a, pl) * p.dim;
+  const bool narrow = p.dtype == PP_E4M3;
+  if (a.dtype == PP_F16) return narrow ? go_dim<true, true>(p, a, pl, ch, st) : go_dim<true, false>(p, a, pl, ch, st);
+  return narrow ? go_dim<false, true>(p, a, pl, ch, st) : go_dim<false, false>(p, a, pl, ch, st);
 }
 
 }  // namespace pp
