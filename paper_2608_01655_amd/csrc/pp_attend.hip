@@ -23,6 +23,8 @@
 
 #include "pp_serve.h"
 
+#include <type_traits>
+
 namespace pp {
 
 namespace {
@@ -177,8 +179,27 @@ __device__ __forceinline__ float counted(float acc, float n) {
   return acc;
 }
 
-template <int MASK>
-__device__ __forceinline__ float swap_max(float x) { return fmaxf(x, __shfl_xor(x, MASK)); }
+// Over the two halves of the wave, and over the two 16-lane rows of each half.
+template <class F>
+__device__ __forceinline__ float over_halves(float x, F f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto v = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return f(__builtin_bit_cast(float, (uint32_t)v[0]), __builtin_bit_cast(float, (uint32_t)v[1]));
+}
+
+template <class F>
+__device__ __forceinline__ float over_rows(float x, F f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto v = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return f(__builtin_bit_cast(float, (uint32_t)v[0]), __builtin_bit_cast(float, (uint32_t)v[1]));
+}
+
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Sum {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
 
 // ------------------------------------------------------------- requests ---
 
@@ -223,6 +244,27 @@ __device__ __forceinline__ int32_t parts_of(const Request& q, int32_t cut, int32
 
 __device__ __forceinline__ bool sees(int32_t pos, int32_t key, int32_t window) {
   return key <= pos && (window == 0 || (uint32_t)(pos - key) < (uint32_t)window);
+}
+
+// Of nt tiles of N keys from `key` on: tiles whole .. tail - 1 are seen whole by every row.
+struct Span3 {
+  int32_t whole, tail;
+};
+
+template <int N>
+__device__ __forceinline__ Span3 spans(int32_t key, int32_t nt, int32_t pos_lo, int32_t pos_hi, int32_t k1,
+                                       int32_t window) {
+  int64_t w = 0;
+  if (window) {                                       // tiles with a key <= pos_hi - window
+    w = (int64_t)pos_hi - window - key;
+    w = w < 0 ? 0 : w / N + 1;
+  }
+  int64_t e = pos_lo + 1 < k1 ? pos_lo + 1 : k1;      // keys before e are seen, but for the window
+  e = e <= key ? 0 : (e - key) / N;
+  Span3 s;
+  s.whole = __builtin_amdgcn_readfirstlane((int32_t)(w < nt ? w : nt));
+  s.tail = __builtin_amdgcn_readfirstlane((int32_t)(e < nt ? e : nt));
+  return s;
 }
 
 // The last r with f(r) <= x, f increasing, f(0) <= x; all lanes active.
@@ -380,8 +422,8 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
   const int32_t pos_lo = q.start;   // the first row's; rows of -1 see nothing in any case
   const int32_t pos_hi = q.start + q.count - 1;
 
-  for (int32_t t = 0; t < NS - 1 && t < nt; ++t) issue(t);
-  for (int32_t t = 0; t < nt; ++t) {
+  auto tile = [&](int32_t t, auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;   // some row does not see all of it
     if (t + NS - 1 < nt) {
       issue(t + NS - 1);
       wait_loads<(NS - 1) * 2 * kLoads>();
@@ -410,8 +452,6 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
       }
     }
     const int32_t key0 = kbase + t * 32 + 4 * grp;   // of s[.][0][0]; + 16 kb + i
-    const bool part_seen = kbase + t * 32 + 31 > pos_lo || kbase + t * 32 + 31 >= k1 ||
-                           (a.window && kbase + t * 32 <= (int64_t)pos_hi - a.window);
     s16x8 pf[RT];
     uint32_t seen[RT];
 #pragma unroll
@@ -420,7 +460,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
       seen[rt] = 0xff;
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = s[rt][j / 4][j % 4];
-      if (part_seen) {
+      if constexpr (kMasked) {
         seen[rt] = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -433,8 +473,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
       float mx = x[0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
-      mx = swap_max<16>(mx);
-      mx = swap_max<32>(mx);
+      mx = over_halves(over_rows(mx, Max()), Max());
       const bool grow = mx > m[rt] && (m[rt] == -INFINITY || (mx - m[rt]) * c > kLag);
       if (__any(grow)) {
         const float n = fmaxf(m[rt], mx);
@@ -449,7 +488,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         w[j] = exp2_(__builtin_fmaf(x[j], c, -mc));
-        if (part_seen && !(seen[rt] >> j & 1)) w[j] = 0;
+        if (kMasked && !(seen[rt] >> j & 1)) w[j] = 0;
         sum += w[j];
       }
       l[rt] += sum;
@@ -466,7 +505,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     };
-    if (!part_seen) {
+    if constexpr (!kMasked) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const s16x8 f = v_frag(db);
@@ -495,6 +534,16 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
       }
     }
     wait_lds();   // this stage's reads are done before its next load is issued
+  };
+  // tiles before `whole` start before the last row's window, those from `tail` on end past what the
+  // first row sees or past the keys
+  const Span3 sp = spans<32>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
+  for (int32_t t = 0; t < NS - 1 && t < nt; ++t) issue(t);
+  int32_t t = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (const int32_t e = pass ? nt : sp.whole; t < e; ++t) tile(t, std::true_type());
+    if (pass == 0)
+      for (; t < sp.tail; ++t) tile(t, std::false_type());
   }
 
   // the waves' parts of the rows are joined in LDS
@@ -505,8 +554,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
   float* jl = jm + NW * R16;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float ls = l[rt] + __shfl_xor(l[rt], 16);
-    ls += __shfl_xor(ls, 32);
+    const float ls = over_halves(over_rows(l[rt], Sum()), Sum());
     const int row = rt * 16 + i16;
     if (grp == 0) {
       jm[wave * R16 + row] = m[rt];
@@ -656,8 +704,8 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   const uint32_t vx = NARROW ? (dh ^ Sw::v(vrow, true)) * 16 + (i16 % 2) * 8
                              : ((dh * 2 + (i16 % 4) / 2) ^ Sw::v(vrow, false)) * 16 + (i16 % 2) * 8;
 
-  if (nt > 0) issue(0);
-  for (int32_t t = 0; t < nt; ++t) {
+  auto tile = [&](int32_t t, auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;   // some row does not see all of it
     wait_loads<0>();
     barrier();                    // every wave's keys are there, and the other buffer is read
     if (t + 1 < nt) issue(t + 1);
@@ -678,9 +726,8 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
       }
     }
     const int32_t tile0 = kbase + t * 64;
-    const bool part_seen = tile0 + 63 > pos_lo || tile0 + 63 >= k1 || (a.window && tile0 <= (int64_t)pos_hi - a.window);
     uint32_t seen = ~0u;
-    if (part_seen) {
+    if constexpr (kMasked) {
       seen = 0;
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
@@ -693,7 +740,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     float mx = s[0][0];
 #pragma unroll
     for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j / 16][j % 16]);
-    mx = swap_max<32>(mx);
+    mx = over_halves(mx, Max());
     const bool grow = mx > m && (m == -INFINITY || (mx - m) * c > kLag);
     if (__any(grow)) {
       const float n = fmaxf(m, mx);
@@ -712,7 +759,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         w[j] = exp2_(__builtin_fmaf(s[k / 2][k % 2 * 8 + j], c, -mc));
-        if (part_seen && !(seen >> (k * 8 + j) & 1)) w[j] = 0;
+        if (kMasked && !(seen >> (k * 8 + j) & 1)) w[j] = 0;
         sum += w[j];
       }
       pf[k] = pack8<F16>(w);
@@ -730,7 +777,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     };
-    if (!part_seen) {
+    if constexpr (!kMasked) {
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -747,34 +794,41 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
           f32x16 n;
 #pragma unroll
           for (int i = 0; i < 16; ++i) n[i] = 0;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            n = mfma32<F16>(marks<F16>(v_frag(db, k)), ones8<F16>(seen >> (k * 8)), n);
-          }
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) n = mfma32<F16>(marks<F16>(v_frag(db, k)), ones8<F16>(seen >> (k * 8)), n);
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[db][i] = counted(acc[db][i], n[i]);
         }
       }
     }
+  };
+  const Span3 sp = spans<64>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
+  if (nt > 0) issue(0);
+  int32_t t = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (const int32_t e = pass ? nt : sp.whole; t < e; ++t) tile(t, std::true_type());
+    if (pass == 0)
+      for (; t < sp.tail; ++t) tile(t, std::false_type());
   }
 
-  l += __shfl_xor(l, 32);
+  l = over_halves(l, Sum());
   if (!live) return;
   const float vs = NARROW && p.v_scale ? p.v_scale[h] : 1.f;
   const float inv = l == 0 ? 0.f : vs / l;
   const float lse = l == 0 ? -INFINITY : m * c + __log2f(l);
   const int32_t tk = q.first + tok;
   const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
+  auto each4 = [&](auto put) {
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      f32x4 o = {acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]};
-      o = l == 0 ? f32x4{0, 0, 0, 0} : o * inv;
-      const int d = db * 32 + b * 8 + half * 4;
-      if (parts == 1) store4<F16>(a, tk, g, d, o);
-      else *(f32x4*)&pl.part[at * D + d] = o;
-    }
+      for (int b = 0; b < 4; ++b) {
+        f32x4 o = {acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]};
+        put(db * 32 + b * 8 + half * 4, o * inv);   // all 0 where l is
+      }
+  };
+  if (parts == 1) each4([&](int d, f32x4 o) { store4<F16>(a, tk, g, d, o); });
+  else each4([&](int d, f32x4 o) { *(f32x4*)&pl.part[at * D + d] = o; });
   if (half == 0) {
     if (parts > 1) pl.part_lse[at] = lse;
     else if (a.lse) a.lse[(int64_t)tk * a.q_heads + g] = lse / kLog2e;
