@@ -24,6 +24,7 @@
 #include "pp_serve.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace pp {
 
@@ -48,6 +49,16 @@ constexpr int kWave = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLag = 8.f;   // growth of the maximum, in the exponent, that is let pass
 
+// f(0), f(1) .. f(N - 1), the numbers as constants.
+template <int N, class F, int... I>
+__device__ __forceinline__ void each_(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) {
+  each_<N>(f, std::make_integer_sequence<int, N>());
+}
+
 extern __shared__ __attribute__((aligned(1024))) char g_lds[];
 
 __device__ __forceinline__ uint32_t lds_base() {
@@ -58,7 +69,14 @@ __device__ __forceinline__ uint32_t lds_base() {
 // load, and the compiler is not told: wait_loads() before the reads.  (It keeps nothing in m0.)
 __device__ __forceinline__ void load_lds(uint32_t to, uint32_t off, const char* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(to), "v"(off), "s"(base) : "memory");
+               :: "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+}
+
+// The same into LDS at to + N.
+template <int N>
+__device__ __forceinline__ void load_lds_at(uint32_t to, uint32_t off, const char* base) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(to), "v"(off), "s"(base), "n"(N) : "memory", "scc");
 }
 
 template <int N>
@@ -282,9 +300,9 @@ __device__ __forceinline__ int32_t find_last(int32_t count, int32_t x, F f) {
 
 // Page numbers of 64 consecutive tiles of keys, one a lane.
 __device__ __forceinline__ int32_t page_of(const pp_kv_pages& p, const pp_attention_args& a,
-                                           const Plan& pl, int32_t r, int64_t key) {
+                                           const Plan& pl, const int32_t* blocks, int64_t key) {
   const int64_t b = key >> pl.shift;
-  int32_t page = b < a.max_blocks ? a.block_table[r * a.row_stride + b] : 0;
+  int32_t page = b < a.max_blocks ? blocks[b] : 0;
   return page < 0 ? 0 : page < p.n_pages ? page : p.n_pages - 1;
 }
 
@@ -385,10 +403,11 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
     voff[0][i] = (uint32_t)(row * tok_b) + ((lane % UPR) ^ Sw::v(row, NARROW)) * 16;
     voff[1][i] = (uint32_t)(row * tok_b) + ((lane % UPR) ^ Sw::v(row + 16, NARROW)) * 16;
   }
+  const int32_t* blocks = a.block_table + r * a.row_stride;
   int32_t held = 0;
   auto issue = [&](int32_t t) {
     const uint32_t to = ring + (t % NS) * Sh::kStage;
-    if ((t & 31) == 0) held = page_of(p, a, pl, r, (int64_t)kbase + (t + lane / 2) * 32 + (lane & 1) * 16);
+    if ((t & 31) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (t + lane / 2) * 32 + (lane & 1) * 16);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int64_t page = __builtin_amdgcn_readlane(held, (t & 31) * 2 + half);
@@ -670,23 +689,38 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   const char* vh = (const char*)p.v + h * p.head_stride * es;
   constexpr uint32_t kTile = 64 * RB;
   const uint32_t lds = lds_base();
-  uint32_t koff[kLoads], voff[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int rr = i * kRowsPerLoad + lane / UPR;          // + 16 wave: no swizzle reads that bit
-    koff[i] = (uint32_t)(rr * tok_b) + ((lane % UPR) ^ Sw::k(rr)) * 16;
-    voff[i] = (uint32_t)(rr * tok_b) + ((lane % UPR) ^ Sw::v(rr, NARROW)) * 16;
-  }
-  int32_t held = 0;
-  auto issue = [&](int32_t t) {   // wave w brings keys 16 w .. 16 w + 15 of the tile
-    const uint32_t to = lds + (t & 1) * 2 * kTile + wave * 16 * RB;
-    if ((t & 63) == 0) held = page_of(p, a, pl, r, (int64_t)kbase + (t + lane) * 64 + wave * 16);
-    const int64_t page = __builtin_amdgcn_readlane(held, t & 63);
-    const int64_t at = page * page_b + ((kbase + t * 64 + wave * 16) & (p.page_size - 1)) * tok_b;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_lds(to + i * 1024, koff[i], kh + at);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_lds(to + kTile + i * 1024, voff[i], vh + at);
+  // this lane's source in a group of 16 keys: row i * kRowsPerLoad + lane / UPR of load i, whose
+  // swizzle is that of the two summands' together (both are linear over xor, and read no higher bit)
+  const uint32_t off_row = (uint32_t)(lane / UPR * tok_b);
+  const uint32_t off_k = ((lane % UPR) ^ Sw::k(lane / UPR)) * 16;
+  const uint32_t off_v = ((lane % UPR) ^ Sw::v(lane / UPR, NARROW)) * 16;
+  // wave w brings keys 16 w .. 16 w + 15 of a tile.  K and V have two buffers each and go their own
+  // pace: V of a tile is brought with K of the same tile or of the next, from the same place in its pages.
+  const int32_t* blocks = a.block_table + r * a.row_stride;
+  const uint32_t tok32 = (uint32_t)tok_b;
+  const Span3 sp = spans<64>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
+  const int32_t flip = sp.whole & 1;                 // the pipeline below starts in buffer 0
+  auto buffer = [&](int32_t t) { return (uint32_t)((t ^ flip) & 1) * kTile; };
+  int32_t held = 0, next_k = 0, next_v = 0;
+  int64_t place = 0;              // of tile next_v
+  auto bring = [&](const char* from, uint32_t to, uint32_t off, auto swizzle) {
+    to = __builtin_amdgcn_readfirstlane(to + wave * 16 * RB);
+    each<kLoads>([&](auto i) {
+      load_lds_at<i * 1024>(to, off_row + (off ^ (swizzle(i * kRowsPerLoad) * 16)), from + i * kRowsPerLoad * tok32);
+    });
+  };
+  auto issue_k = [&] {
+    const int32_t t = next_k++;
+    if (t >= nt) return;
+    if ((t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (t + lane) * 64 + wave * 16);
+    const uint32_t page = __builtin_amdgcn_readlane(held, t & 63);
+    place = (int64_t)page * page_b + ((kbase + t * 64 + wave * 16) & (p.page_size - 1)) * tok32;
+    bring(kh + place, lds + buffer(t), off_k, [](int x) { return Sw::k(x); });
+  };
+  auto issue_v = [&] {            // before issue_k moves on
+    const int32_t t = next_v++;
+    if (t >= nt) return;
+    bring(vh + place, lds + 2 * kTile + buffer(t), off_v, [](int x) { return Sw::v(x, NARROW); });
   };
 
   f32x16 acc[DB];
@@ -704,112 +738,204 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   const uint32_t vx = NARROW ? (dh ^ Sw::v(vrow, true)) * 16 + (i16 % 2) * 8
                              : ((dh * 2 + (i16 % 4) / 2) ^ Sw::v(vrow, false)) * 16 + (i16 % 2) * 8;
 
-  auto tile = [&](int32_t t, auto masked) {
-    constexpr bool kMasked = decltype(masked)::value;   // some row does not see all of it
-    wait_loads<0>();
-    barrier();                    // every wave's keys are there, and the other buffer is read
-    if (t + 1 < nt) issue(t + 1);
-    const uint32_t kt = lds + (t & 1) * 2 * kTile, vt = kt + kTile;
-    f32x16 s[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = 0;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        s16x8 f;
-        if constexpr (NARROW)
-          f = widen8<F16>(*LDS_PTR(i32x2, kt + kb * 32 * RB + krow + (kx ^ (ks * 16))));
-        else
-          f = *LDS_PTR(s16x8, kt + kb * 32 * RB + krow + (kx ^ (ks * 32)));
-        s[kb] = mfma32<F16>(f, qf[ks], s[kb]);
-      }
-    }
-    const int32_t tile0 = kbase + t * 64;
-    uint32_t seen = ~0u;
-    if constexpr (kMasked) {
-      seen = 0;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        const int32_t key = tile0 + (j / 16) * 32 + (j % 16 / 4) * 8 + 4 * half + j % 4;
-        const bool ok = sees(pos, key, a.window) && key < k1;
-        seen |= ok ? 1u << j : 0;
-        if (!ok) s[j / 16][j % 16] = -INFINITY;
-      }
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int j = 1; j < 32; ++j) mx = fmaxf(mx, s[j / 16][j % 16]);
-    mx = over_halves(mx, Max());
-    const bool grow = mx > m && (m == -INFINITY || (mx - m) * c > kLag);
-    if (__any(grow)) {
-      const float n = fmaxf(m, mx);
-      const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
-      l *= al;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] *= al;
-      m = n;
-    }
-    const float mc = m == -INFINITY ? 0.f : m * c;
-    s16x8 pf[4];
-    float sum = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        w[j] = exp2_(__builtin_fmaf(s[k / 2][k % 2 * 8 + j], c, -mc));
-        if (kMasked && !(seen >> (k * 8 + j) & 1)) w[j] = 0;
-        sum += w[j];
-      }
-      pf[k] = pack8<F16>(w);
-    }
-    l += sum;
-    // keys 16 k + 8 (j / 4) + 4 half + j % 4 of the tile, as the weights' registers have them
-    auto v_frag = [&](int db, int k) -> s16x8 {
-      if constexpr (NARROW) {
-        return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            LDS_PTR(i32x2, vt + k * 16 * RB + vat + (vx ^ (db * 32))))));
-      } else {
-        const uint32_t at = vt + k * 16 * RB + vat + (vx ^ (db * 64));
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 8 * RB));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    };
-    if constexpr (!kMasked) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) acc[db] = mfma32<F16>(v_frag(db, k), pf[k], acc[db]);
+  // addresses of the fragments in the first tile; opaque, so that the pipeline's constant offsets go
+  // into the instructions
+  uint32_t k_lds[KS], v_lds[DB];
+  each<KS>([&](auto i) {
+    k_lds[i] = lds + krow + (kx ^ (i * (NARROW ? 16 : 32)));
+    asm volatile("" : "+v"(k_lds[i]));
+  });
+  each<DB>([&](auto i) {
+    v_lds[i] = lds + 2 * kTile + vat + (vx ^ (i * (NARROW ? 32 : 64)));
+    asm volatile("" : "+v"(v_lds[i]));
+  });
+  auto k_frag = [&](uint32_t at, int ks) -> s16x8 {
+    const auto* f = LDS_PTR(char, k_lds[ks]) + at;
+    if constexpr (NARROW) return widen8<F16>(*(__attribute__((address_space(3))) i32x2*)f);
+    else return *(__attribute__((address_space(3))) s16x8*)f;
+  };
+  // keys 8 (j / 4) + 4 half + j % 4 of 16, as the weights' registers have them
+  auto v_frag = [&](uint32_t at, int db) -> s16x8 {
+    auto* f = LDS_PTR(char, v_lds[db]) + at;
+    if constexpr (NARROW) {
+      return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+          (__attribute__((address_space(3))) i32x2*)f)));
     } else {
-      uint32_t odd = 0;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) acc[db] = mfma32<F16>(only_finite<F16>(v_frag(db, k), odd), pf[k], acc[db]);
-      if (__any(odd != 0)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          f32x16 n;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) n[i] = 0;
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) n = mfma32<F16>(marks<F16>(v_frag(db, k)), ones8<F16>(seen >> (k * 8)), n);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[db][i] = counted(acc[db][i], n[i]);
-        }
-      }
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)f);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(f + 8 * RB));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   };
-  const Span3 sp = spans<64>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
-  if (nt > 0) issue(0);
+  auto scores = [&](uint32_t at) -> f32x16 {       // of 32 keys
+    f32x16 x;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0;
+    each<KS>([&](auto ks) { x = mfma32<F16>(k_frag(at, ks), qf[ks], x); });
+    return x;
+  };
+  auto largest = [&](const f32x16& x) {
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    return mx;
+  };
+  auto rescale = [&](float old) {
+    const float al = old == -INFINITY ? 0.f : exp2_((old - m) * c);
+    l *= al;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] *= al;
+  };
+  auto grows = [&](float mx) { return __any(mx > m && (m == -INFINITY || (mx - m) * c > kLag)); };
+
+  // Half a tile that some row does not see whole.
+  auto masked_half = [&](uint32_t at, int32_t key0) {
+    f32x16 s = scores(at);
+    uint32_t seen = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int32_t key = key0 + (j / 4) * 8 + j % 4;
+      const bool ok = sees(pos, key, a.window) && key < k1;
+      seen |= ok ? 1u << j : 0;
+      if (!ok) s[j] = -INFINITY;
+    }
+    const float mx = over_halves(largest(s), Max());
+    if (grows(mx)) {
+      const float old = m;
+      m = fmaxf(m, mx);
+      rescale(old);
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+    float w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      w[j] = (seen >> j & 1) ? exp2_(__builtin_fmaf(s[j], c, -mc)) : 0.f;
+      l += w[j];
+    }
+    const s16x8 x[2] = {pack8<F16>(w), pack8<F16>(w + 8)};
+    uint32_t odd = 0;
+    each<2 * DB>([&](auto i) {
+      acc[i / 2] = mfma32<F16>(only_finite<F16>(v_frag(at + i % 2 * 16 * RB, i / 2), odd), x[i % 2], acc[i / 2]);
+    });
+    if (__any(odd != 0)) {
+      each<DB>([&](auto db) {
+        f32x16 n;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) n[i] = 0;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k)
+          n = mfma32<F16>(marks<F16>(v_frag(at + k * 16 * RB, db)), ones8<F16>(seen >> (k * 8)), n);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[db][i] = counted(acc[db][i], n[i]);
+      });
+    }
+  };
+  auto masked_tile = [&](int32_t t) {
+    wait_loads<0>();
+    barrier();                    // every wave's keys are there, and the other buffers are read
+    if (next_k == t + 1) issue_k();
+    issue_v();
+#pragma unroll 1
+    for (int b = 0; b < 2; ++b) masked_half(buffer(t) + b * 32 * RB, kbase + t * 64 + b * 32 + 4 * half);
+  };
+
+  // Tiles that every row sees whole go through a pipeline of 32 keys: while the weights of one half
+  // tile are worked out, the matrix cores have the scores of the next and the values of the one
+  // before.  (Without it the two took turns, although two waves share a SIMD.)
+  // Its order is laid down by hand, one matrix instruction at a time with a sixteenth of the rest
+  // beside it: left alone the compiler reads each fragment right before its use.
+  f32x16 even, odds;              // scores of a tile's first and second half
+  s16x8 pf[2];
+  float mc = 0, old = 0;
+  bool grow = false;              // of the scores that a step starts with
+  auto peak = [&](float mx) {
+    mx = over_halves(mx, Max());
+    grow = grows(mx);
+    old = m;
+    m = grow ? fmaxf(m, mx) : m;
+    mc = m == -INFINITY ? 0.f : m * c;
+  };
+  auto step = [&](const f32x16& cur, f32x16& next, uint32_t k_next, uint32_t v_last, auto first) {
+    constexpr int NV = decltype(first)::value ? 0 : 2 * DB, NM = KS + NV, kAhead = 3;
+    s16x8 f[NM], x[2];
+    auto read = [&](auto at) {
+      constexpr int i = decltype(at)::value;
+      if constexpr (i < KS) f[i] = k_frag(k_next, i);
+      else f[i] = v_frag(v_last + (i - KS) % 2 * 16 * RB, (i - KS) / 2);
+    };
+    float w[16], sum = 0, mx = -INFINITY;
+    f32x16 y;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = 0;
+    each<kAhead>(read);
+    each<NM>([&](auto at) {
+      constexpr int i = decltype(at)::value;
+      if constexpr (i + kAhead < NM) read(std::integral_constant<int, i + kAhead>());
+      if constexpr (i < KS) y = mfma32<F16>(f[i], qf[i], y);
+      else acc[(i - KS) / 2] = mfma32<F16>(f[i], pf[(i - KS) % 2], acc[(i - KS) / 2]);
+#pragma unroll
+      for (int j = i * 16 / NM; j < (i + 1) * 16 / NM; ++j) {
+        w[j] = exp2_(__builtin_fmaf(cur[j], c, -mc));
+        asm volatile("" : "+v"(w[j]));   // here, and not behind the branch at the end: so for the others
+        sum += w[j];
+      }
+      asm volatile("" : "+v"(sum));
+      if constexpr (i == NM / 2) {
+        x[0] = pack8<F16>(w);
+        asm volatile("" : "+v"(x[0]));
+      }
+      if constexpr (i >= KS) {
+        constexpr int q = i - KS;     // the scores are there a little after their last instruction
+#pragma unroll
+        for (int j = q > 0 ? (q - 1) * 16 / (NV - 1) : 0; j < q * 16 / (NV - 1); ++j) mx = fmaxf(mx, y[j]);
+        asm volatile("" : "+v"(mx));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    x[1] = pack8<F16>(w + 8);
+    asm volatile("" : "+v"(x[1]));
+    next = y;
+    pf[0] = x[0];
+    pf[1] = x[1];
+    if (grow) rescale(old);
+    l += sum;
+    peak(NV ? mx : largest(y));
+  };
+
+  issue_k();
+  issue_v();
   int32_t t = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (const int32_t e = pass ? nt : sp.whole; t < e; ++t) tile(t, std::true_type());
-    if (pass == 0)
-      for (; t < sp.tail; ++t) tile(t, std::false_type());
+  for (; t < sp.whole; ++t) masked_tile(t);
+  const int32_t tail = t + ((sp.tail - t) & ~1);   // the loop takes two at a time
+  if (t < tail) {
+    constexpr uint32_t kHalf = 32 * RB;
+    wait_loads<0>();
+    barrier();
+    issue_k();
+    even = scores(0);
+    peak(largest(even));
+    step(even, odds, kHalf, 0, std::true_type());
+    auto turn = [&](auto buf) {   // K of t + 1 and V of t are there; K of t and V of t - 1 are read
+      constexpr uint32_t k = (1 - decltype(buf)::value) * kTile, v = decltype(buf)::value * kTile;
+      wait_loads<0>();
+      barrier();
+      issue_v();
+      issue_k();
+      step(odds, even, k, v, std::false_type());
+      ++t;
+    };
+    for (;;) {
+      turn(std::integral_constant<int, 0>());
+      step(even, odds, kTile + kHalf, kHalf, std::false_type());
+      turn(std::integral_constant<int, 1>());
+      if (t == tail) break;
+      step(even, odds, kHalf, kTile + kHalf, std::false_type());
+    }
+    m = old;                      // the scores past the last tile are nobody's
+    each<2 * DB>([&](auto i) {
+      acc[i / 2] = mfma32<F16>(v_frag(kTile + kHalf + i % 2 * 16 * RB, i / 2), pf[i % 2], acc[i / 2]);
+    });
   }
+  for (; t < nt; ++t) masked_tile(t);
 
   l = over_halves(l, Sum());
   if (!live) return;
