@@ -23,6 +23,7 @@
 
 #include "pp_serve.h"
 
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -331,8 +332,8 @@ template <bool NARROW, int D, int RT>
 struct RowsShape {
   static constexpr int kRB = D * (NARROW ? 1 : 2);          // bytes of a row
   static constexpr int kStage = 2 * 32 * kRB;               // K and V of 32 keys
-  static constexpr int kNW = kStage > 16384 ? 2 : 4;        // waves
-  static constexpr int kNS = kStage > 8192 ? 2 : 4;         // stages of a wave's ring
+  static constexpr int kNW = kStage > 8192 ? 2 : 4;         // waves
+  static constexpr int kNS = kStage > 4096 ? 2 : 4;         // stages of a wave's ring
   static constexpr int kRing = kNW * kNS * kStage;
   static constexpr int kRow = D + 4;                        // floats of a joined row
   static constexpr int kJoin = kNW * 16 * RT * (kRow + 2) * 4;
@@ -642,13 +643,33 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   const int part = (blockIdx.x / p.heads) % pl.parts_tiles;
   const int32_t slot = blockIdx.x / p.heads / pl.parts_tiles;
   const int G = pl.group;
-  // request r's tiles start at slot floor(first token * G / 128) + r, which leaves it enough of them
-  auto base_of = [&](int32_t r) { return (int32_t)((int64_t)a.query_start[r] * G / 128) + r; };
-  const int32_t r = find_last(a.requests, slot, base_of);
-  if (r < 0 || base_of(r) > slot) return;
+  int32_t r, first_slot;
+  if (a.requests <= kWave) {
+    // longest request first, so that no long block starts late: on 4 requests of 8,192 to 16,384 tokens the
+    // last blocks end 4% after the average and not 18%
+    const Request mine = request(a, pl, lane < a.requests ? lane : 0);
+    const int64_t mine_rows = lane < a.requests ? (int64_t)mine.count * G : 0;
+    const int32_t tiles = mine_rows > pl.few ? (int32_t)((mine_rows + 127) / 128) : 0, keys = mine.hi - mine.lo;
+    int32_t base = 0;
+    for (int j = 0; j < a.requests; ++j) {
+      const int32_t kj = __builtin_amdgcn_readlane(keys, j), tj = __builtin_amdgcn_readlane(tiles, j);
+      if (kj > keys || (kj == keys && j < lane)) base += tj;
+    }
+    const uint64_t at = __ballot(slot >= base && slot < base + tiles);
+    if (!at) return;
+    r = __builtin_ctzll(at);
+    first_slot = __builtin_amdgcn_readlane(base, r);
+  } else {
+    // request r's tiles start at slot floor(first token * G / 128) + r, which leaves it enough of them
+    auto base_of = [&](int32_t i) { return (int32_t)((int64_t)a.query_start[i] * G / 128) + i; };
+    r = find_last(a.requests, slot, base_of);
+    if (r < 0) return;
+    first_slot = base_of(r);
+    if (first_slot > slot) return;
+  }
   const Request q = request(a, pl, r);
   const int64_t rows = (int64_t)q.count * G;
-  const int64_t row0 = (int64_t)(slot - base_of(r)) * 128;
+  const int64_t row0 = (int64_t)(slot - first_slot) * 128;
   if (rows <= pl.few || row0 >= rows) return;
   const int32_t parts = parts_of(q, pl.cut_tiles, pl.parts_tiles);
   if (part >= parts) return;
@@ -963,48 +984,95 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
 
 // ---------------------------------------------------------------- k_join ---
 
-// One wave a (token, query head) of a request in several parts.
+// One wave a (token, query head) of a request in several parts.  Bound by the chain of its loads, so
+// the log sums are read before it is known how many count, and four parts' values at a time.
+// few_rows: a wave's number is one of few_rows rows of one of the key heads of a request of k_rows
+// (where no request of k_tiles is in parts); 0: it is a row of the call.
 template <bool F16, int D>
-__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl) {
-  const int lane = threadIdx.x % kWave;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (at >= (int64_t)a.tokens * a.q_heads) return;
-  const int32_t t = (int32_t)(at / a.q_heads), g = (int32_t)(at % a.q_heads);
-  const int32_t r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
-  if (r < 0) return;
-  const Request q = request(a, pl, r);
-  if (t >= q.first + q.count) return;
-  const bool small = (int64_t)q.count * pl.group <= pl.few;
-  const int32_t parts = small ? parts_of(q, pl.cut_rows, pl.parts_rows) : parts_of(q, pl.cut_tiles, pl.parts_tiles);
-  if (parts == 1) return;
-  const int64_t step = (int64_t)a.tokens * a.q_heads;
-  float mm = -INFINITY;
-  for (int32_t i = lane; i < parts; i += kWave) mm = fmaxf(mm, pl.part_lse[i * step + at]);
-  for (int o = kWave / 2; o; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
+__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int32_t most, int32_t few_rows,
+                                              int32_t heads) {
   constexpr int N = D / kWave;
-  float o[N] = {}, sum = 0;
-  for (int32_t i = 0; i < parts; ++i) {
-    const float x = pl.part_lse[i * step + at];
-    if (x == -INFINITY) continue;
-    const float w = x == mm ? 1.f : exp2_(x - mm);
-    sum += w;
+  typedef __attribute__((__vector_size__(N * 4))) float fN;
+  const int lane = threadIdx.x % kWave;
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t step = (int64_t)a.tokens * a.q_heads;
+  int64_t at;
+  int32_t t, g, parts;
+  float own = -INFINITY;
+  if (few_rows) {
+    const int32_t row = (int32_t)(id % few_rows), h = (int32_t)(id / few_rows % heads);
+    const int64_t r = id / few_rows / heads;
+    if (r >= a.requests) return;
+    const Request q = request(a, pl, (int32_t)r);
+    const int64_t rows = (int64_t)q.count * pl.group;
+    if (row >= rows || rows > pl.few) return;
+    parts = parts_of(q, pl.cut_rows, pl.parts_rows);
+    t = q.first + row / pl.group;
+    g = h * pl.group + row % pl.group;
+    at = (int64_t)t * a.q_heads + g;
+    if (lane < most) own = pl.part_lse[lane * step + at];
+  } else {
+    at = id;
+    if (at >= step) return;
+    if (lane < most) own = pl.part_lse[lane * step + at];
+    t = (int32_t)(at / a.q_heads);
+    g = (int32_t)(at % a.q_heads);
+    const int32_t r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
+    if (r < 0) return;
+    const Request q = request(a, pl, r);
+    if (t >= q.first + q.count) return;
+    parts = (int64_t)q.count * pl.group <= pl.few ? parts_of(q, pl.cut_rows, pl.parts_rows)
+                                                  : parts_of(q, pl.cut_tiles, pl.parts_tiles);
+  }
+  if (parts == 1) return;
+  float m = -INFINITY, sum = 0;
+  fN o = {};
+  const float* from = pl.part + at * D + lane * N;
+  for (int32_t base = 0; base < parts; base += kWave) {
+    if (base) own = base + lane < most ? pl.part_lse[(base + lane) * step + at] : -INFINITY;
+    if (base + lane >= parts) own = -INFINITY;
+    float n = own;
+    for (int x = kWave / 2; x; x >>= 1) n = fmaxf(n, __shfl_xor(n, x));
+    n = fmaxf(n, m);
+    if (n == -INFINITY && !__any(own != own)) continue;
+    const float al = m == -INFINITY ? 0.f : exp2_(m - n);
+    m = n;
+    float w = own == -INFINITY ? 0.f : own == n ? 1.f : exp2_(own - n);
+    o *= al;
+    sum *= al;
+    const int32_t here = parts - base < kWave ? parts - base : kWave;
+    for (int32_t i = 0; i < here; i += 4) {
+      fN x[4];
+      float wi[4];
 #pragma unroll
-    for (int j = 0; j < N; ++j) o[j] += w * pl.part[(i * step + at) * D + lane * N + j];
+      for (int j = 0; j < 4; ++j) {      // a part of weight 0 may never have been written
+        wi[j] = i + j < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (i + j) & 63)) : 0.f;
+        x[j] = fN{};
+        if (wi[j] != 0) x[j] = *(const fN*)(from + (base + i + j) * step * D);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o += wi[j] * x[j];
+        sum += wi[j];
+      }
+    }
   }
   uint16_t* out = (uint16_t*)a.out + t * a.out_token_stride + g * a.out_head_stride + lane * N;
-  const float inv = sum == 0 ? 0.f : 1.f / sum;
+  o *= sum == 0 ? 0.f : 1.f / sum;
   if constexpr (N == 1) {
-    out[0] = (uint16_t)pack2<F16>(o[0] * inv, 0.f);
+    out[0] = (uint16_t)pack2<F16>(o[0], 0.f);
   } else {
 #pragma unroll
-    for (int j = 0; j < N; j += 2) *(int*)(out + j) = pack2<F16>(o[j] * inv, o[j + 1] * inv);
+    for (int j = 0; j < N; j += 2) *(int*)(out + j) = pack2<F16>(o[j], o[j + 1]);
   }
-  if (a.lse && lane == 0) a.lse[at] = sum == 0 ? -INFINITY : (mm + __log2f(sum)) / kLog2e;
+  if (a.lse && lane == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }
 
 // -------------------------------------------------------------- dispatch ---
 
-constexpr int kFill = 1024;     // blocks a call is cut towards
+constexpr int kRowBlocks = 4096;   // blocks k_rows is cut towards
+constexpr int kLeastKeys = 256;    // and the least keys of one
+constexpr int kTileBlocks = 512;   // blocks of k_tiles that are resident
 
 int32_t round_up(int64_t x, int32_t m) { return (int32_t)((x + m - 1) / m * m); }
 
@@ -1029,19 +1097,39 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     if (pl.group <= most && (int64_t)a.requests * a.max_new != a.tokens) ch.rt = tiles16(pl.group);
   }
   pl.few = ch.rt * 16;
-  const int64_t keys = a.max_len > 1 ? a.max_len : 1;
-  auto cut = [&](int64_t blocks, int32_t unit, int32_t least, int32_t& size, int32_t& parts) {
-    int64_t want = (kFill + blocks - 1) / blocks;
-    int64_t c = (keys + want - 1) / want;
-    if (c < least) c = least;
-    size = round_up(c, unit);
-    parts = (int32_t)((keys + size - 1) / size);
-  };
+  // keys that a request's rows see, at most
+  int64_t keys = a.max_len > 1 ? a.max_len : 1;
+  if (a.window && (int64_t)a.window + a.max_new + 64 < keys) keys = (int64_t)a.window + a.max_new + 64;
   pl.parts_rows = pl.parts_tiles = 1;
   pl.cut_rows = pl.cut_tiles = round_up(keys, 128);
-  if (ch.rt) cut((int64_t)a.requests * p.heads, 128, 256, pl.cut_rows, pl.parts_rows);
+  auto cut = [&](int32_t n, int32_t unit, int32_t& size, int32_t& parts) {
+    size = round_up((keys + n - 1) / n, unit);
+    parts = (int32_t)((keys + size - 1) / size);
+  };
+  if (ch.rt) {
+    // lengths differ, so blocks are many and small; below 256 keys a block's start and end are most of it
+    int64_t n = (kRowBlocks + (int64_t)a.requests * p.heads - 1) / ((int64_t)a.requests * p.heads);
+    if (n > keys / kLeastKeys) n = keys / kLeastKeys;
+    cut((int32_t)(n > 1 ? n : 1), 128, pl.cut_rows, pl.parts_rows);
+  }
   pl.slots = (int32_t)((int64_t)a.tokens * pl.group / 128) + a.requests;
-  if (ch.tiles) cut((int64_t)a.tokens * pl.group / 128 * p.heads + 1, 64, 512, pl.cut_tiles, pl.parts_tiles);
+  if (ch.tiles) {
+    // as many parts as end soonest: rounds of resident blocks, each of its share of the tiles and some
+    // four tiles' time to start and end, and the join's reading and writing of every part
+    const double blocks = (double)a.tokens * pl.group / 128 * p.heads + 1, tiles = keys / 64.0;
+    const double tile_us = 0.8 + 0.8 * p.dim / 128;
+    const double part_us = (double)a.tokens * a.q_heads * p.dim * 8 / 4e6;
+    double best = 0;
+    int32_t n = 1;
+    for (int32_t i = 1; i <= 64 && (i == 1 || tiles / i >= 8); ++i) {
+      const double t = std::ceil(blocks * i / kTileBlocks) * (tiles / i + 4) * tile_us + (i > 1 ? 4 + i * part_us : 0);
+      if (i == 1 || t < best) {
+        best = t;
+        n = i;
+      }
+    }
+    cut(n, 64, pl.cut_tiles, pl.parts_tiles);
+  }
   ch.join = (ch.rt && pl.parts_rows > 1) || (ch.tiles && pl.parts_tiles > 1);
   return ch;
 }
@@ -1086,8 +1174,13 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, 
     if (ch.rt == 4) e = go_rows<F16, NARROW, D, 4>(p, a, pl, st);
   if (e != hipSuccess) return e;
   if (ch.join) {
-    const int64_t rows = (int64_t)a.tokens * a.q_heads;
-    k_join<F16, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pl);
+    int64_t few_rows = 0, rows = (int64_t)a.tokens * a.q_heads;
+    if (pl.parts_tiles == 1) {
+      few_rows = (int64_t)a.max_new * pl.group < pl.few ? (int64_t)a.max_new * pl.group : pl.few;
+      rows = (int64_t)a.requests * p.heads * few_rows;
+    }
+    k_join<F16, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(
+        a, pl, pl.parts_rows > pl.parts_tiles ? pl.parts_rows : pl.parts_tiles, (int32_t)few_rows, p.heads);
     e = hipGetLastError();
   }
   return e;
