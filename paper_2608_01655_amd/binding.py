@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -556,18 +557,43 @@ def pp_cache_slots(target, n_slots, held=None):
     return slot, fresh.value
 
 
+# A decode step makes these calls once a layer, so their checks cost a few microseconds at most:
+# arguments are packed as the C structures lay them out, not field by field through ctypes.
+_BLOCK_ARGS = struct.Struct("@9iq13P")
+_KV_PAGES = struct.Struct("@4P5i3q")
+_ATTENTION_ARGS = struct.Struct("@8if5q7Pq")
+_torch = None
+_types = {}
+
+
+def _with_torch():
+    global _torch
+    if _torch is None:
+        import torch
+
+        _types.update({torch.bfloat16: PP_BF16, torch.float16: PP_F16,
+                       torch.float8_e4m3fn: PP_E4M3})
+        _torch = torch
+    return _torch
+
+
 def _stream_of(torch, t, stream):
     """The stream to enqueue on, where tensor `t` lies."""
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    device = t.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError("tensors must lie on the current GPU")
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _ints(torch, t, what, *shape):
-    """Address of a contiguous int32 device tensor of that shape."""
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() \
-            or tuple(t.shape) != shape:
-        raise ValueError(f"{what}: want a contiguous int32 tensor of shape {shape} on the GPU")
+def _refuse_ints(t, what, dtype, shape):
+    raise ValueError(f"{what}: want a contiguous {dtype} tensor of shape {tuple(shape)} on the "
+                     f"GPU, got {t.dtype} {tuple(t.shape)}")
+
+
+def _table(torch, t, R):
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] != R \
+            or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("block_table: want int32 rows, one a request, on the GPU")
     return t.data_ptr()
 
 
@@ -580,34 +606,33 @@ def pp_block_tables(leaf, length, cached, prefix_table, slot, free_pages, block_
     rows of block_table int32 [R][blocks] are updated in place; outputs
     query_start int32 [R + 1], start, end int32 [R], slot_map int64 [t],
     position int32 [t], taken int32 [1]."""
-    import torch
-
+    torch = _torch or _with_torch()
     st = _stream_of(torch, length, stream)
-    R, n, t = length.shape[0], slot.shape[0], slot_map.shape[0]
-    if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 \
-            or block_table.shape[0] != R or block_table.stride(1) != 1:
-        raise ValueError("block_table: want int32 rows, one a request, on the GPU")
-    if slot_map.dtype != torch.int64 or not slot_map.is_cuda or not slot_map.is_contiguous():
-        raise ValueError("slot_map: want a contiguous int64 tensor on the GPU")
-    a = pp_block_args(
-        R, n, int(n_slots), free_pages.shape[0], block_table.shape[1], t, int(page_size),
-        int(chunk_tokens), int(max_new), block_table.stride(0), _ints(torch, leaf, "leaf", R),
-        _ints(torch, length, "length", R), _ints(torch, cached, "cached", R),
-        _ints(torch, prefix_table, "prefix_table", n, 16), _ints(torch, slot, "slot", n),
-        _ints(torch, free_pages, "free_pages", free_pages.shape[0]), block_table.data_ptr(),
-        _ints(torch, query_start, "query_start", R + 1), _ints(torch, start, "start", R),
-        _ints(torch, end, "end", R), slot_map.data_ptr(), _ints(torch, position, "position", t),
-        _ints(torch, taken, "taken", 1))
-    _check(lib().pp_block_tables(ctypes.byref(a), st))
+    i32 = torch.int32
+    R, n, f, t = length.shape[0], slot.shape[0], free_pages.shape[0], slot_map.shape[0]
+    at = []
+    for x, shape, what in (
+            (leaf, (R,), "leaf"), (length, (R,), "length"), (cached, (R,), "cached"),
+            (prefix_table, (n, 16), "prefix_table"), (slot, (n,), "slot"),
+            (free_pages, (f,), "free_pages"), (query_start, (R + 1,), "query_start"),
+            (start, (R,), "start"), (end, (R,), "end"), (position, (t,), "position"),
+            (taken, (1,), "taken")):
+        if x.dtype != i32 or x.shape != shape or not x.is_cuda or not x.is_contiguous():
+            _refuse_ints(x, what, i32, shape)
+        at.append(x.data_ptr())
+    if slot_map.dtype != torch.int64 or slot_map.dim() != 1 or not slot_map.is_cuda \
+            or not slot_map.is_contiguous():
+        _refuse_ints(slot_map, "slot_map", torch.int64, ("t",))
+    rows = _table(torch, block_table, R)
+    rc = lib().pp_block_tables(_BLOCK_ARGS.pack(
+        R, n, n_slots, f, block_table.shape[1], t, page_size, chunk_tokens, max_new,
+        block_table.stride(0), at[0], at[1], at[2], at[3], at[4], at[5], rows, at[6], at[7],
+        at[8], slot_map.data_ptr(), at[9], at[10]), st)
+    if rc:
+        _check(rc)
 
 
-_types = {}
-
-
-def _type(torch, t):
-    if not _types:
-        _types.update({torch.bfloat16: PP_BF16, torch.float16: PP_F16,
-                       torch.float8_e4m3fn: PP_E4M3})
+def _type(t):
     try:
         return _types[t.dtype]
     except KeyError:
@@ -616,27 +641,34 @@ def _type(torch, t):
 
 def _rows(t, what):
     """(token stride, head stride) of device rows [tokens][heads][dim]."""
-    if t.dim() != 3 or not t.is_cuda or (t.stride(2) != 1 and t.shape[2] != 1):
+    if t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{what}: want [tokens][heads][dim] on the GPU, dim contiguous")
-    return t.stride(0), t.stride(1)
+    token, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{what}: want [tokens][heads][dim] on the GPU, dim contiguous")
+    return token, head
+
+
+def _scale(torch, s, H):
+    if s is None:
+        return 0
+    if s.dtype != torch.float32 or not s.is_cuda or s.shape != (H,) or not s.is_contiguous():
+        raise ValueError("scales: want float32 [heads] on the GPU")
+    return s.data_ptr()
 
 
 def _pages(torch, k_cache, v_cache, k_scale, v_scale):
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape \
-            or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1 \
-            or k_cache.dtype != v_cache.dtype or not k_cache.is_cuda or not v_cache.is_cuda:
+    """(packed pp_kv_pages, heads, dim)."""
+    strides = k_cache.stride()
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or strides != v_cache.stride() \
+            or strides[3] != 1 or k_cache.dtype != v_cache.dtype or not k_cache.is_cuda \
+            or not v_cache.is_cuda:
         raise ValueError("pages: want two device tensors [pages][heads][page_size][dim] "
                          "alike, dim contiguous")
     P, H, ps, D = k_cache.shape
-    scales = []
-    for s in (k_scale, v_scale):
-        if s is not None and (s.dtype != torch.float32 or not s.is_cuda or s.shape != (H,)
-                              or not s.is_contiguous()):
-            raise ValueError("scales: want float32 [heads] on the GPU")
-        scales.append(None if s is None else s.data_ptr())
-    sp, sh, st, _ = k_cache.stride()
-    return pp_kv_pages(k_cache.data_ptr(), v_cache.data_ptr(), scales[0], scales[1],
-                       _type(torch, k_cache), P, ps, H, D, sp, sh, st)
+    return _KV_PAGES.pack(k_cache.data_ptr(), v_cache.data_ptr(), _scale(torch, k_scale, H),
+                          _scale(torch, v_scale, H), _type(k_cache), P, ps, H, D,
+                          *strides[:3]), H, D
 
 
 def pp_kv_write(k, v, slot_map, k_cache, v_cache, *, k_scale=None, v_scale=None, stream=None):
@@ -644,38 +676,19 @@ def pp_kv_write(k, v, slot_map, k_cache, v_cache, *, k_scale=None, v_scale=None,
     [tokens]) names, on torch device tensors (see include/prefixplace.h).
     Pages are [pages][heads][page_size][dim] views in any memory order, of
     the rows' type or float8_e4m3fn."""
-    import torch
-
+    torch = _torch or _with_torch()
     st = _stream_of(torch, k, stream)
-    pages = _pages(torch, k_cache, v_cache, k_scale, v_scale)
+    pages, H, D = _pages(torch, k_cache, v_cache, k_scale, v_scale)
     (kt, kh), (vt, vh) = _rows(k, "k"), _rows(v, "v")
     T = slot_map.shape[0]
-    if tuple(k.shape) != (T, pages.heads, pages.dim) or k.shape != v.shape or k.dtype != v.dtype:
+    if k.shape != (T, H, D) or v.shape != k.shape or k.dtype != v.dtype:
         raise ValueError("shape mismatch")
     if slot_map.dtype != torch.int64 or not slot_map.is_cuda or not slot_map.is_contiguous():
-        raise ValueError("slot_map: want a contiguous int64 tensor on the GPU")
-    _check(lib().pp_kv_write(ctypes.byref(pages), T, _type(torch, k), k.data_ptr(), kt, kh,
-                             v.data_ptr(), vt, vh, slot_map.data_ptr(), st))
-
-
-def _attention_args(torch, q, pages, block_table, query_start, length, out, lse, scale, max_new,
-                    max_len, window):
-    T, Hq, D = q.shape
-    R = length.shape[0]
-    (qt, qh), (ot, oh) = _rows(q, "q"), _rows(out, "out")
-    if D != pages.dim or out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("shape mismatch")
-    if block_table.dtype != torch.int32 or not block_table.is_cuda or block_table.dim() != 2 \
-            or block_table.shape[0] != R or block_table.stride(1) != 1:
-        raise ValueError("block_table: want int32 rows, one a request, on the GPU")
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda
-                            or tuple(lse.shape) != (T, Hq) or not lse.is_contiguous()):
-        raise ValueError("lse: want a contiguous float32 tensor [tokens][q_heads] on the GPU")
-    return pp_attention_args(
-        R, T, Hq, _type(torch, q), int(max_new), int(max_len), block_table.shape[1], int(window),
-        float(scale), qt, qh, ot, oh, block_table.stride(0), q.data_ptr(), out.data_ptr(),
-        None if lse is None else lse.data_ptr(), _ints(torch, query_start, "query_start", R + 1),
-        _ints(torch, length, "length", R), block_table.data_ptr(), None, 0)
+        _refuse_ints(slot_map, "slot_map", torch.int64, (T,))
+    rc = lib().pp_kv_write(pages, T, _type(k), k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+                           slot_map.data_ptr(), st)
+    if rc:
+        _check(rc)
 
 
 def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, out, lse=None, *,
@@ -685,31 +698,70 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
     torch device tensors (see include/prefixplace.h): q and out
     [tokens][q_heads][dim], pages as in pp_kv_write, block_table int32
     [R][blocks], query_start int32 [R + 1], length int32 [R], lse float32
-    [tokens][q_heads] or None.  Without a `workspace` (a uint8 tensor that
-    the caller keeps) one is taken from torch's allocator for the call."""
-    import torch
-
+    [tokens][q_heads] or None.  Without a `workspace` (a tensor that the
+    caller keeps) one is taken from torch's allocator for the call."""
+    torch = _torch or _with_torch()
     st = _stream_of(torch, q, stream)
     L = lib()
-    pages = _pages(torch, k_cache, v_cache, k_scale, v_scale)
-    a = _attention_args(torch, q, pages, block_table, query_start, length, out, lse, scale,
-                        max_new, max_len, window)
-    pr, ar = ctypes.byref(pages), ctypes.byref(a)
-    need = L.pp_attention_workspace(pr, ar)
-    if need < 0:
-        _check(need)
-    if need:
-        if workspace is None:
+    pages, _, D = _pages(torch, k_cache, v_cache, k_scale, v_scale)
+    (qt, qh), (ot, oh) = _rows(q, "q"), _rows(out, "out")
+    T, Hq, d = q.shape
+    R = length.shape[0]
+    if d != D or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("shape mismatch")
+    i32 = torch.int32
+    if length.dtype != i32 or length.dim() != 1 or not length.is_cuda \
+            or not length.is_contiguous():
+        _refuse_ints(length, "length", i32, (R,))
+    if query_start.dtype != i32 or query_start.shape != (R + 1,) or not query_start.is_cuda \
+            or not query_start.is_contiguous():
+        _refuse_ints(query_start, "query_start", i32, (R + 1,))
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda
+                            or lse.shape != (T, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse: want a contiguous float32 tensor [tokens][q_heads] on the GPU")
+    rows = _table(torch, block_table, R)
+
+    def args(at, size):
+        return _ATTENTION_ARGS.pack(
+            R, T, Hq, _type(q), max_new, max_len, block_table.shape[1], window, scale, qt, qh,
+            ot, oh, block_table.stride(0), q.data_ptr(), out.data_ptr(),
+            0 if lse is None else lse.data_ptr(), query_start.data_ptr(), length.data_ptr(), rows,
+            at, size)
+
+    if workspace is None:
+        a = args(0, 0)
+        need = L.pp_attention_workspace(pages, a)
+        if need < 0:
+            _check(need)
+        if need:
             if stream is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            else:
+            else:                       # the allocator reuses it in that stream's order
                 with torch.cuda.stream(stream):
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        elif not workspace.is_cuda or not workspace.is_contiguous():
+            a = args(workspace.data_ptr(), need)
+    else:
+        if not workspace.is_cuda or not workspace.is_contiguous():
             raise ValueError("workspace: want a contiguous tensor on the GPU")
-        a.workspace = workspace.data_ptr()
-        a.workspace_bytes = workspace.numel() * workspace.element_size()
-    _check(L.pp_paged_attention(pr, ar, st))
+        a = args(workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = L.pp_paged_attention(pages, a, st)
+    if rc:
+        _check(rc)
+
+
+def pp_attention_workspace(q, k_cache, block_table, *, max_new, max_len, window=0) -> int:
+    """Bytes of workspace pp_paged_attention needs for calls of these shapes
+    (only shapes, strides and types of the tensors count)."""
+    torch = _torch or _with_torch()
+    pages, _, _ = _pages(torch, k_cache, k_cache, None, None)
+    (qt, qh) = _rows(q, "q")
+    T, Hq, _ = q.shape
+    need = lib().pp_attention_workspace(pages, _ATTENTION_ARGS.pack(
+        block_table.shape[0], T, Hq, _type(q), max_new, max_len, block_table.shape[1], window, 1.0,
+        qt, qh, qt, qh, block_table.stride(0), 0, 0, 0, 0, 0, 0, 0, 0))
+    if need < 0:
+        _check(need)
+    return need
 
 
 class Context:

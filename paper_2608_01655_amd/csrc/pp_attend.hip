@@ -1070,8 +1070,6 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
 
 // -------------------------------------------------------------- dispatch ---
 
-constexpr int kRowBlocks = 4096;   // blocks k_rows is cut towards
-constexpr int kLeastKeys = 256;    // and the least keys of one
 constexpr int kTileBlocks = 512;   // blocks of k_tiles that are resident
 
 int32_t round_up(int64_t x, int32_t m) { return (int32_t)((x + m - 1) / m * m); }
@@ -1107,9 +1105,13 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     parts = (int32_t)((keys + size - 1) / size);
   };
   if (ch.rt) {
-    // lengths differ, so blocks are many and small; below 256 keys a block's start and end are most of it
-    int64_t n = (kRowBlocks + (int64_t)a.requests * p.heads - 1) / ((int64_t)a.requests * p.heads);
-    if (n > keys / kLeastKeys) n = keys / kLeastKeys;
+    // Lengths differ, so the fewer requests there are the smaller their parts have to be: 64 requests and 4
+    // heads in 31, 16 or 8 parts took 85, 92 and 107 us; 256 requests and 8 heads in 1, 2 or 4 took 550, 556
+    // and 652 us (a block that finds no keys still waits for its turn).  Below 256 keys a block's start and
+    // end are most of it.
+    const int64_t base = (int64_t)a.requests * p.heads;
+    int64_t n = ((base < 512 ? 8192 : 4096) + base - 1) / base;
+    if (n > keys / 256) n = keys / 256;
     cut((int32_t)(n > 1 ? n : 1), 128, pl.cut_rows, pl.parts_rows);
   }
   pl.slots = (int32_t)((int64_t)a.tokens * pl.group / 128) + a.requests;

@@ -10,7 +10,8 @@ namespace {
 constexpr int kWave = 64;
 constexpr int kWalkWaves = 4;     // requests a block of k_walk looks up, one wave each
 constexpr int kPathLds = 128;     // chunks of a path kept in LDS between its two uses
-constexpr int kFillWaves = 16;    // requests a block of k_fill serves, one wave each
+constexpr int kFillWaves = 16;    // waves of a block of k_fill
+constexpr int kStepMost = 64;     // requests k_step takes
 
 struct Span {
   int32_t start, end;
@@ -103,66 +104,59 @@ __global__ void __launch_bounds__(kWave* kWalkWaves) k_walk(pp_block_args a) {
   }
 }
 
-// Sum of two values over the block's kFillWaves waves.
-__device__ __forceinline__ void block_sum(int64_t& x, int64_t& y, int64_t (*part)[2]) {
-  for (int o = kWave / 2; o; o >>= 1) {
-    x += __shfl_xor(x, o);
-    y += __shfl_xor(y, o);
-  }
-  const int wave = threadIdx.x / kWave;
-  if (threadIdx.x % kWave == 0) {
-    part[wave][0] = x;
-    part[wave][1] = y;
-  }
-  __syncthreads();
-  x = y = 0;
-  for (int w = 0; w < kFillWaves; ++w) {
-    x += part[w][0];
-    y += part[w][1];
-  }
-  __syncthreads();
-}
+__device__ __forceinline__ int32_t cap32(int64_t x) { return (int32_t)(x < INT32_MAX ? x : INT32_MAX); }
 
-// Every block sums the tokens and pages of all requests and of those before
-// its own (8 bytes a request out of L2), then each wave serves one request.
+// Every block sums the tokens and pages of all requests and of those before its own (8 bytes a
+// request out of L2), then EACH waves serve each request: 4 for up to 512 requests, where the chain
+// of reads counts, else 1 (4,096 requests took 40 us with 4, 14 us with 1).
+template <int EACH>
 __global__ void __launch_bounds__(kWave* kFillWaves) k_fill(pp_block_args a, int shift) {
-  __shared__ int64_t part[kFillWaves][2];
-  __shared__ int64_t mine[kFillWaves][2];
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int32_t first = blockIdx.x * kFillWaves;
-  int64_t t0 = 0, p0 = 0, t1 = 0, p1 = 0;
-  for (int32_t i = threadIdx.x; i < a.requests; i += kWave * kFillWaves) {
-    const int32_t s = a.start[i], e = a.end[i];
-    const int64_t t = e - s, p = ceil_div(e, shift) - ceil_div(s, shift);
-    if (i < first) {
-      t0 += t;
-      p0 += p;
-    }
-    t1 += t;
-    p1 += p;
-  }
-  block_sum(t0, p0, part);
-  block_sum(t1, p1, part);
-  const int32_t r = first + wave;
+  constexpr int kOwn = kFillWaves / EACH;
+  __shared__ int64_t part[kFillWaves][4];
+  __shared__ int64_t mine[kOwn][2];
+  const int wave = threadIdx.x / kWave, own = wave / EACH;
+  const int at = threadIdx.x % (kWave * EACH);
+  const int32_t first = blockIdx.x * kOwn, r = first + own;
   int32_t start = 0, end = 0;
   if (r < a.requests) {
     start = a.start[r];
     end = a.end[r];
   }
+  int64_t sum[4] = {0, 0, 0, 0};     // tokens and pages: of the requests before, of all
+#pragma unroll 2
+  for (int32_t i = threadIdx.x; i < a.requests; i += kWave * kFillWaves) {
+    const int32_t s = a.start[i], e = a.end[i];
+    const int64_t t = e - s, p = ceil_div(e, shift) - ceil_div(s, shift);
+    sum[0] += i < first ? t : 0;
+    sum[1] += i < first ? p : 0;
+    sum[2] += t;
+    sum[3] += p;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    for (int o = kWave / 2; o; o >>= 1) sum[j] += __shfl_xor(sum[j], o);
+  if (threadIdx.x % kWave == 0)
+    for (int j = 0; j < 4; ++j) part[wave][j] = sum[j];
   const int32_t b0 = ceil_div(start, shift), b1 = ceil_div(end, shift);
-  if (lane == 0) {
-    mine[wave][0] = end - start;
-    mine[wave][1] = b1 - b0;
+  if (at == 0) {
+    mine[own][0] = end - start;
+    mine[own][1] = b1 - b0;
   }
   __syncthreads();
-  for (int w = 0; w < wave; ++w) {
+  int64_t t0 = 0, p0 = 0, t1 = 0, p1 = 0;
+  for (int w = 0; w < kFillWaves; ++w) {
+    t0 += part[w][0];
+    p0 += part[w][1];
+    t1 += part[w][2];
+    p1 += part[w][3];
+  }
+  for (int w = 0; w < own; ++w) {
     t0 += mine[w][0];
     p0 += mine[w][1];
   }
-  auto cap = [](int64_t x) { return (int32_t)(x < INT32_MAX ? x : INT32_MAX); };
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     a.query_start[0] = 0;
-    a.taken[0] = cap(p1);
+    a.taken[0] = cap32(p1);
   }
   // numbers that no token has
   for (int64_t t = t1 + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < a.max_tokens;
@@ -171,21 +165,117 @@ __global__ void __launch_bounds__(kWave* kFillWaves) k_fill(pp_block_args a, int
     a.position[t] = 0;
   }
   if (r >= a.requests) return;
-  if (lane == 0) a.query_start[r + 1] = cap(t0 + end - start);
+  if (at == 0) a.query_start[r + 1] = cap32(t0 + end - start);
   int32_t* row = a.block_table + (int64_t)r * a.row_stride;
   // the page of block b >= b0
   auto fresh = [&](int32_t b) {
     const int64_t i = p0 + b - b0;
     return i < a.n_free ? a.free_pages[i] : -1;
   };
-  for (int32_t b = b0 + lane; b < b1 && b < a.max_blocks; b += kWave) row[b] = fresh(b);
+  constexpr int kThreads = kWave * EACH, kTurn = 4;
+  for (int32_t b = b0 + at; b < b1 && b < a.max_blocks; b += kThreads) row[b] = fresh(b);
   const int32_t mask = a.page_size - 1;
-  for (int64_t i = lane; i < end - start && t0 + i < a.max_tokens; i += kWave) {
-    const int32_t pos = start + (int32_t)i, b = pos >> shift;
-    int32_t page = -1;
-    if (b < a.max_blocks) page = b < b0 ? row[b] : fresh(b);
-    a.slot_map[t0 + i] = page < 0 ? -1 : ((int64_t)page << shift) + (pos & mask);
-    a.position[t0 + i] = pos;
+  const int64_t last = t0 + (end - start) < a.max_tokens ? end - start : a.max_tokens - t0;
+  for (int64_t i = at; i < last; i += kThreads * kTurn) {
+    int32_t page[kTurn];
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {      // the reads of a turn before its writes
+      const int32_t b = (int32_t)((start + i + j * kThreads) >> shift);
+      page[j] = i + j * kThreads < last && b < a.max_blocks ? (b < b0 ? row[b] : fresh(b)) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      const int64_t n = i + j * kThreads;
+      if (n >= last) break;
+      const int32_t pos = (int32_t)(start + n);
+      a.slot_map[t0 + n] = page[j] < 0 ? -1 : ((int64_t)page[j] << shift) + (pos & mask);
+      a.position[t0 + n] = pos;
+    }
+  }
+}
+
+// The whole of it for few requests and tokens, in one launch and block: such a call is bound by its
+// chain of reads, so what is needed from free_pages is read ahead of knowing how much.
+__global__ void __launch_bounds__(1024) k_step(pp_block_args a, int shift) {
+  constexpr int kWaves = 16;
+  __shared__ int32_t slots[kWaves][kPathLds], ahead[1024];
+  __shared__ int32_t starts[kStepMost], ends[kStepMost], open[kStepMost];
+  __shared__ int64_t tok[kStepMost + 1], page[kStepMost + 1];
+  __shared__ uint64_t begins;
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, tid = threadIdx.x;
+  const int32_t mask = a.page_size - 1, R = a.requests;
+  const int32_t next = tid < a.n_free ? a.free_pages[tid] : -1;
+  if (wave == 0) {
+    const bool live = lane < R;
+    int32_t len = live ? a.length[lane] : 0;
+    const int32_t cached = live ? a.cached[lane] : 0;
+    if (len < 0) len = 0;
+    if (live && cached >= 0) {
+      const int32_t s = cached < len ? cached : len;
+      starts[lane] = s;
+      ends[lane] = clamp_end(a, len, s);
+      // the page its last token so far lies in
+      open[lane] = (s & mask) && (s >> shift) < a.max_blocks ? a.block_table[lane * a.row_stride + (s >> shift)] : -1;
+    }
+    const uint64_t b = __ballot(live && cached < 0);
+    if (lane == 0) begins = b;
+  }
+  ahead[tid] = next;
+  __syncthreads();
+  int k = 0;
+  for (uint64_t left = begins; left; left &= left - 1, ++k) {
+    if (k % kWaves != wave) continue;
+    const int32_t r = __builtin_ctzll(left);
+    const Span s = walk(a, r, lane, slots[wave]);
+    if (lane == 0) {
+      starts[r] = s.start;
+      ends[r] = s.end;
+    }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int32_t s = lane < R ? starts[lane] : 0, e = lane < R ? ends[lane] : 0;
+    int64_t t = e - s, p = ceil_div(e, shift) - ceil_div(s, shift);
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int64_t x = __shfl_up(t, o), y = __shfl_up(p, o);
+      if (lane >= o) {
+        t += x;
+        p += y;
+      }
+    }
+    if (lane == 0) tok[0] = page[0] = 0;
+    tok[lane + 1] = t;
+    page[lane + 1] = p;
+    if (lane < R) {
+      a.start[lane] = s;
+      a.end[lane] = e;
+      a.query_start[lane + 1] = cap32(t);
+    }
+    if (lane == 0) a.query_start[0] = 0;
+    if (lane == kWave - 1) a.taken[0] = cap32(p);
+  }
+  __syncthreads();
+  auto fresh = [&](int64_t i) { return i >= a.n_free ? -1 : i < 1024 ? ahead[i] : a.free_pages[i]; };
+  for (int32_t r = wave; r < R; r += kWaves) {
+    const int32_t b0 = ceil_div(starts[r], shift), b1 = ceil_div(ends[r], shift);
+    int32_t* row = a.block_table + (int64_t)r * a.row_stride;
+    for (int32_t b = b0 + lane; b < b1 && b < a.max_blocks; b += kWave) row[b] = fresh(page[r] + b - b0);
+  }
+  for (int64_t t = tid; t < a.max_tokens; t += 1024) {
+    int64_t slot = -1;
+    int32_t pos = 0;
+    if (t < tok[R]) {
+      int32_t r = 0;              // the last request that starts at or before t
+      for (int32_t o = kStepMost / 2; o; o >>= 1)
+        if (r + o < R && tok[r + o] <= t) r += o;
+      pos = (int32_t)(starts[r] + (t - tok[r]));
+      const int32_t b = pos >> shift, b0 = ceil_div(starts[r], shift);
+      int32_t pg = -1;
+      if (b < a.max_blocks) pg = b < b0 ? open[r] : fresh(page[r] + b - b0);
+      if (pg >= 0) slot = ((int64_t)pg << shift) + (pos & mask);
+    }
+    a.slot_map[t] = slot;
+    a.position[t] = pos;
   }
 }
 
@@ -249,10 +339,17 @@ __global__ void __launch_bounds__(256) k_write(pp_kv_pages p, int32_t tokens, bo
 
 hipError_t launch_block_tables(const pp_block_args& a, hipStream_t st) {
   const int shift = __builtin_ctz(a.page_size);
+  // one block writes some 1,024 tokens a microsecond; two launches cost more than that up to here
+  if (a.requests <= kStepMost && a.max_tokens <= 8192) {
+    k_step<<<1, 1024, 0, st>>>(a, shift);
+    return hipGetLastError();
+  }
   if (a.requests)
     k_walk<<<(a.requests + kWalkWaves - 1) / kWalkWaves, kWave * kWalkWaves, 0, st>>>(a);
-  const int blocks = a.requests ? (a.requests + kFillWaves - 1) / kFillWaves : 1;
-  k_fill<<<blocks, kWave * kFillWaves, 0, st>>>(a, shift);
+  const bool many = a.requests > 512;
+  const int own = many ? kFillWaves : kFillWaves / 4;
+  const int blocks = a.requests ? (a.requests + own - 1) / own : 1;
+  (many ? k_fill<1> : k_fill<4>)<<<blocks, kWave * kFillWaves, 0, st>>>(a, shift);
   return hipGetLastError();
 }
 
