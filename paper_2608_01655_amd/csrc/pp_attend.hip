@@ -984,39 +984,36 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
 
 // ---------------------------------------------------------------- k_join ---
 
-// One wave a (token, query head) of a request in several parts.  Bound by the chain of its loads, so
-// the log sums are read before it is known how many count, and four parts' values at a time.
-// few_rows: a wave's number is one of few_rows rows of one of the key heads of a request of k_rows
-// (where no request of k_tiles is in parts); 0: it is a row of the call.
+// Rows of requests in several parts: a wave takes 256 / D of them, four values a lane.  Bound by the
+// chain of its loads, so eight parts are read at a time, their log sums with them.
+// few_rows: a wave's rows are some of few_rows rows of one of the key heads of a request of k_rows
+// (where no request of k_tiles is in parts); 0: they are heads of one of the call's tokens.
 template <bool F16, int D>
-__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int32_t most, int32_t few_rows,
-                                              int32_t heads) {
-  constexpr int N = D / kWave;
-  typedef __attribute__((__vector_size__(N * 4))) float fN;
-  const int lane = threadIdx.x % kWave;
+__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int32_t few_rows, int32_t heads) {
+  constexpr int kRows = 256 / D, kTurn = 8;
+  const int lane = threadIdx.x % kWave, sub = lane / (D / 4), d = lane % (D / 4) * 4;
   const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t step = (int64_t)a.tokens * a.q_heads;
-  int64_t at;
   int32_t t, g, parts;
-  float own = -INFINITY;
+  bool live;
   if (few_rows) {
-    const int32_t row = (int32_t)(id % few_rows), h = (int32_t)(id / few_rows % heads);
-    const int64_t r = id / few_rows / heads;
+    const int32_t each = (few_rows + kRows - 1) / kRows;
+    const int32_t row = (int32_t)(id % each) * kRows + sub, h = (int32_t)(id / each % heads);
+    const int64_t r = id / each / heads;
     if (r >= a.requests) return;
     const Request q = request(a, pl, (int32_t)r);
     const int64_t rows = (int64_t)q.count * pl.group;
-    if (row >= rows || rows > pl.few) return;
+    if (rows > pl.few) return;
+    live = row < rows;
     parts = parts_of(q, pl.cut_rows, pl.parts_rows);
     t = q.first + row / pl.group;
     g = h * pl.group + row % pl.group;
-    at = (int64_t)t * a.q_heads + g;
-    if (lane < most) own = pl.part_lse[lane * step + at];
   } else {
-    at = id;
-    if (at >= step) return;
-    if (lane < most) own = pl.part_lse[lane * step + at];
-    t = (int32_t)(at / a.q_heads);
-    g = (int32_t)(at % a.q_heads);
+    const int32_t each = (a.q_heads + kRows - 1) / kRows;
+    if (id / each >= a.tokens) return;
+    t = (int32_t)(id / each);
+    g = (int32_t)(id % each) * kRows + sub;
+    live = g < a.q_heads;
     const int32_t r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
     if (r < 0) return;
     const Request q = request(a, pl, r);
@@ -1024,48 +1021,38 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
     parts = (int64_t)q.count * pl.group <= pl.few ? parts_of(q, pl.cut_rows, pl.parts_rows)
                                                   : parts_of(q, pl.cut_tiles, pl.parts_tiles);
   }
-  if (parts == 1) return;
+  if (parts == 1 || !live) return;
+  const int64_t at = (int64_t)t * a.q_heads + g;
+  const float* from = pl.part + at * D + d;
   float m = -INFINITY, sum = 0;
-  fN o = {};
-  const float* from = pl.part + at * D + lane * N;
-  for (int32_t base = 0; base < parts; base += kWave) {
-    if (base) own = base + lane < most ? pl.part_lse[(base + lane) * step + at] : -INFINITY;
-    if (base + lane >= parts) own = -INFINITY;
-    float n = own;
-    for (int x = kWave / 2; x; x >>= 1) n = fmaxf(n, __shfl_xor(n, x));
-    n = fmaxf(n, m);
-    if (n == -INFINITY && !__any(own != own)) continue;
+  f32x4 o = {0, 0, 0, 0};
+  for (int32_t base = 0; base < parts; base += kTurn) {
+    float x[kTurn];
+    f32x4 y[kTurn];
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      const int32_t i = base + j < parts ? base + j : parts - 1;
+      x[j] = pl.part_lse[i * step + at];
+      y[j] = *(const f32x4*)(from + i * step * D);
+    }
+    float n = m;
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) n = fmaxf(n, x[j]);
     const float al = m == -INFINITY ? 0.f : exp2_(m - n);
-    m = n;
-    float w = own == -INFINITY ? 0.f : own == n ? 1.f : exp2_(own - n);
     o *= al;
     sum *= al;
-    const int32_t here = parts - base < kWave ? parts - base : kWave;
-    for (int32_t i = 0; i < here; i += 4) {
-      fN x[4];
-      float wi[4];
+    m = n;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {      // a part of weight 0 may never have been written
-        wi[j] = i + j < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (i + j) & 63)) : 0.f;
-        x[j] = fN{};
-        if (wi[j] != 0) x[j] = *(const fN*)(from + (base + i + j) * step * D);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        o += wi[j] * x[j];
-        sum += wi[j];
-      }
+    for (int j = 0; j < kTurn; ++j) {
+      if (base + j >= parts || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
+      const float w = x[j] == n ? 1.f : exp2_(x[j] - n);
+      sum += w;
+      o += w * y[j];
     }
   }
-  uint16_t* out = (uint16_t*)a.out + t * a.out_token_stride + g * a.out_head_stride + lane * N;
   o *= sum == 0 ? 0.f : 1.f / sum;
-  if constexpr (N == 1) {
-    out[0] = (uint16_t)pack2<F16>(o[0], 0.f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; j += 2) *(int*)(out + j) = pack2<F16>(o[j], o[j + 1]);
-  }
-  if (a.lse && lane == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
+  store4<F16>(a, t, g, d, o);
+  if (a.lse && d == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }
 
 // -------------------------------------------------------------- dispatch ---
@@ -1176,13 +1163,13 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, 
     if (ch.rt == 4) e = go_rows<F16, NARROW, D, 4>(p, a, pl, st);
   if (e != hipSuccess) return e;
   if (ch.join) {
-    int64_t few_rows = 0, rows = (int64_t)a.tokens * a.q_heads;
+    constexpr int kRows = 256 / D;
+    int64_t few_rows = 0, waves = (int64_t)a.tokens * ((a.q_heads + kRows - 1) / kRows);
     if (pl.parts_tiles == 1) {
       few_rows = (int64_t)a.max_new * pl.group < pl.few ? (int64_t)a.max_new * pl.group : pl.few;
-      rows = (int64_t)a.requests * p.heads * few_rows;
+      waves = (int64_t)a.requests * p.heads * ((few_rows + kRows - 1) / kRows);
     }
-    k_join<F16, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(
-        a, pl, pl.parts_rows > pl.parts_tiles ? pl.parts_rows : pl.parts_tiles, (int32_t)few_rows, p.heads);
+    k_join<F16, D><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)few_rows, p.heads);
     e = hipGetLastError();
   }
   return e;
