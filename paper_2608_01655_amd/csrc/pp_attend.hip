@@ -724,24 +724,28 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   auto buffer = [&](int32_t t) { return (uint32_t)((t ^ flip) & 1) * kTile; };
   int32_t held = 0, next_k = 0, next_v = 0;
   int64_t place = 0;              // of tile next_v
-  auto bring = [&](const char* from, uint32_t to, uint32_t off, auto swizzle) {
-    to = __builtin_amdgcn_readfirstlane(to + wave * 16 * RB);
-    each<kLoads>([&](auto i) {
-      load_lds_at<i * 1024>(to, off_row + (off ^ (swizzle(i * kRowsPerLoad) * 16)), from + i * kRowsPerLoad * tok32);
-    });
+  auto bring_k = [&](auto i, const char* from, uint32_t to) {
+    load_lds_at<i * 1024>(to, off_row + (off_k ^ (Sw::k(i * kRowsPerLoad) * 16)), from + i * kRowsPerLoad * tok32);
+  };
+  auto bring_v = [&](auto i, const char* from, uint32_t to) {
+    load_lds_at<i * 1024>(to, off_row + (off_v ^ (Sw::v(i * kRowsPerLoad, NARROW) * 16)), from + i * kRowsPerLoad * tok32);
+  };
+  const uint32_t own = __builtin_amdgcn_readfirstlane(lds + wave * 16 * RB);
+  auto place_of = [&](int32_t t) {
+    if ((t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (t + lane) * 64 + wave * 16);
+    const uint32_t page = __builtin_amdgcn_readlane(held, t & 63);
+    place = (int64_t)page * page_b + ((kbase + t * 64 + wave * 16) & (p.page_size - 1)) * tok32;
   };
   auto issue_k = [&] {
     const int32_t t = next_k++;
     if (t >= nt) return;
-    if ((t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (t + lane) * 64 + wave * 16);
-    const uint32_t page = __builtin_amdgcn_readlane(held, t & 63);
-    place = (int64_t)page * page_b + ((kbase + t * 64 + wave * 16) & (p.page_size - 1)) * tok32;
-    bring(kh + place, lds + buffer(t), off_k, [](int x) { return Sw::k(x); });
+    place_of(t);
+    each<kLoads>([&](auto i) { bring_k(i, kh + place, own + buffer(t)); });
   };
   auto issue_v = [&] {            // before issue_k moves on
     const int32_t t = next_v++;
     if (t >= nt) return;
-    bring(vh + place, lds + 2 * kTile + buffer(t), off_v, [](int x) { return Sw::v(x, NARROW); });
+    each<kLoads>([&](auto i) { bring_v(i, vh + place, own + 2 * kTile + buffer(t)); });
   };
 
   f32x16 acc[DB];
@@ -800,8 +804,8 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
     return mx;
   };
-  auto rescale = [&](float old) {
-    const float al = old == -INFINITY ? 0.f : exp2_((old - m) * c);
+  auto rescale = [&](float from, float to) {
+    const float al = from == -INFINITY ? 0.f : exp2_((from - to) * c);
     l *= al;
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] *= al;
@@ -821,9 +825,9 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     }
     const float mx = over_halves(largest(s), Max());
     if (grows(mx)) {
-      const float old = m;
-      m = fmaxf(m, mx);
-      rescale(old);
+      const float to = fmaxf(m, mx);
+      rescale(m, to);
+      m = to;
     }
     const float mc = m == -INFINITY ? 0.f : m * c;
     float w[16];
@@ -875,8 +879,14 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     m = grow ? fmaxf(m, mx) : m;
     mc = m == -INFINITY ? 0.f : m * c;
   };
-  auto step = [&](const f32x16& cur, f32x16& next, uint32_t k_next, uint32_t v_last, auto first) {
-    constexpr int NV = decltype(first)::value ? 0 : 2 * DB, NM = KS + NV, kAhead = 3;
+  constexpr int kAhead = 3;       // fragments read ahead of their use
+  s16x8 pre[kAhead];              // the first ones of the next step, where no barrier comes before it
+  constexpr std::integral_constant<int, 0> kFirst{};     // nothing before it yet
+  constexpr std::integral_constant<int, 1> kTurn{};      // behind a barrier, with loads to issue
+  constexpr std::integral_constant<int, 2> kSecond{};    // `pre` is there
+  auto step = [&](const f32x16& cur, f32x16& next, uint32_t k_next, uint32_t v_last, auto kind, auto beside) {
+    constexpr int kKind = decltype(kind)::value;
+    constexpr int NV = kKind == 0 ? 0 : 2 * DB, NM = KS + NV;
     s16x8 f[NM], x[2];
     auto read = [&](auto at) {
       constexpr int i = decltype(at)::value;
@@ -884,18 +894,25 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
       else f[i] = v_frag(v_last + (i - KS) % 2 * 16 * RB, (i - KS) / 2);
     };
     float w[16], sum = 0, mx = -INFINITY;
+    const float mc_now = mc, m_now = m, old_now = old;
+    const bool grow_now = grow;
     f32x16 y;
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = 0;
-    each<kAhead>(read);
+    each<kAhead>([&](auto i) {
+      if constexpr (kKind == 2) f[i] = pre[i];
+      else read(i);
+    });
     each<NM>([&](auto at) {
       constexpr int i = decltype(at)::value;
       if constexpr (i + kAhead < NM) read(std::integral_constant<int, i + kAhead>());
+      else if constexpr (kKind == 1) pre[i + kAhead - NM] = k_frag(k_next + 32 * RB, i + kAhead - NM);
       if constexpr (i < KS) y = mfma32<F16>(f[i], qf[i], y);
       else acc[(i - KS) / 2] = mfma32<F16>(f[i], pf[(i - KS) % 2], acc[(i - KS) / 2]);
+      beside(at);
 #pragma unroll
       for (int j = i * 16 / NM; j < (i + 1) * 16 / NM; ++j) {
-        w[j] = exp2_(__builtin_fmaf(cur[j], c, -mc));
+        w[j] = exp2_(__builtin_fmaf(cur[j], c, -mc_now));
         asm volatile("" : "+v"(w[j]));   // here, and not behind the branch at the end: so for the others
         sum += w[j];
       }
@@ -904,11 +921,15 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
         x[0] = pack8<F16>(w);
         asm volatile("" : "+v"(x[0]));
       }
-      if constexpr (i >= KS) {
+      if constexpr (i >= KS && i < NM - 1) {
         constexpr int q = i - KS;     // the scores are there a little after their last instruction
 #pragma unroll
-        for (int j = q > 0 ? (q - 1) * 16 / (NV - 1) : 0; j < q * 16 / (NV - 1); ++j) mx = fmaxf(mx, y[j]);
+        for (int j = q > 0 ? (q - 1) * 16 / (NV - 2) : 0; j < q * 16 / (NV - 2); ++j) mx = fmaxf(mx, y[j]);
         asm volatile("" : "+v"(mx));
+        if constexpr (i == NM - 2) {
+          peak(mx);
+          asm volatile("" : "+v"(m), "+v"(mc));
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -917,9 +938,9 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     next = y;
     pf[0] = x[0];
     pf[1] = x[1];
-    if (grow) rescale(old);
+    if (grow_now) rescale(old_now, m_now);
     l += sum;
-    peak(NV ? mx : largest(y));
+    if constexpr (NV == 0) peak(largest(y));
   };
 
   issue_k();
@@ -934,22 +955,32 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     issue_k();
     even = scores(0);
     peak(largest(even));
-    step(even, odds, kHalf, 0, std::true_type());
+    const auto nothing = [](auto) {};
+    step(even, odds, kHalf, 0, kFirst, nothing);
     auto turn = [&](auto buf) {   // K of t + 1 and V of t are there; K of t and V of t - 1 are read
-      constexpr uint32_t k = (1 - decltype(buf)::value) * kTile, v = decltype(buf)::value * kTile;
+      constexpr uint32_t other = (1 - decltype(buf)::value) * kTile, same = decltype(buf)::value * kTile;
       wait_loads<0>();
       barrier();
-      issue_v();
-      issue_k();
-      step(odds, even, k, v, std::false_type());
+      // V of t + 1 and K of t + 2, or some tile again where there are no more
+      const char* vp = vh + place;
+      place_of(next_k < nt ? next_k : nt - 1);
+      const char* kp = kh + place;
+      ++next_k;
+      ++next_v;
+      __builtin_amdgcn_s_setprio(1);   // over the other block's wave, until this one is ahead: 1.08 to 1.06 ms
+      step(odds, even, other, same, kTurn, [&](auto i) {
+        if constexpr (i < kLoads) bring_v(i, vp, own + 2 * kTile + other);
+        else if constexpr (i < 2 * kLoads) bring_k(std::integral_constant<int, i - kLoads>(), kp, own + same);
+      });
+      __builtin_amdgcn_s_setprio(0);
       ++t;
     };
     for (;;) {
       turn(std::integral_constant<int, 0>());
-      step(even, odds, kTile + kHalf, kHalf, std::false_type());
+      step(even, odds, kTile + kHalf, kHalf, kSecond, nothing);
       turn(std::integral_constant<int, 1>());
       if (t == tail) break;
-      step(even, odds, kHalf, kTile + kHalf, std::false_type());
+      step(even, odds, kHalf, kTile + kHalf, kSecond, nothing);
     }
     m = old;                      // the scores past the last tile are nobody's
     each<2 * DB>([&](auto i) {
@@ -957,6 +988,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     });
   }
   for (; t < nt; ++t) masked_tile(t);
+  wait_loads<0>();                // the last loads of a tile that was there already
 
   l = over_halves(l, Sum());
   if (!live) return;
