@@ -527,8 +527,8 @@ int pp_block_tables(const pp_block_args *args, void *hip_stream);
 /* One layer's pages: element (page, head, token, i) of k and of v lies at
  * page * page_stride + head * head_stride + token * token_stride + i
  * elements (any order of the three).  PP_E4M3 pages hold value / scale of
- * their head, k_scale and v_scale [heads] (device; NULL = 1); other types
- * have no scales. */
+ * their head, k_scale and v_scale [heads] (device; NULL = 1; finite and
+ * above 0, which the host cannot see); other types have no scales. */
 typedef struct {
     void *k, *v;
     const float *k_scale, *v_scale;
@@ -563,8 +563,9 @@ int pp_kv_write(const pp_kv_pages *pages, int32_t tokens, int32_t dtype,
  * the last as the last; tokens past a row of the block table do not exist.
  * Scores, sums and the accumulation are held in 32 bits; weights are rounded
  * to the queries' type for the product with V.
- * max_new and max_len bound every request's new tokens and length; new
- * tokens past max_new may be left unwritten.  `workspace` is device memory
+ * max_new and max_len bound every request's new tokens and length; a request
+ * of more than max_new new tokens may be left unwritten, and rows of tokens
+ * that no request has are.  `workspace` is device memory
  * of pp_attention_workspace bytes at least (256-byte aligned); the call
  * writes it before it reads it, so its contents need not be kept. */
 typedef struct {

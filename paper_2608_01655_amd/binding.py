@@ -578,20 +578,24 @@ def _with_torch():
 
 
 def _stream_of(torch, t, stream):
-    """The stream to enqueue on, where tensor `t` lies."""
+    """(the GPU that every tensor of the call has to lie on, the stream to enqueue on)."""
     device = t.get_device()
     if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError("tensors must lie on the current GPU")
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if stream is None:
+        return device, torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError("the stream is another GPU's")
+    return device, stream.cuda_stream
 
 
 def _refuse_ints(t, what, dtype, shape):
     raise ValueError(f"{what}: want a contiguous {dtype} tensor of shape {tuple(shape)} on the "
-                     f"GPU, got {t.dtype} {tuple(t.shape)}")
+                     f"current GPU, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _table(torch, t, R):
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] != R \
+def _table(torch, t, R, device):
+    if t.dtype != torch.int32 or t.get_device() != device or t.dim() != 2 or t.shape[0] != R \
             or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError("block_table: want int32 rows, one a request, on the GPU")
     return t.data_ptr()
@@ -607,7 +611,7 @@ def pp_block_tables(leaf, length, cached, prefix_table, slot, free_pages, block_
     query_start int32 [R + 1], start, end int32 [R], slot_map int64 [t],
     position int32 [t], taken int32 [1]."""
     torch = _torch or _with_torch()
-    st = _stream_of(torch, length, stream)
+    device, st = _stream_of(torch, length, stream)
     i32 = torch.int32
     R, n, f, t = length.shape[0], slot.shape[0], free_pages.shape[0], slot_map.shape[0]
     at = []
@@ -617,13 +621,14 @@ def pp_block_tables(leaf, length, cached, prefix_table, slot, free_pages, block_
             (free_pages, (f,), "free_pages"), (query_start, (R + 1,), "query_start"),
             (start, (R,), "start"), (end, (R,), "end"), (position, (t,), "position"),
             (taken, (1,), "taken")):
-        if x.dtype != i32 or x.shape != shape or not x.is_cuda or not x.is_contiguous():
+        if x.dtype != i32 or x.shape != shape or x.get_device() != device \
+                or not x.is_contiguous():
             _refuse_ints(x, what, i32, shape)
         at.append(x.data_ptr())
-    if slot_map.dtype != torch.int64 or slot_map.dim() != 1 or not slot_map.is_cuda \
-            or not slot_map.is_contiguous():
+    if slot_map.dtype != torch.int64 or slot_map.dim() != 1 \
+            or slot_map.get_device() != device or not slot_map.is_contiguous():
         _refuse_ints(slot_map, "slot_map", torch.int64, ("t",))
-    rows = _table(torch, block_table, R)
+    rows = _table(torch, block_table, R, device)
     rc = lib().pp_block_tables(_BLOCK_ARGS.pack(
         R, n, n_slots, f, block_table.shape[1], t, page_size, chunk_tokens, max_new,
         block_table.stride(0), at[0], at[1], at[2], at[3], at[4], at[5], rows, at[6], at[7],
@@ -639,9 +644,9 @@ def _type(t):
         raise ValueError(f"no rows or pages of {t.dtype}") from None
 
 
-def _rows(t, what):
+def _rows(t, what, device):
     """(token stride, head stride) of device rows [tokens][heads][dim]."""
-    if t.dim() != 3 or not t.is_cuda:
+    if t.dim() != 3 or t.get_device() != device:
         raise ValueError(f"{what}: want [tokens][heads][dim] on the GPU, dim contiguous")
     token, head, one = t.stride()
     if one != 1:
@@ -649,25 +654,25 @@ def _rows(t, what):
     return token, head
 
 
-def _scale(torch, s, H):
+def _scale(torch, s, H, device):
     if s is None:
         return 0
-    if s.dtype != torch.float32 or not s.is_cuda or s.shape != (H,) or not s.is_contiguous():
+    if s.dtype != torch.float32 or s.get_device() != device or s.shape != (H,) or not s.is_contiguous():
         raise ValueError("scales: want float32 [heads] on the GPU")
     return s.data_ptr()
 
 
-def _pages(torch, k_cache, v_cache, k_scale, v_scale):
+def _pages(torch, k_cache, v_cache, k_scale, v_scale, device):
     """(packed pp_kv_pages, heads, dim)."""
     strides = k_cache.stride()
     if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or strides != v_cache.stride() \
-            or strides[3] != 1 or k_cache.dtype != v_cache.dtype or not k_cache.is_cuda \
-            or not v_cache.is_cuda:
+            or strides[3] != 1 or k_cache.dtype != v_cache.dtype \
+            or k_cache.get_device() != device or v_cache.get_device() != device:
         raise ValueError("pages: want two device tensors [pages][heads][page_size][dim] "
                          "alike, dim contiguous")
     P, H, ps, D = k_cache.shape
-    return _KV_PAGES.pack(k_cache.data_ptr(), v_cache.data_ptr(), _scale(torch, k_scale, H),
-                          _scale(torch, v_scale, H), _type(k_cache), P, ps, H, D,
+    return _KV_PAGES.pack(k_cache.data_ptr(), v_cache.data_ptr(), _scale(torch, k_scale, H, device),
+                          _scale(torch, v_scale, H, device), _type(k_cache), P, ps, H, D,
                           *strides[:3]), H, D
 
 
@@ -677,13 +682,14 @@ def pp_kv_write(k, v, slot_map, k_cache, v_cache, *, k_scale=None, v_scale=None,
     Pages are [pages][heads][page_size][dim] views in any memory order, of
     the rows' type or float8_e4m3fn."""
     torch = _torch or _with_torch()
-    st = _stream_of(torch, k, stream)
-    pages, H, D = _pages(torch, k_cache, v_cache, k_scale, v_scale)
-    (kt, kh), (vt, vh) = _rows(k, "k"), _rows(v, "v")
+    device, st = _stream_of(torch, k, stream)
+    pages, H, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
+    (kt, kh), (vt, vh) = _rows(k, "k", device), _rows(v, "v", device)
     T = slot_map.shape[0]
     if k.shape != (T, H, D) or v.shape != k.shape or k.dtype != v.dtype:
         raise ValueError("shape mismatch")
-    if slot_map.dtype != torch.int64 or not slot_map.is_cuda or not slot_map.is_contiguous():
+    if slot_map.dtype != torch.int64 or slot_map.get_device() != device \
+            or not slot_map.is_contiguous():
         _refuse_ints(slot_map, "slot_map", torch.int64, (T,))
     rc = lib().pp_kv_write(pages, T, _type(k), k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
                            slot_map.data_ptr(), st)
@@ -701,25 +707,25 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
     [tokens][q_heads] or None.  Without a `workspace` (a tensor that the
     caller keeps) one is taken from torch's allocator for the call."""
     torch = _torch or _with_torch()
-    st = _stream_of(torch, q, stream)
+    device, st = _stream_of(torch, q, stream)
     L = lib()
-    pages, _, D = _pages(torch, k_cache, v_cache, k_scale, v_scale)
-    (qt, qh), (ot, oh) = _rows(q, "q"), _rows(out, "out")
+    pages, _, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
+    (qt, qh), (ot, oh) = _rows(q, "q", device), _rows(out, "out", device)
     T, Hq, d = q.shape
     R = length.shape[0]
     if d != D or out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("shape mismatch")
     i32 = torch.int32
-    if length.dtype != i32 or length.dim() != 1 or not length.is_cuda \
+    if length.dtype != i32 or length.dim() != 1 or length.get_device() != device \
             or not length.is_contiguous():
         _refuse_ints(length, "length", i32, (R,))
-    if query_start.dtype != i32 or query_start.shape != (R + 1,) or not query_start.is_cuda \
-            or not query_start.is_contiguous():
+    if query_start.dtype != i32 or query_start.shape != (R + 1,) \
+            or query_start.get_device() != device or not query_start.is_contiguous():
         _refuse_ints(query_start, "query_start", i32, (R + 1,))
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda
+    if lse is not None and (lse.dtype != torch.float32 or lse.get_device() != device
                             or lse.shape != (T, Hq) or not lse.is_contiguous()):
         raise ValueError("lse: want a contiguous float32 tensor [tokens][q_heads] on the GPU")
-    rows = _table(torch, block_table, R)
+    rows = _table(torch, block_table, R, device)
 
     def args(at, size):
         return _ATTENTION_ARGS.pack(
@@ -741,8 +747,8 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
             a = args(workspace.data_ptr(), need)
     else:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace: want a contiguous tensor on the GPU")
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace: want a contiguous tensor on the current GPU")
         a = args(workspace.data_ptr(), workspace.numel() * workspace.element_size())
     rc = L.pp_paged_attention(pages, a, st)
     if rc:
@@ -753,8 +759,11 @@ def pp_attention_workspace(q, k_cache, block_table, *, max_new, max_len, window=
     """Bytes of workspace pp_paged_attention needs for calls of these shapes
     (only shapes, strides and types of the tensors count)."""
     torch = _torch or _with_torch()
-    pages, _, _ = _pages(torch, k_cache, k_cache, None, None)
-    (qt, qh) = _rows(q, "q")
+    device = q.get_device()
+    if device < 0:
+        raise ValueError("tensors must lie on the GPU")
+    pages, _, _ = _pages(torch, k_cache, k_cache, None, None, device)
+    qt, qh = _rows(q, "q", device)
     T, Hq, _ = q.shape
     need = lib().pp_attention_workspace(pages, _ATTENTION_ARGS.pack(
         block_table.shape[0], T, Hq, _type(q), max_new, max_len, block_table.shape[1], window, 1.0,

@@ -230,8 +230,9 @@ struct Plan {
   int32_t slots;                 // tiles of rows at most, for k_tiles' grid
   float c;                       // |scale| log2(e)
   int32_t negative, shift;
-  float* part;                   // [parts][tokens * q_heads][dim], then the log sums
-  float* part_lse;               // [parts][tokens * q_heads]
+  // normalised parts [parts_tiles][tokens][q_heads][dim] of k_tiles, [parts_rows][requests][heads][few][dim]
+  // of k_rows (which may have many parts, but of few rows), and their log sums
+  float *part, *part_lse, *row_part, *row_lse;
 };
 
 struct Request {
@@ -608,9 +609,9 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
       store4<F16>(a, tk, g, d, o);
       if (a.lse && d == 0) a.lse[(int64_t)tk * a.q_heads + g] = lse / kLog2e;
     } else {
-      const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
-      *(f32x4*)&pl.part[at * D + d] = o;
-      if (d == 0) pl.part_lse[at] = lse;
+      const int64_t at = (((int64_t)part * a.requests + r) * p.heads + h) * pl.few + row;
+      *(f32x4*)&pl.row_part[at * D + d] = o;
+      if (d == 0) pl.row_lse[at] = lse;
     }
   }
 }
@@ -661,7 +662,10 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     first_slot = __builtin_amdgcn_readlane(base, r);
   } else {
     // request r's tiles start at slot floor(first token * G / 128) + r, which leaves it enough of them
-    auto base_of = [&](int32_t i) { return (int32_t)((int64_t)a.query_start[i] * G / 128) + i; };
+    auto base_of = [&](int32_t i) {
+      const int32_t t = a.query_start[i];
+      return (int32_t)((int64_t)(t < 0 ? 0 : t < a.tokens ? t : a.tokens) * G / 128) + i;
+    };
     r = find_last(a.requests, slot, base_of);
     if (r < 0) return;
     first_slot = base_of(r);
@@ -1025,19 +1029,20 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
   constexpr int kRows = 256 / D, kTurn = 8;
   const int lane = threadIdx.x % kWave, sub = lane / (D / 4), d = lane % (D / 4) * 4;
   const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t step = (int64_t)a.tokens * a.q_heads;
-  int32_t t, g, parts;
-  bool live;
+  int32_t t, g, r, row, h;
+  Request q;
+  bool live, few;
   if (few_rows) {
     const int32_t each = (few_rows + kRows - 1) / kRows;
-    const int32_t row = (int32_t)(id % each) * kRows + sub, h = (int32_t)(id / each % heads);
-    const int64_t r = id / each / heads;
-    if (r >= a.requests) return;
-    const Request q = request(a, pl, (int32_t)r);
+    if (id / each / heads >= a.requests) return;
+    r = (int32_t)(id / each / heads);
+    row = (int32_t)(id % each) * kRows + sub;
+    h = (int32_t)(id / each % heads);
+    q = request(a, pl, r);
     const int64_t rows = (int64_t)q.count * pl.group;
     if (rows > pl.few) return;
-    live = row < rows;
-    parts = parts_of(q, pl.cut_rows, pl.parts_rows);
+    few = true;
+    live = row < few_rows && row < rows;
     t = q.first + row / pl.group;
     g = h * pl.group + row % pl.group;
   } else {
@@ -1046,16 +1051,21 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
     t = (int32_t)(id / each);
     g = (int32_t)(id % each) * kRows + sub;
     live = g < a.q_heads;
-    const int32_t r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
+    r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
     if (r < 0) return;
-    const Request q = request(a, pl, r);
-    if (t >= q.first + q.count) return;
-    parts = (int64_t)q.count * pl.group <= pl.few ? parts_of(q, pl.cut_rows, pl.parts_rows)
-                                                  : parts_of(q, pl.cut_tiles, pl.parts_tiles);
+    q = request(a, pl, r);
+    if (t < q.first || t >= q.first + q.count) return;
+    few = (int64_t)q.count * pl.group <= pl.few;
+    row = few ? (t - q.first) * pl.group + g % pl.group : 0;
+    h = g / pl.group;
   }
+  const int32_t parts = few ? parts_of(q, pl.cut_rows, pl.parts_rows) : parts_of(q, pl.cut_tiles, pl.parts_tiles);
   if (parts == 1 || !live) return;
   const int64_t at = (int64_t)t * a.q_heads + g;
-  const float* from = pl.part + at * D + d;
+  const int64_t own = few ? ((int64_t)r * heads + h) * pl.few + row : at;
+  const int64_t step = few ? (int64_t)a.requests * heads * pl.few : (int64_t)a.tokens * a.q_heads;
+  const float* from = (few ? pl.row_part : pl.part) + own * D + d;
+  const float* sums = (few ? pl.row_lse : pl.part_lse) + own;
   float m = -INFINITY, sum = 0;
   f32x4 o = {0, 0, 0, 0};
   for (int32_t base = 0; base < parts; base += kTurn) {
@@ -1064,7 +1074,7 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) {
       const int32_t i = base + j < parts ? base + j : parts - 1;
-      x[j] = pl.part_lse[i * step + at];
+      x[j] = sums[i * step];
       y[j] = *(const f32x4*)(from + i * step * D);
     }
     float n = m;
@@ -1142,7 +1152,9 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     const double part_us = (double)a.tokens * a.q_heads * p.dim * 8 / 4e6;
     double best = 0;
     int32_t n = 1;
-    for (int32_t i = 1; i <= 64 && (i == 1 || tiles / i >= 8); ++i) {
+    const double part_bytes = (double)a.tokens * a.q_heads * p.dim * 4;
+    // 512 MiB of parts at most: calls beyond have so many blocks that cutting gains a percent or two
+    for (int32_t i = 1; i <= 64 && (i == 1 || (tiles / i >= 8 && i * part_bytes <= 0x1p29)); ++i) {
       const double t = std::ceil(blocks * i / kTileBlocks) * (tiles / i + 4) * tile_us + (i > 1 ? 4 + i * part_us : 0);
       if (i == 1 || t < best) {
         best = t;
@@ -1155,9 +1167,16 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
   return ch;
 }
 
-int64_t part_floats(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl) {
-  const int64_t parts = pl.parts_rows > pl.parts_tiles ? pl.parts_rows : pl.parts_tiles;
-  return parts * a.tokens * a.q_heads;
+// Rows of the two regions of parts.
+struct PartRows {
+  int64_t tiles, rows;
+};
+
+PartRows part_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, const Choice& ch) {
+  PartRows n{0, 0};
+  if (ch.tiles && pl.parts_tiles > 1) n.tiles = (int64_t)pl.parts_tiles * a.tokens * a.q_heads;
+  if (ch.rt && pl.parts_rows > 1) n.rows = (int64_t)pl.parts_rows * a.requests * p.heads * pl.few;
+  return n;
 }
 
 template <class K>
@@ -1219,7 +1238,8 @@ hipError_t go_dim(const pp_kv_pages& p, const pp_attention_args& a, const Plan& 
 int64_t attention_workspace(const pp_kv_pages& p, const pp_attention_args& a) {
   Plan pl{};
   const Choice ch = choose(p, a, pl);
-  return ch.join ? part_floats(p, a, pl) * (p.dim + 1) * 4 : 0;
+  const PartRows n = part_rows(p, a, pl, ch);
+  return (n.tiles + n.rows) * (p.dim + 1) * 4;
 }
 
 hipError_t launch_attention(const pp_kv_pages& p, const pp_attention_args& a, hipStream_t st) {
@@ -1228,7 +1248,10 @@ hipError_t launch_attention(const pp_kv_pages& p, const pp_attention_args& a, hi
   pl.negative = a.scale < 0;
   pl.c = (a.scale < 0 ? -a.scale : a.scale) * kLog2e;
   pl.part = (float*)a.workspace;
-  pl.part_lse = pl.part + part_floats(p, a, pl) * p.dim;
+  const PartRows n = part_rows(p, a, pl, ch);
+  pl.row_part = pl.part + n.tiles * p.dim;
+  pl.part_lse = pl.row_part + n.rows * p.dim;
+  pl.row_lse = pl.part_lse + n.tiles;
   const bool narrow = p.dtype == PP_E4M3;
   if (a.dtype == PP_F16) return narrow ? go_dim<true, true>(p, a, pl, ch, st) : go_dim<true, false>(p, a, pl, ch, st);
   return narrow ? go_dim<false, true>(p, a, pl, ch, st) : go_dim<false, false>(p, a, pl, ch, st);

@@ -19,7 +19,8 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Rows whose starts are 16-byte aligned, whatever their numbers.
 bool row_layout(const void* p, int64_t size, int64_t s0, int64_t s1, int64_t s2 = 0) {
-  return aligned16(p) && s0 >= 0 && s1 >= 0 && s2 >= 0 && s0 * size % 16 == 0 &&
+  auto ok = [](int64_t s) { return s >= 0 && s < (int64_t)1 << 48; };   // bytes stay within 64 bits
+  return aligned16(p) && ok(s0) && ok(s1) && ok(s2) && s0 * size % 16 == 0 &&
          s1 * size % 16 == 0 && s2 * size % 16 == 0;
 }
 
@@ -44,8 +45,8 @@ int check_pages(const pp_kv_pages* p, int32_t dtype) {
       !row_layout(p->v, size, p->page_stride, p->head_stride, p->token_stride))
     return report(PP_E_ARG, "page rows start at 16-byte boundaries, at strides >= 0");
   // kernels keep offsets inside a page in 32 bits
-  if ((p->heads - 1) * p->head_stride * size + (p->page_size - 1) * p->token_stride * size +
-          p->dim * size > (int64_t)1 << 31)
+  if (((__int128)(p->heads - 1) * p->head_stride + (__int128)(p->page_size - 1) * p->token_stride +
+       p->dim) * size > (int64_t)1 << 31)
     return report(PP_E_UNSUPPORTED, "one page spans more than 2 GiB");
   return PP_OK;
 }

@@ -198,3 +198,21 @@ def test_paths_of_a_workload(L):
     table = B.pp_prefix_table(inst.parent)
     assert np.array_equal(table[:, 15], inst.depth)
     assert np.array_equal(table[:, 1], inst.parent)
+
+
+@pytest.mark.parametrize("requests,tokens,q_heads,heads,max_new,max_len", [
+    (8, 8192, 64, 8, 2048, 131_072), (33, 16_384, 128, 8, 4096, 1_000_000), (1, 1, 64, 1, 1, 2 ** 30)])
+def test_attention_workspace_stays_small(L, requests, tokens, q_heads, heads, max_new, max_len):
+    """Single tokens beside long prompts: parts of the few rows that are cut, not of every token."""
+    a = _attention(requests=requests, tokens=tokens, q_heads=q_heads, max_new=max_new, max_len=max_len, max_blocks=1000)
+    need = L.pp_attention_workspace(ctypes.byref(_kv_pages(heads=heads)), ctypes.byref(a))
+    rows = 4 * 128 * tokens * q_heads
+    assert 0 <= need < 2 ** 29 + 2 * rows
+
+
+def test_refuses_a_page_whose_span_overflows(L):
+    big = 1 << 47
+    p = _kv_pages(heads=2 ** 30, head_stride=big, token_stride=big, page_stride=big)
+    a = _attention(q_heads=2 ** 30, tokens=1)
+    assert L.pp_attention_workspace(ctypes.byref(p), ctypes.byref(a)) == B.PP_E_UNSUPPORTED
+    assert L.pp_attention_workspace(ctypes.byref(_kv_pages(page_stride=1 << 48)), ctypes.byref(a)) == B.PP_E_ARG
