@@ -1,0 +1,192 @@
+"""One worker's prefix cache from plan to attention, on one attention layer with random weights.
+
+    python examples/prefix_cache.py [--requests 48] [--window 0] [--cache e4m3]
+
+A plan says which chunks of the prefix tree stay on the worker (pp_plan), they get slots
+(pp_cache_slots) and their keys and values are written once (pp_kv_write).  Then requests come:
+every step finds the prefixes of the new ones, hands out pages and places the new tokens
+(pp_block_tables), writes their keys and values (pp_kv_write) and computes their attention
+(pp_paged_attention), prompts in pieces of `max_new` tokens beside the single tokens of requests
+that are past their prompt.
+"""
+
+from __future__ import annotations
+
+import argparse
+import math
+import os
+import sys
+import time
+from dataclasses import dataclass
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2608_01655_amd import binding as B  # noqa: E402
+from paper_2608_01655_amd import workloads as W  # noqa: E402
+
+
+@dataclass
+class Layer:
+    """Tokens to queries, keys and values: embedding and position, then one projection."""
+
+    heads: int
+    kv_heads: int
+    dim: int
+    embed: torch.Tensor         # [vocabulary][width]
+    place: torch.Tensor         # [positions][width]
+    weight: torch.Tensor        # [width][(heads + 2 kv_heads) dim]
+
+    @staticmethod
+    def random(heads=8, kv_heads=2, dim=64, vocabulary=1024, positions=8192, width=256, dtype=torch.bfloat16, seed=0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *shape: torch.randn(shape, generator=g, device="cuda", dtype=dtype)  # noqa: E731
+        return Layer(heads, kv_heads, dim, rand(vocabulary, width), rand(positions, width),
+                     rand(width, (heads + 2 * kv_heads) * dim) / math.sqrt(2 * width))
+
+    def project(self, token, position):
+        """(q, k, v), side by side in one tensor."""
+        x = (self.embed[token] + self.place[position]) @ self.weight
+        return x.view(-1, self.heads + 2 * self.kv_heads, self.dim).split([self.heads, self.kv_heads, self.kv_heads], 1)
+
+
+class Worker:
+    """Pages, slots and running requests of one worker."""
+
+    def __init__(self, layer, parent, target, chunk_tokens, words, *, requests, max_len, page_size=16, pages=None,
+                 cache=torch.bfloat16, window=0):
+        """parent [n] and words [n][chunk_tokens]: the tree and its chunks' tokens; target [n]: what stays here."""
+        self.layer, self.page, self.chunk, self.window, self.requests = layer, page_size, chunk_tokens, window, requests
+        n_slots = int(target.sum())
+        slot, _ = B.pp_cache_slots(target, n_slots)
+        self.n_slots, resident = n_slots, n_slots * (chunk_tokens // page_size)
+        self.blocks = -(-max_len // page_size)
+        pages = resident + requests * self.blocks if pages is None else pages
+        d = self.device = torch.device("cuda")
+        self.lines = torch.from_numpy(B.pp_prefix_table(parent)).to(d)
+        self.slot = torch.from_numpy(slot).to(d)
+        pool = torch.zeros((2, pages, layer.kv_heads, page_size, layer.dim), dtype=cache, device=d)
+        self.k_cache, self.v_cache = pool[0], pool[1]
+        self.scale = dict.fromkeys(("k_scale", "v_scale"))
+        if cache == torch.float8_e4m3fn:     # the largest values here stay far below 448 / 16
+            self.scale = {k: torch.full((layer.kv_heads,), 1 / 16, device=d) for k in self.scale}
+        self.free = list(range(resident, pages))
+        self.table = torch.full((requests, self.blocks), -1, dtype=torch.int32, device=d)
+        self.max_len = max_len
+        # the resident chunks' keys and values, written once
+        node = torch.nonzero(self.slot >= 0).flatten()
+        if node.numel():
+            i = torch.arange(chunk_tokens, device=d)
+            position = (self.lines[node, 15:].long() * chunk_tokens + i).flatten()
+            _, k, v = layer.project(torch.as_tensor(words, device=d)[node].flatten(), position)
+            place = (self.slot[node].long()[:, None] * chunk_tokens + i).flatten()
+            B.pp_kv_write(k, v, place, self.k_cache, self.v_cache, **self.scale)
+
+    def step(self, leaf, tokens, cached, max_new):
+        """One batch step.  leaf [R]; tokens [R]: every request's tokens so far, as lists; cached [R]: how many
+        of them are done (-1: a new request).  Returns (out [t][heads][dim], query_start, start, end)."""
+        R, d, layer = len(leaf), self.device, self.layer
+        put = lambda x: torch.tensor(x, dtype=torch.int32, device=d)  # noqa: E731
+        length = [len(t) for t in tokens]
+        T = sum(min(max_new, n - max(c, 0)) for n, c in zip(length, cached))   # at most
+        most = min(sum(-(-min(max_new, n - max(c, 0)) // self.page) + 1 for n, c in zip(length, cached)), len(self.free))
+        n_length = put(length)
+        empty = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=d)  # noqa: E731
+        query_start, start, end, taken = empty(R + 1), empty(R), empty(R), empty(1)
+        slot_map, position = empty(T, torch.int64), empty(T)
+        B.pp_block_tables(put(leaf), n_length, put(cached), self.lines, self.slot, put(self.free[:most]), self.table[:R],
+                          query_start, start, end, slot_map, position, taken, page_size=self.page,
+                          chunk_tokens=self.chunk, n_slots=self.n_slots, max_new=max_new)
+        # the step's new tokens, which the host picks once it knows what was found
+        starts, ends, used = start.tolist(), end.tolist(), int(taken)
+        if used > most:
+            raise RuntimeError("out of pages")
+        del self.free[:used]
+        new = torch.tensor([x for t, a, b in zip(tokens, starts, ends) for x in t[a:b]], device=d)
+        t = new.shape[0]
+        q, k, v = layer.project(new, position[:t].long())
+        B.pp_kv_write(k, v, slot_map[:t], self.k_cache, self.v_cache, **self.scale)
+        out = torch.empty((t, layer.heads, layer.dim), dtype=q.dtype, device=d)
+        B.pp_paged_attention(q, self.k_cache, self.v_cache, self.table[:R], query_start, end, out,
+                             scale=1 / math.sqrt(layer.dim), window=self.window,
+                             max_new=max(b - a for a, b in zip(starts, ends)), max_len=max(ends), **self.scale)
+        return out, query_start.tolist(), starts, ends
+
+
+def serve(worker, leaf, prompts, decode, max_new, vocabulary=1024):
+    """Serves all requests at once to `decode` tokens behind their prompts; the next token is read off a hash of
+    the attention's output's sign bits, which stands in for the rest of a model.  Returns (tokens, the last
+    prompt token's and each decoded token's outputs, tokens computed, tokens found)."""
+    R = len(leaf)
+    tokens = [list(map(int, p)) for p in prompts]
+    cached, want = [-1] * R, [len(p) + decode for p in prompts]
+    outs = [[] for _ in range(R)]
+    computed = found = 0
+    weigh = torch.arange(1, worker.layer.heads * worker.layer.dim + 1, device=worker.device)
+    while any(c < n for c, n in zip(cached, want)):
+        out, begin, start, end = worker.step(leaf, tokens, cached, max_new)
+        found += sum(a for a, c in zip(start, cached) if c < 0)
+        computed += begin[-1]
+        last = torch.tensor(begin[1:], device=worker.device) - 1
+        word = (((out[last.clamp(min=0)] > 0).flatten(1) * weigh).sum(1) % vocabulary).tolist()
+        for r in range(R):
+            cached[r] = end[r]
+            if end[r] == len(tokens[r]) and end[r] > start[r]:
+                outs[r].append(out[begin[r + 1] - 1])
+                if len(tokens[r]) < want[r]:
+                    tokens[r].append(word[r])
+    return tokens, [torch.stack(o) for o in outs], computed, found
+
+
+def make_inputs(seed=0, requests=48, chunk_tokens=64, vocabulary=1024, n=400, resident=160, suffix=90):
+    """A tree with skewed demand, its plan on one worker, and a batch's prompts."""
+    rng = np.random.default_rng(seed)
+    parent = W.random_forest(n, rng, p_root=0.02, shuffle=False)
+    depth = B.pp_prefix_table(parent)[:, 15].astype(np.int64)
+    own = rng.zipf(1.3, n).clip(max=1000).astype(np.int64)
+    demand = own.copy()
+    for v in range(n - 1, -1, -1):      # a request for a chunk needs its path
+        if parent[v] >= 0:
+            demand[parent[v]] += demand[v]
+    cost = (20_000 + 6_000 * depth).astype(np.int64)
+    plan = B.pp_plan(parent, demand[None], cost[None], np.zeros((1, 1, n), np.int64), np.array([resident], np.int32),
+                     n_starts=1)
+    words = rng.integers(0, vocabulary, (n, chunk_tokens))
+    leaf = rng.choice(n, requests, p=own / own.sum()).astype(np.int32)
+    prompts = []
+    for v in leaf:
+        path = []
+        u = int(v)
+        while u >= 0:
+            path.append(u)
+            u = int(parent[u])
+        text = [words[u] for u in reversed(path)]
+        prompts.append(np.concatenate(text + [rng.integers(0, vocabulary, rng.integers(1, suffix))]))
+    return parent, plan.target[0], words, leaf.tolist(), prompts
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--requests", type=int, default=48)
+    ap.add_argument("--decode", type=int, default=16)
+    ap.add_argument("--max-new", type=int, default=256)
+    ap.add_argument("--window", type=int, default=0)
+    ap.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
+    o = ap.parse_args()
+    cache = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[o.cache]
+    layer = Layer.random()
+    parent, target, words, leaf, prompts = make_inputs(requests=o.requests)
+    worker = Worker(layer, parent, target, words.shape[1], words, requests=o.requests,
+                    max_len=max(map(len, prompts)) + o.decode, cache=cache, window=o.window)
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    _, _, computed, found = serve(worker, leaf, prompts, o.decode, o.max_new)
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t) * 1e3
+    print(f"{o.requests} requests over {int(target.sum())} resident chunks: {found} prompt tokens found, "
+          f"{computed} tokens computed in {ms:.1f} ms")
+
+
+if __name__ == "__main__":
+    main()
