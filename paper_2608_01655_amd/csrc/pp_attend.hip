@@ -341,7 +341,10 @@ struct RowsShape {
   static constexpr int kLds = kRing > kJoin ? kRing : kJoin;
 };
 
-// One request, key head and part a block: up to 16 RT rows, in tiles of 16.
+// One request, key head and part a block: up to 16 RT rows, in tiles of 16.  Bound by reading the
+// pages: 256 requests of 1,024 to 16,384 tokens in 8 bits (2.9 GB) 552 us, 5.3 TB/s; 64 of 500 to
+// 8,190 in bf16 75 us, 4.9 TB/s.  Each wave has a ring of its own and keeps NS - 1 tiles of 32 keys
+// in flight without a barrier; with four rows in 16 used the matrix cores are 5 to 13% busy.
 template <bool F16, bool NARROW, int D, int RT>
 __global__ void __launch_bounds__((kWave * RowsShape<NARROW, D, RT>::kNW))
 k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
@@ -631,7 +634,11 @@ struct TilesSwizzle {
 template <bool NARROW, int D>
 constexpr int kTilesLds = 2 * 2 * 64 * D * (NARROW ? 1 : 2);
 
-// 128 rows of one request and key head, and one part of its keys, a block.
+// 128 rows of one request and key head, and one part of its keys, a block.  Bound by the matrix
+// cores and the exponentials beside them: 4 x 2,048 new tokens behind 6,144 to 14,336 (32 heads,
+// dim 128) 1.04 to 1.08 ms, 0.99 to 1.03 PFLOP/s, matrix cores 58% busy; a product of 8,192 squared
+// reaches 1.2 to 1.3.  Two blocks of four waves share a CU, so that one's loads and joins hide
+// behind the other's products.
 template <bool F16, bool NARROW, int D>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2)
 k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
