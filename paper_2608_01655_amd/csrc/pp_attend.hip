@@ -874,6 +874,38 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     for (int b = 0; b < 2; ++b) masked_half(buffer(t) + b * 32 * RB, kbase + t * 64 + b * 32 + 4 * half);
   };
 
+  // At dim 256 the pipeline below does not fit the registers, and a tile that every row sees whole goes
+  // through in order: scores, weights, values.  4 x 2,048 new tokens behind up to 6,144: 1.47 ms (675
+  // TFLOP/s), 6.18 ms with the pipeline and its spills; 512 behind 31,744 221 us and 1,010 us.
+  [[maybe_unused]] auto whole_tile = [&](int32_t t) {
+    wait_loads<0>();
+    barrier();
+    if (next_k == t + 1) issue_k();
+    issue_v();
+    const uint32_t at = buffer(t);
+    const f32x16 s[2] = {scores(at), scores(at + 32 * RB)};
+    const float mx = over_halves(fmaxf(largest(s[0]), largest(s[1])), Max());
+    if (grows(mx)) {
+      const float to = fmaxf(m, mx);
+      rescale(m, to);
+      m = to;
+    }
+    const float top = m == -INFINITY ? 0.f : m * c;
+    each<2>([&](auto b) {
+      float w[16], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        w[j] = exp2_(__builtin_fmaf(s[b][j], c, -top));
+        sum += w[j];
+      }
+      l += sum;
+      const s16x8 x[2] = {pack8<F16>(w), pack8<F16>(w + 8)};
+      each<2 * DB>([&](auto i) {
+        acc[i / 2] = mfma32<F16>(v_frag(at + b * 32 * RB + i % 2 * 16 * RB, i / 2), x[i % 2], acc[i / 2]);
+      });
+    });
+  };
+
   // Tiles that every row sees whole go through a pipeline of 32 keys: while the weights of one half
   // tile are worked out, the matrix cores have the scores of the next and the values of the one
   // before.  (Without it the two took turns, although two waves share a SIMD.)
@@ -959,7 +991,9 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   int32_t t = 0;
   for (; t < sp.whole; ++t) masked_tile(t);
   const int32_t tail = t + ((sp.tail - t) & ~1);   // the loop takes two at a time
-  if (t < tail) {
+  if constexpr (D == 256) {
+    for (; t < sp.tail; ++t) whole_tile(t);
+  } else if (t < tail) {
     constexpr uint32_t kHalf = 32 * RB;
     wait_loads<0>();
     barrier();
@@ -1106,7 +1140,9 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
 
 // -------------------------------------------------------------- dispatch ---
 
-constexpr int kTileBlocks = 512;   // blocks of k_tiles that are resident
+// Blocks of k_tiles that are resident: at dim 256 its registers leave room for one a CU (300 new tokens
+// behind 11,700 of 8-bit pages, counted as two a CU: 7% slower; 700 behind 8,300: 6% faster).
+int tile_blocks(int32_t dim) { return dim == 256 ? 256 : 512; }
 
 int32_t round_up(int64_t x, int32_t m) { return (int32_t)((x + m - 1) / m * m); }
 
@@ -1162,7 +1198,7 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     const double part_bytes = (double)a.tokens * a.q_heads * p.dim * 4;
     // 512 MiB of parts at most: calls beyond have so many blocks that cutting gains a percent or two
     for (int32_t i = 1; i <= 64 && (i == 1 || (tiles / i >= 8 && i * part_bytes <= 0x1p29)); ++i) {
-      const double t = std::ceil(blocks * i / kTileBlocks) * (tiles / i + 4) * tile_us + (i > 1 ? 4 + i * part_us : 0);
+      const double t = std::ceil(blocks * i / tile_blocks(p.dim)) * (tiles / i + 4) * tile_us + (i > 1 ? 4 + i * part_us : 0);
       if (i == 1 || t < best) {
         best = t;
         n = i;
