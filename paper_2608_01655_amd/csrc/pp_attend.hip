@@ -1180,7 +1180,7 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     // Lengths differ, so the fewer requests there are the smaller their parts have to be: 64 requests and 4
     // heads in 31, 16 or 8 parts took 85, 92 and 107 us; 256 requests and 8 heads in 1, 2 or 4 took 550, 556
     // and 652 us (a block that finds no keys still waits for its turn).  Below 256 keys a block's start and
-    // end are most of it.
+    // end are most of it: with 128, 64 requests take 90 us and not 84, one of 16,000 tokens 26 and not 18.
     const int64_t base = (int64_t)a.requests * p.heads;
     int64_t n = ((base < 512 ? 8192 : 4096) + base - 1) / base;
     if (n > keys / 256) n = keys / 256;
