@@ -1,8 +1,8 @@
 // pp_attend.hip -- attention of new tokens over paged keys and values (gfx950).
 //
 // out = sum_j w_j V_j / sum_j w_j, w_j = 2^(c s_j - c m), c = scale log2(e) k_scale, s = <q, K_j>,
-// in one pass over the keys with a running maximum m: where it grows by more than 8 in the exponent
-// (weights stay below 2^8), sums and accumulators are scaled down by 2^(c (m_old - m_new)).
+// in one pass over the keys with a running maximum m: where it grows by more than kLag in the exponent
+// (weights stay below 2^(kLag + kLift)), sums and accumulators are scaled down by 2^(c (m_old - m_new)).
 //
 // The query heads of a key head and the new tokens of a request are packed into rows (row =
 // token * G + head), so that a tile of keys is read once for all of them.  Both products are taken
@@ -17,8 +17,10 @@
 // share each tile of 64 keys.  Both split long requests over blocks, which leave normalised parts
 // and their log sums in the workspace for k_join.
 //
-// Weights are rounded to the queries' type for the second product (their error averages out over
-// the keys and is below that of rounding the output); scores, sums and accumulators are 32 bits.
+// Weights are rounded to the queries' type for the second product (the matrix cores take 32-bit ones
+// at a sixteenth of the rate); scores, sums and accumulators are 32 bits.  What it costs: half a unit
+// of each weight, in all about as much as rounding the output does (error against 64 bits 2.3e-3 in
+// bf16 and 2.9e-4 in f16, where rounding the output alone gives 1.7e-3 and 2.1e-4).
 // 8-bit pages are widened to the queries' type after LDS, which is exact.
 
 #include "pp_serve.h"
@@ -48,7 +50,16 @@ typedef __attribute__((__vector_size__(16))) _Float16 f16x8;
 
 constexpr int kWave = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLag = 8.f;   // growth of the maximum, in the exponent, that is let pass
+
+// Growth of the maximum, in the exponent, that is let pass, and what the weights are scaled up by for
+// the second product.  f16 has a smallest normal value of 2^-14: without the scale a key 10 below the
+// maximum is held in fewer bits and one 18 below not at all, although many such keys may be all that
+// the output is made of.  With it weights lie below 2^14 (the type ends at 2^16, which leaves room for
+// the rounding of c m), and a key is held whole down to 2^-24 of the largest, in units of 2^-34 below.
+template <bool F16>
+constexpr float kLag = F16 ? 4.f : 8.f;
+template <bool F16>
+constexpr float kLift = F16 ? 10.f : 0.f;
 
 // f(0), f(1) .. f(N - 1), the numbers as constants.
 template <int N, class F, int... I>
@@ -92,6 +103,12 @@ __device__ __forceinline__ void barrier() {
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What is taken off a score's exponent under the maximum m.
+template <bool F16>
+__device__ __forceinline__ float top_of(float m, float c) {
+  return m == -INFINITY ? 0.f : F16 ? __builtin_fmaf(m, c, -kLift<F16>) : m * c;
+}
 
 template <bool F16>
 __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
@@ -498,7 +515,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
 #pragma unroll
       for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
       mx = over_halves(over_rows(mx, Max()), Max());
-      const bool grow = mx > m[rt] && (m[rt] == -INFINITY || (mx - m[rt]) * c > kLag);
+      const bool grow = mx > m[rt] && (m[rt] == -INFINITY || (mx - m[rt]) * c > kLag<F16>);
       if (__any(grow)) {
         const float n = fmaxf(m[rt], mx);
         const float al = m[rt] == -INFINITY ? 0.f : exp2_((m[rt] - n) * c);
@@ -507,7 +524,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
         for (int d = 0; d < DB; ++d) acc[rt][d] *= al;
         m[rt] = n;
       }
-      const float mc = m[rt] == -INFINITY ? 0.f : m[rt] * c;
+      const float mc = top_of<F16>(m[rt], c);
       float sum = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -606,7 +623,7 @@ k_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
     }
     const float inv = ll == 0 ? 0.f : vs / ll;
     o *= inv;
-    const float lse = ll == 0 ? -INFINITY : mm * c + __log2f(ll);
+    const float lse = ll == 0 ? -INFINITY : mm * c + (__log2f(ll) - kLift<F16>);
     const int32_t tk = q.first + row / G, g = h * G + row % G;
     if (parts == 1) {
       store4<F16>(a, tk, g, d, o);
@@ -821,7 +838,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] *= al;
   };
-  auto grows = [&](float mx) { return __any(mx > m && (m == -INFINITY || (mx - m) * c > kLag)); };
+  auto grows = [&](float mx) { return __any(mx > m && (m == -INFINITY || (mx - m) * c > kLag<F16>)); };
 
   // Half a tile that some row does not see whole.
   auto masked_half = [&](uint32_t at, int32_t key0) {
@@ -840,7 +857,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
       rescale(m, to);
       m = to;
     }
-    const float mc = m == -INFINITY ? 0.f : m * c;
+    const float mc = top_of<F16>(m, c);
     float w[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -891,7 +908,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
       rescale(m, to);
       m = to;
     }
-    const float top = m == -INFINITY ? 0.f : m * c;
+    const float top = top_of<F16>(m, c);
     each<2>([&](auto b) {
       float w[16], sum = 0;
 #pragma unroll
@@ -921,7 +938,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
     grow = grows(mx);
     old = m;
     m = grow ? fmaxf(m, mx) : m;
-    mc = m == -INFINITY ? 0.f : m * c;
+    mc = top_of<F16>(m, c);
   };
   constexpr int kAhead = 3;       // fragments read ahead of their use
   s16x8 pre[kAhead];              // the first ones of the next step, where no barrier comes before it
@@ -1040,7 +1057,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   if (!live) return;
   const float vs = NARROW && p.v_scale ? p.v_scale[h] : 1.f;
   const float inv = l == 0 ? 0.f : vs / l;
-  const float lse = l == 0 ? -INFINITY : m * c + __log2f(l);
+  const float lse = l == 0 ? -INFINITY : m * c + (__log2f(l) - kLift<F16>);
   const int32_t tk = q.first + tok;
   const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
   auto each4 = [&](auto put) {

@@ -1,0 +1,69 @@
+"""Edges of the paged attention: what the ordinary cases do not reach."""
+
+import math
+
+import pytest
+import torch
+
+from tests import serve_ref as S
+from tests.test_gpu_serve import BF, E4, HF, attend, attend_case, close
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _say_case(request):
+    print(f"\n[case] {request.node.name}", flush=True)
+    yield
+
+
+def put(c, name, r, at, x):
+    """Sets tokens `at` of request r in the pages of c[name] to x (a value or rows [tokens][heads][dim])."""
+    page = c[name].shape[2]
+    at = torch.as_tensor(at, device="cuda")
+    c[name][c["table"][r].long()[at // page], :, at % page] = x
+
+
+@pytest.mark.parametrize("gap", [14.0, 16.0, 18.0, 20.0])
+@pytest.mark.parametrize("new", [1, 5, 100])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype,cache", [(HF, HF), (HF, E4), (BF, BF)])
+def test_small_weights_beside_large_ones(dtype, cache, dim, new, gap):
+    """Every 32nd key takes nearly all the weight and has V = 0, so that the output is what the others
+    add, `gap` below in the exponent: their weights keep the type's precision.
+
+    Tolerance: serve_ref's, but for f16 with weights held in units of 2^-10 of the largest (or smaller
+    ones): a weight below the normal range is off by 2^-25 of that unit, 2^-35 |v| a key, over a sum of
+    at least 1; the output's own subnormal rounding is 2^-25."""
+    n, heads, kv_heads = 1100, 8, 2
+    c = attend_case(3, [new], [n], heads, kv_heads, dim, dtype, cache, scale=1.0)
+    c["ks"] = c["vs"] = None
+    g = torch.Generator(device="cuda").manual_seed(int(gap))
+    c["q"][...] = 0
+    c["q"][..., 0] = 1
+    sink = torch.arange(0, n, 32)
+    v = (128 + 128 * torch.rand((n, kv_heads, dim), generator=g, device="cuda")).to(dtype).to(cache)
+    put(c, "k", 0, range(n), torch.zeros((), device="cuda").to(cache))
+    put(c, "v", 0, range(n), v)
+    gap_key = torch.zeros(dim, device="cuda")
+    gap_key[0] = gap
+    put(c, "k", 0, sink, gap_key.to(cache))
+    put(c, "v", 0, sink, torch.zeros((), device="cuda").to(cache))
+    out, lse = attend(c)
+    torch.cuda.synchronize()
+    v = v.double().cpu()
+    v[sink] = 0
+    v = v.repeat_interleave(heads // kv_heads, 1)
+    w = torch.full((n,), math.exp(-gap), dtype=torch.float64)
+    w[sink] = 1
+    u = S.UNIT[dtype]
+    for i in range(new):
+        e = n - new + i + 1
+        total = w[:e].sum()
+        o = torch.einsum("j,jhd->hd", w[:e], v[:e]) / total
+        tol = 2 * u * o + ((dim + 8) * 2.0 ** -24 * gap * 2 + (e + 64) * 2.0 ** -23) * o
+        if dtype == HF:
+            tol += 2.0 ** -35 * v[:e].sum(0) + 2.0 ** -25
+        close(out[i], o, tol)
+        want = torch.full((heads,), float(gap + total.log()), dtype=torch.float64)
+        close(lse[i], want, torch.full_like(want, (dim + 8) * 2.0 ** -24 * gap + (e + 64) * 2.0 ** -23 + 2.0 ** -22 * float(want[0])))
