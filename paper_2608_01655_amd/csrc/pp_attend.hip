@@ -1056,7 +1056,7 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   l = over_halves(l, Sum());
   if (!live) return;
   const float vs = NARROW && p.v_scale ? p.v_scale[h] : 1.f;
-  const float inv = l == 0 ? 0.f : vs / l;
+  const float inv = vs / l;
   const float lse = l == 0 ? -INFINITY : m * c + (__log2f(l) - kLift<F16>);
   const int32_t tk = q.first + tok;
   const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + g;
@@ -1066,7 +1066,8 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         f32x4 o = {acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]};
-        put(db * 32 + b * 8 + half * 4, o * inv);   // all 0 where l is
+        // where l is 0 the products may still hold 0 times an infinity
+        put(db * 32 + b * 8 + half * 4, l == 0 ? f32x4{0, 0, 0, 0} : o * inv);
       }
   };
   if (parts == 1) each4([&](int d, f32x4 o) { store4<F16>(a, tk, g, d, o); });

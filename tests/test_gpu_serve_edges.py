@@ -67,3 +67,23 @@ def test_small_weights_beside_large_ones(dtype, cache, dim, new, gap):
         close(out[i], o, tol)
         want = torch.full((heads,), float(gap + total.log()), dtype=torch.float64)
         close(lse[i], want, torch.full_like(want, (dim + 8) * 2.0 ** -24 * gap + (e + 64) * 2.0 ** -23 + 2.0 ** -22 * float(want[0])))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,n", [(1, 40), (5, 90), (100, 100), (100, 400), (100, 9000)])
+def test_rows_of_minus_infinity_whatever_the_values(new, n, dim, dtype):
+    """A row whose seen keys all score -infinity is empty, also where their values are infinite or NaN."""
+    c = attend_case(4, [new], [n], 8, 2, dim, dtype, dtype)
+    c["q"].abs_().add_(0.01)
+    dead = new - new // 4                                 # new tokens that see nothing else
+    last = n - new + dead                                 # the first key that scores
+    k = torch.zeros(dim, device="cuda", dtype=dtype)
+    k[0] = -math.inf
+    put(c, "k", 0, range(last), k)
+    for at, x in ((0, math.inf), (last // 2, math.nan), (max(last - 2, 0), -math.inf), (last - 1, math.inf)):
+        put(c, "v", 0, [at], x)
+    out, lse = attend(c)
+    torch.cuda.synchronize()
+    assert bool((out[:dead] == 0).all()) and bool((lse[:dead] == -math.inf).all())
+    assert bool(torch.isfinite(lse[dead:]).all())
