@@ -1163,7 +1163,7 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
 // behind 11,700 of 8-bit pages, counted as two a CU: 7% slower; 700 behind 8,300: 6% faster).
 int tile_blocks(int32_t dim) { return dim == 256 ? 256 : 512; }
 
-int32_t round_up(int64_t x, int32_t m) { return (int32_t)((x + m - 1) / m * m); }
+int64_t round_up(int64_t x, int32_t m) { return (x + m - 1) / m * m; }
 
 struct Choice {
   int rt;                       // tiles of 16 rows in k_rows, 0 = not launched
@@ -1186,15 +1186,20 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
     if (pl.group <= most && (int64_t)a.requests * a.max_new != a.tokens) ch.rt = tiles16(pl.group);
   }
   pl.few = ch.rt * 16;
-  // keys that a request's rows see, at most
-  int64_t keys = a.max_len > 1 ? a.max_len : 1;
+  // keys that a request's rows see, at most; tokens past a row of the block table do not exist
+  int64_t keys = (int64_t)a.max_blocks * p.page_size;
+  if (a.max_len < keys) keys = a.max_len;
+  if (keys < 1) keys = 1;
   if (a.window && (int64_t)a.window + a.max_new + 64 < keys) keys = (int64_t)a.window + a.max_new + 64;
-  pl.parts_rows = pl.parts_tiles = 1;
-  pl.cut_rows = pl.cut_tiles = round_up(keys, 128);
+  // n parts at most; the last one is open, so a size held to 31 bits loses no key
   auto cut = [&](int32_t n, int32_t unit, int32_t& size, int32_t& parts) {
-    size = round_up((keys + n - 1) / n, unit);
-    parts = (int32_t)((keys + size - 1) / size);
+    const int64_t x = round_up((keys + n - 1) / n, unit), most = INT32_MAX / 128 * 128;
+    size = (int32_t)(x < most ? x : most);
+    const int64_t count = (keys + size - 1) / size;
+    parts = (int32_t)(count < n ? count : n);
   };
+  cut(1, 128, pl.cut_rows, pl.parts_rows);
+  cut(1, 128, pl.cut_tiles, pl.parts_tiles);
   if (ch.rt) {
     // Lengths differ, so the fewer requests there are the smaller their parts have to be: 64 requests and 4
     // heads in 31, 16 or 8 parts took 85, 92 and 107 us; 256 requests and 8 heads in 1, 2 or 4 took 550, 556

@@ -87,3 +87,22 @@ def test_rows_of_minus_infinity_whatever_the_values(new, n, dim, dtype):
     torch.cuda.synchronize()
     assert bool((out[:dead] == 0).all()) and bool((lse[:dead] == -math.inf).all())
     assert bool(torch.isfinite(lse[dead:]).all())
+
+
+@pytest.mark.parametrize("requests,new,heads,kv_heads", [(512, 1, 8, 8), (64, 128, 64, 8), (80, 3, 16, 2)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_no_bound_at_all(requests, new, heads, kv_heads, wide):
+    """max_len as large as its type, behind block tables of a few pages and of as many as there may be:
+    the same as with a bound that fits, but for the rounding where the latter takes parts."""
+    c = attend_case(6, [new] * requests, [new + r % 7 for r in range(requests)], heads, kv_heads, 128, BF, BF)
+    out, lse = attend(c)
+    want, want_lse = out.double().cpu(), lse.double().cpu()
+    if wide:                                              # rows may overlap where they are only read
+        blocks, row = (1 << 27) - 1, c["table"].shape[1]
+        table = torch.zeros(blocks + requests * row, dtype=torch.int32, device="cuda")
+        table[:requests * row] = c["table"].flatten()
+        c["table"] = table.as_strided((requests, blocks), (row, 1))
+    out, lse = attend(c, max_len=2 ** 31 - 1)
+    torch.cuda.synchronize()
+    close(out, want, 2 ** -7 * want.abs() + 2 ** -12)
+    close(lse, want_lse, 2 ** -18 * want_lse.abs() + 2 ** -18)
