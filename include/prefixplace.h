@@ -540,8 +540,11 @@ typedef struct {
 } pp_kv_pages;
 
 /* Writes rows k, v [tokens][heads][dim] (PP_BF16 or PP_F16) into the places
- * slot_map names; a place below 0 or past the pages is skipped, and one named
- * twice gets either row.  Pages of the rows' own type take them as they are;
+ * slot_map names; a place below 0 or past the pages is skipped.  No place is
+ * to be named twice: it ends up with elements of either row, mixed, and its
+ * key need not be of the row that its value is of.  (pp_block_tables names
+ * none twice as long as no page is handed out twice.)
+ * Pages of the rows' own type take them as they are;
  * PP_E4M3 pages take row / scale rounded to nearest even, values past +-448
  * (infinities too) as +-448, NaN as NaN.  Strides in elements. */
 int pp_kv_write(const pp_kv_pages *pages, int32_t tokens, int32_t dtype,

@@ -678,8 +678,8 @@ def _pages(torch, k_cache, v_cache, k_scale, v_scale, device):
 
 def pp_kv_write(k, v, slot_map, k_cache, v_cache, *, k_scale=None, v_scale=None, stream=None):
     """New rows k, v [tokens][heads][dim] into the places slot_map (int64
-    [tokens]) names, on torch device tensors (see include/prefixplace.h).
-    Pages are [pages][heads][page_size][dim] views in any memory order, of
+    [tokens], no place twice) names, on torch device tensors (see
+    include/prefixplace.h).  Pages are [pages][heads][page_size][dim] views in any memory order, of
     the rows' type or float8_e4m3fn."""
     torch = _torch or _with_torch()
     device, st = _stream_of(torch, k, stream)

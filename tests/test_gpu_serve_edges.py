@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+from paper_2608_01655_amd import binding as B
 from tests import serve_ref as S
 from tests.test_gpu_serve import BF, E4, HF, attend, attend_case, close
 
@@ -106,3 +107,19 @@ def test_no_bound_at_all(requests, new, heads, kv_heads, wide):
     torch.cuda.synchronize()
     close(out, want, 2 ** -7 * want.abs() + 2 ** -12)
     close(lse, want_lse, 2 ** -18 * want_lse.abs() + 2 ** -18)
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF, BF), (HF, E4)])
+def test_write_to_a_place_named_twice(dtype, cache):
+    """Such a place holds elements of either row, in any mix; the others are whole."""
+    T, heads, dim, page = 40, 4, 128, 16
+    rows = torch.randn((2, T, heads, dim), device="cuda", dtype=dtype).clamp(-400, 400)
+    pages = torch.zeros((2, 3, heads, page, dim), device="cuda", dtype=cache)
+    place = torch.arange(T, device="cuda")
+    place[::2] = 0
+    B.pp_kv_write(rows[0], rows[1], place, pages[0], pages[1])
+    got = pages.permute(0, 1, 3, 2, 4).reshape(2, -1, heads, dim)[:, :T].float()
+    want = rows.to(cache).float()
+    assert torch.equal(got[:, 1::2], want[:, 1::2])
+    assert bool((got[:, :1] == want[:, ::2]).any(1).all())
+    assert bool((got[:, 2::2] == 0).all())
