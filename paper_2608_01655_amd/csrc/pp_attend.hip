@@ -1247,14 +1247,18 @@ PartRows part_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan&
 }
 
 template <class K>
-hipError_t allow_lds(K kern, int bytes) {
-  return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+hipError_t allow_lds(OnEachGpu& once, K kern, int bytes) {
+  int gpu;
+  const hipError_t e = hipGetDevice(&gpu);
+  if (e != hipSuccess) return e;
+  return once(gpu, [&] { return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
 template <bool F16, bool NARROW, int D, int RT>
 hipError_t go_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, hipStream_t st) {
   constexpr int lds = RowsShape<NARROW, D, RT>::kLds;
-  static const hipError_t ok = allow_lds(&k_rows<F16, NARROW, D, RT>, lds);
+  static OnEachGpu once;
+  const hipError_t ok = allow_lds(once, &k_rows<F16, NARROW, D, RT>, lds);
   if (ok != hipSuccess) return ok;
   const int64_t grid = (int64_t)a.requests * pl.parts_rows * p.heads;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
@@ -1266,7 +1270,8 @@ template <bool F16, bool NARROW, int D>
 hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, const Choice& ch, hipStream_t st) {
   if (ch.tiles) {
     constexpr int lds = kTilesLds<NARROW, D>;
-    static const hipError_t ok = allow_lds(&k_tiles<F16, NARROW, D>, lds);
+    static OnEachGpu once;
+    const hipError_t ok = allow_lds(once, &k_tiles<F16, NARROW, D>, lds);
     if (ok != hipSuccess) return ok;
     const int64_t grid = (int64_t)pl.slots * pl.parts_tiles * p.heads;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;

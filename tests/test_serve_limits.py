@@ -1,10 +1,13 @@
 """Bounds and sizes at their ends: what the prefix cache's host side makes of them (no GPU needed)."""
 
 import ctypes
+import os
+import subprocess
 
 import pytest
 
 from paper_2608_01655_amd import binding as B
+from paper_2608_01655_amd import build
 from tests.test_serve_host import L, _attention, _kv_pages  # noqa: F401
 
 
@@ -21,3 +24,43 @@ def test_keys_end_with_the_rows_of_the_block_table(L, requests, tokens, max_new,
     for max_len in (blocks * 16 + 1, 1 << 20, (1 << 31) - 128, (1 << 31) - 1):
         if max_len > blocks * 16:
             assert workspace(L, max_len=max_len, **kw) == want >= 0
+
+
+ON_EACH_GPU = r"""
+#include "pp_serve.h"
+#include <cstdio>
+
+int main() {
+  pp::OnEachGpu once;
+  int calls = 0;
+  hipError_t answer = hipErrorUnknown;
+  auto at = [&](int gpu) {
+    return once(gpu, [&] {
+      ++calls;
+      return answer;
+    });
+  };
+  if (at(0) != hipErrorUnknown || at(0) != hipErrorUnknown || calls != 2) return 1;   // a failure is not kept
+  answer = hipSuccess;
+  if (at(0) != hipSuccess || at(0) != hipSuccess || calls != 3) return 2;             // once where it succeeds
+  if (at(1) != hipSuccess || calls != 4 || at(63) != hipSuccess || calls != 5) return 3;   // on each GPU
+  answer = hipErrorUnknown;
+  if (at(0) != hipSuccess || at(1) != hipSuccess || at(63) != hipSuccess || calls != 5) return 4;
+  if (at(2) != hipErrorUnknown || at(64) != hipErrorUnknown || calls != 7) return 5;
+  answer = hipSuccess;
+  if (at(64) != hipSuccess || at(64) != hipSuccess || calls != 9) return 6;
+  return 0;
+}
+"""
+
+
+def test_what_is_set_up_on_each_gpu(tmp_path):
+    """A kernel's LDS size is set on every GPU that it is launched on, and a failure is tried again."""
+    src, exe = tmp_path / "once.cpp", tmp_path / "once"
+    src.write_text(ON_EACH_GPU)
+    include = os.path.join(os.path.dirname(os.path.dirname(build.hipcc())), "include")
+    if not os.path.isdir(os.path.join(include, "hip")):
+        include = "/opt/rocm/include"
+    subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", include, "-I", build.INCLUDE, "-I", build.CSRC,
+                    str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0
