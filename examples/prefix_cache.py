@@ -1,13 +1,14 @@
 """One worker's prefix cache from plan to attention, on one attention layer with random weights.
 
-    python examples/prefix_cache.py [--requests 48] [--window 0] [--cache e4m3]
+    python examples/prefix_cache.py [--requests 48] [--window 0] [--cache e4m3] [--replan 4]
 
 A plan says which chunks of the prefix tree stay on the worker (pp_plan), they get slots
 (pp_cache_slots) and their keys and values are written once (pp_kv_write).  Then requests come:
 every step finds the prefixes of the new ones, hands out pages and places the new tokens
 (pp_block_tables), writes their keys and values (pp_kv_write) and computes their attention
 (pp_paged_attention), prompts in pieces of `max_new` tokens beside the single tokens of requests
-that are past their prompt.
+that are past their prompt.  A later plan moves chunks in and out; those that running requests found
+keep their slots until they are through.
 """
 
 from __future__ import annotations
@@ -55,17 +56,17 @@ class Worker:
     """Pages, slots and running requests of one worker."""
 
     def __init__(self, layer, parent, target, chunk_tokens, words, *, requests, max_len, page_size=16, pages=None,
-                 cache=torch.bfloat16, window=0):
-        """parent [n] and words [n][chunk_tokens]: the tree and its chunks' tokens; target [n]: what stays here."""
+                 cache=torch.bfloat16, window=0, spare=0):
+        """parent [n] and words [n][chunk_tokens]: the tree and its chunks' tokens; target [n]: what stays here;
+        spare: slots beyond the target's, for what running requests hold when the plan changes."""
         self.layer, self.page, self.chunk, self.window, self.requests = layer, page_size, chunk_tokens, window, requests
-        n_slots = int(target.sum())
-        slot, _ = B.pp_cache_slots(target, n_slots)
-        self.n_slots, resident = n_slots, n_slots * (chunk_tokens // page_size)
+        self.parent, self.words = parent, words
+        self.n_slots = int(target.sum()) + spare
+        resident = self.n_slots * (chunk_tokens // page_size)
         self.blocks = -(-max_len // page_size)
         pages = resident + requests * self.blocks if pages is None else pages
         d = self.device = torch.device("cuda")
         self.lines = torch.from_numpy(B.pp_prefix_table(parent)).to(d)
-        self.slot = torch.from_numpy(slot).to(d)
         pool = torch.zeros((2, pages, layer.kv_heads, page_size, layer.dim), dtype=cache, device=d)
         self.k_cache, self.v_cache = pool[0], pool[1]
         self.scale = dict.fromkeys(("k_scale", "v_scale"))
@@ -74,14 +75,30 @@ class Worker:
         self.free = list(range(resident, pages))
         self.table = torch.full((requests, self.blocks), -1, dtype=torch.int32, device=d)
         self.max_len = max_len
-        # the resident chunks' keys and values, written once
-        node = torch.nonzero(self.slot >= 0).flatten()
-        if node.numel():
-            i = torch.arange(chunk_tokens, device=d)
-            position = (self.lines[node, 15:].long() * chunk_tokens + i).flatten()
-            _, k, v = layer.project(torch.as_tensor(words, device=d)[node].flatten(), position)
-            place = (self.slot[node].long()[:, None] * chunk_tokens + i).flatten()
+        self.held = np.full(len(parent), -1, np.int32)
+        self.place_chunks(target)
+
+    def place_chunks(self, target, running=()):
+        """Slots for a plan's target; `running`: (leaf, prefix tokens found) of the requests that go on.  The keys
+        and values of chunks that are new here are written once."""
+        keep = np.array(target, np.uint8)
+        for node, found in running:
+            path = []
+            while node >= 0:
+                path.append(node)
+                node = int(self.parent[node])
+            keep[path[len(path) - found // self.chunk:]] = 1    # root side of the path
+        slot, _ = B.pp_cache_slots(keep, self.n_slots, held=self.held)
+        new, self.held = np.flatnonzero((slot >= 0) & (self.held < 0)), slot
+        d = self.device
+        if new.size:
+            i = torch.arange(self.chunk, device=d)
+            node = torch.from_numpy(new).to(d)
+            position = (self.lines[node, 15:].long() * self.chunk + i).flatten()
+            _, k, v = self.layer.project(torch.as_tensor(self.words[new], device=d).flatten(), position)
+            place = (torch.from_numpy(slot[new]).to(d).long()[:, None] * self.chunk + i).flatten()
             B.pp_kv_write(k, v, place, self.k_cache, self.v_cache, **self.scale)
+        self.slot = torch.from_numpy(slot).to(d)
 
     def step(self, leaf, tokens, cached, max_new):
         """One batch step.  leaf [R]; tokens [R]: every request's tokens so far, as lists; cached [R]: how many
@@ -114,18 +131,23 @@ class Worker:
         return out, query_start.tolist(), starts, ends
 
 
-def serve(worker, leaf, prompts, decode, max_new, vocabulary=1024):
+def serve(worker, leaf, prompts, decode, max_new, vocabulary=1024, plans=None):
     """Serves all requests at once to `decode` tokens behind their prompts; the next token is read off a hash of
     the attention's output's sign bits, which stands in for the rest of a model.  Returns (tokens, the last
-    prompt token's and each decoded token's outputs, tokens computed, tokens found)."""
+    prompt token's and each decoded token's outputs, tokens computed, tokens found).  plans: {step: target}, plans
+    that come while the requests run."""
     R = len(leaf)
     tokens = [list(map(int, p)) for p in prompts]
-    cached, want = [-1] * R, [len(p) + decode for p in prompts]
+    cached, want, behind = [-1] * R, [len(p) + decode for p in prompts], [0] * R
     outs = [[] for _ in range(R)]
-    computed = found = 0
+    computed = found = steps = 0
     weigh = torch.arange(1, worker.layer.heads * worker.layer.dim + 1, device=worker.device)
     while any(c < n for c, n in zip(cached, want)):
+        if plans and steps in plans:
+            worker.place_chunks(plans[steps], [(v, b) for v, b, c, n in zip(leaf, behind, cached, want) if c < n])
+        steps += 1
         out, begin, start, end = worker.step(leaf, tokens, cached, max_new)
+        behind = [a if c < 0 else b for a, b, c in zip(start, behind, cached)]
         found += sum(a for a, c in zip(start, cached) if c < 0)
         computed += begin[-1]
         last = torch.tensor(begin[1:], device=worker.device) - 1
@@ -139,19 +161,24 @@ def serve(worker, leaf, prompts, decode, max_new, vocabulary=1024):
     return tokens, [torch.stack(o) for o in outs], computed, found
 
 
-def make_inputs(seed=0, requests=48, chunk_tokens=64, vocabulary=1024, n=400, resident=160, suffix=90):
-    """A tree with skewed demand, its plan on one worker, and a batch's prompts."""
-    rng = np.random.default_rng(seed)
-    parent = W.random_forest(n, rng, p_root=0.02, shuffle=False)
+def plan_one(parent, own, resident):
+    """What one worker keeps for requests that end at chunk v with frequency own[v]: [n] uint8."""
+    n = len(parent)
     depth = B.pp_prefix_table(parent)[:, 15].astype(np.int64)
-    own = rng.zipf(1.3, n).clip(max=1000).astype(np.int64)
     demand = own.copy()
     for v in range(n - 1, -1, -1):      # a request for a chunk needs its path
         if parent[v] >= 0:
             demand[parent[v]] += demand[v]
     cost = (20_000 + 6_000 * depth).astype(np.int64)
-    plan = B.pp_plan(parent, demand[None], cost[None], np.zeros((1, 1, n), np.int64), np.array([resident], np.int32),
-                     n_starts=1)
+    return B.pp_plan(parent, demand[None], cost[None], np.zeros((1, 1, n), np.int64), np.array([resident], np.int32),
+                     n_starts=1).target[0]
+
+
+def make_inputs(seed=0, requests=48, chunk_tokens=64, vocabulary=1024, n=400, resident=160, suffix=90):
+    """A tree with skewed demand, its plan on one worker, and a batch's prompts."""
+    rng = np.random.default_rng(seed)
+    parent = W.random_forest(n, rng, p_root=0.02, shuffle=False)
+    own = rng.zipf(1.3, n).clip(max=1000).astype(np.int64)
     words = rng.integers(0, vocabulary, (n, chunk_tokens))
     leaf = rng.choice(n, requests, p=own / own.sum()).astype(np.int32)
     prompts = []
@@ -163,7 +190,7 @@ def make_inputs(seed=0, requests=48, chunk_tokens=64, vocabulary=1024, n=400, re
             u = int(parent[u])
         text = [words[u] for u in reversed(path)]
         prompts.append(np.concatenate(text + [rng.integers(0, vocabulary, rng.integers(1, suffix))]))
-    return parent, plan.target[0], words, leaf.tolist(), prompts
+    return parent, plan_one(parent, own, resident), words, leaf.tolist(), prompts
 
 
 def main():
@@ -172,16 +199,22 @@ def main():
     ap.add_argument("--decode", type=int, default=16)
     ap.add_argument("--max-new", type=int, default=256)
     ap.add_argument("--window", type=int, default=0)
+    ap.add_argument("--replan", type=int, default=0, help="step before which a plan for other demand comes (0: none)")
     ap.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
     o = ap.parse_args()
     cache = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[o.cache]
     layer = Layer.random()
     parent, target, words, leaf, prompts = make_inputs(requests=o.requests)
+    plans = None
+    if o.replan:
+        later = np.random.default_rng(1).zipf(1.3, len(parent)).clip(max=1000).astype(np.int64)
+        plans = {o.replan: plan_one(parent, later, int(target.sum()))}
     worker = Worker(layer, parent, target, words.shape[1], words, requests=o.requests,
-                    max_len=max(map(len, prompts)) + o.decode, cache=cache, window=o.window)
+                    max_len=max(map(len, prompts)) + o.decode, cache=cache, window=o.window,
+                    spare=int(target.sum()) if plans else 0)
     torch.cuda.synchronize()
     t = time.perf_counter()
-    _, _, computed, found = serve(worker, leaf, prompts, o.decode, o.max_new)
+    _, _, computed, found = serve(worker, leaf, prompts, o.decode, o.max_new, plans=plans)
     torch.cuda.synchronize()
     ms = (time.perf_counter() - t) * 1e3
     print(f"{o.requests} requests over {int(target.sum())} resident chunks: {found} prompt tokens found, "

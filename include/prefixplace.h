@@ -470,7 +470,13 @@ int pp_prefix_table(int32_t n, const int32_t *parent, int32_t *table);
  * is held and still targeted keeps its slot; the others of the target take
  * the free slots in increasing order, chunks in increasing id; every other
  * chunk gets -1.  slot [n] out (may be `held` itself); n_new out, may be
- * NULL: chunks without a slot so far, whose pages have to be filled.
+ * NULL: chunks without a slot so far, whose pages have to be filled before
+ * pp_block_tables is given the slots.
+ * A slot is free as soon as its chunk is not in the target, and may go to
+ * another chunk in the same call.  Rows of requests that go on still name its
+ * pages, so a chunk that such a request found has to stay in the target given
+ * here, whatever the plan says, until the request has ended; the worker needs
+ * that many slots beyond the plan's.
  * PP_E_RANGE if the target has more than n_slots chunks, or held names a
  * slot out of range or twice. */
 int pp_cache_slots(int32_t n, const uint8_t *target, const int32_t *held,

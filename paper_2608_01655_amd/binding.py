@@ -544,7 +544,8 @@ def pp_prefix_table(parent):
 
 def pp_cache_slots(target, n_slots, held=None):
     """Slots for a worker's target row: (int32 [n], chunks new to the cache)
-    (host only; see include/prefixplace.h)."""
+    (host only; see include/prefixplace.h).  Chunks that running requests
+    found have to be in the target too: the slots of others are given away."""
     target = _c(target, np.uint8)
     held = None if held is None else _c(held, np.int32)
     n = target.shape[0]
