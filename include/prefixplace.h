@@ -516,7 +516,7 @@ typedef struct {
     int32_t page_size;         /* a power of two, 16 .. 1,024 */
     int32_t chunk_tokens;      /* a multiple of page_size */
     int32_t max_new;
-    int64_t row_stride;        /* entries from a row of block_table to the next */
+    int64_t row_stride;        /* entries from a row of block_table to the next, max_blocks at least */
     const int32_t *leaf, *length, *cached;      /* [requests] */
     const int32_t *prefix_table;                /* [n][16], 16-byte aligned */
     const int32_t *slot;                        /* [n] */

@@ -173,6 +173,8 @@ int pp_block_tables(const pp_block_args* a, void* hip_stream) {
       (a->max_tokens && (!a->slot_map || !a->position)))
     return report(PP_E_ARG, "null pointer");
   if (!aligned16(a->prefix_table)) return report(PP_E_ARG, "prefix_table is 16-byte aligned");
+  if (a->requests > 1 && a->row_stride < a->max_blocks)
+    return report(PP_E_ARG, "rows of block_table overlap");   // they are written
   return launched(launch_block_tables(*a, (hipStream_t)hip_stream));
 }
 

@@ -8,7 +8,7 @@ import pytest
 
 from paper_2608_01655_amd import binding as B
 from paper_2608_01655_amd import build
-from tests.test_serve_host import L, _attention, _kv_pages  # noqa: F401
+from tests.test_serve_host import L, _attention, _block_args, _kv_pages  # noqa: F401
 
 
 def workspace(L, **kw):
@@ -64,3 +64,10 @@ def test_what_is_set_up_on_each_gpu(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", include, "-I", build.INCLUDE, "-I", build.CSRC,
                     str(src), "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+def test_block_tables_refuse_rows_that_overlap(L):
+    """Rows of an expanded tensor, or closer than they are long, would be written over one another."""
+    for kw in (dict(row_stride=0), dict(row_stride=7), dict(requests=65536, row_stride=7)):
+        assert L.pp_block_tables(ctypes.byref(_block_args(**kw)), None) == B.PP_E_ARG
+        assert "overlap" in B.pp_last_error()
