@@ -123,3 +123,100 @@ def test_write_to_a_place_named_twice(dtype, cache):
     assert torch.equal(got[:, 1::2], want[:, 1::2])
     assert bool((got[:, :1] == want[:, ::2]).any(1).all())
     assert bool((got[:, 2::2] == 0).all())
+
+
+def test_a_workspace_that_does_not_do():
+    c = attend_case(10, [1], [30_000], 16, 2, 128, BF, BF)
+    need = B.pp_attention_workspace(c["q"], c["k"], c["table"], max_new=1, max_len=30_000)
+    assert need > 64
+    kept = torch.zeros(need + 256, dtype=torch.uint8, device="cuda")
+    for bad in (kept[:64], kept[:need - 1], kept[16:need + 16]):
+        with pytest.raises(B.PPError) as e:
+            attend(c, workspace=bad)
+        assert e.value.code == B.PP_E_ARG
+    want = [x.clone() for x in attend(c)]
+    got = attend(c, workspace=kept[:need])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("R", [3, 100])
+def test_tables_without_a_tree(R):
+    """No chunk at all: nothing is found, whatever the requests ask for."""
+    e = torch.empty(0, dtype=torch.int32, device="cuda")
+    leaf = torch.arange(R, dtype=torch.int32, device="cuda") - 1
+    length = torch.arange(R, dtype=torch.int32, device="cuda") * 3
+    T = int(length.sum())
+    i32 = lambda *s: torch.full(s, -7, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, begin, start, end, position, taken = i32(R, 20), i32(R + 1), i32(R), i32(R), i32(T), i32(1)
+    slot_map = torch.empty(T, dtype=torch.int64, device="cuda")
+    free = torch.arange(100, 100 + 20 * R, dtype=torch.int32, device="cuda")
+    B.pp_block_tables(leaf, length, torch.full_like(leaf, -1), e.view(0, 16), e, free, table, begin, start, end, slot_map,
+                      position, taken, page_size=16, chunk_tokens=32, n_slots=0)
+    assert bool((start == 0).all()) and torch.equal(end, length) and begin[1:].tolist() == length.cumsum(0).tolist()
+    need = -(-length // 16)
+    assert int(taken) == int(need.sum())
+    for r in range(R):
+        first = 100 + int(need[:r].sum())
+        n, a, b = int(need[r]), int(begin[r]), int(begin[r + 1])
+        assert table[r].tolist() == list(range(first, first + n)) + [-7] * (20 - n)
+        assert slot_map[a:b].tolist() == list(range(first * 16, first * 16 + b - a))
+        assert position[a:b].tolist() == list(range(b - a))
+
+
+def check_requests(c, which, window=0):
+    """Requests `which` of the call against the 64-bit implementation, one at a time."""
+    out, lse = attend(c, window)
+    torch.cuda.synchronize()
+    k, v, begin = c["k"].cpu(), c["v"].cpu(), c["begin"].tolist()
+    for r in which:
+        rows = slice(begin[r], begin[r + 1])
+        sub = torch.tensor([0, begin[r + 1] - begin[r]], dtype=torch.int32)
+        want, want_lse, tol, tol_lse = S.attend(c["q"][rows], k, v, c["table"][r:r + 1], sub, c["length"][r:r + 1],
+                                                scale=c["scale"], window=window, k_scale=c["ks"], v_scale=c["vs"])
+        close(out[rows], want, tol)
+        close(lse[rows], want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("window", [0, 4500])
+@pytest.mark.parametrize("dim,dtype,cache", [(64, HF, E4), (64, BF, BF), (128, BF, BF), (128, BF, E4), (256, HF, HF), (256, BF, E4)])
+@pytest.mark.parametrize("new,heads", [(1, 8), (4, 32), (3, 64), (8, 64)])
+def test_long_requests_in_one_part(new, heads, dim, dtype, cache, window):
+    """Many requests, so that the long ones among them are not cut and a wave goes through more than 32 tiles:
+    its page numbers are read again, its ring comes round."""
+    if dim == 256 and new == 8:
+        new = 4                                           # 32 rows are its most
+    length = [new + r % 9 for r in range(512)]
+    long = {5: 9000, 100: 4097, 250: 4096 * 2 + 1, 511: 6111}
+    for r, n in long.items():
+        length[r] = n
+    c = attend_case(new + dim, [new] * 512, length, heads, 8, dim, dtype, cache)
+    assert B.pp_attention_workspace(c["q"], c["k"], c["table"], max_new=new, max_len=9000, window=window) == 0
+    check_requests(c, [*long, 0, 8, 400], window)
+
+
+@pytest.mark.parametrize("window", [0, 4500])
+@pytest.mark.parametrize("dim,dtype,cache", [(64, HF, HF), (64, BF, E4), (128, BF, BF), (128, HF, E4), (256, BF, BF), (256, HF, E4)])
+def test_long_prompts_in_one_part(dim, dtype, cache, window):
+    """As many new tokens as leave no room for parts, so that a block goes through more than 64 tiles of keys."""
+    filler = 8
+    each = 2 ** 29 // (2 * 64 * dim * 4) // filler
+    long = [64 * 64 - 1, 64 * 64 + 1, 64 * 130, 12_007]
+    new, length = [37, 40, 9, 70] + [each] * filler, long + [each] * filler
+    c = attend_case(dim, new, length, 64, 8, dim, dtype, cache)
+    # two parts of the prompts' rows would take 2^29 bytes; what there is, is of single tokens, had there been any
+    assert B.pp_attention_workspace(c["q"], c["k"], c["table"], max_new=each, max_len=12_007, window=window) < 2 ** 29
+    check_requests(c, range(4), window)
+
+
+@pytest.mark.parametrize("R", [65, 200])
+@pytest.mark.parametrize("single", [False, True])
+@pytest.mark.parametrize("dim,dtype,cache,top", [(128, BF, BF, 300), (64, HF, E4, 3000), (256, BF, BF, 3000)])
+def test_many_prompts(R, single, dim, dtype, cache, top):
+    """More requests than a wave has lanes, some of them empty, in one part and in several."""
+    new = [0 if r % 11 == 3 else 1 if single and r % 3 else 5 + r * 7 % 40 for r in range(R)]
+    length = [n + r * 37 % 130 for r, n in enumerate(new)]
+    length[R // 2], length[-1] = top, top - 1
+    c = attend_case(R, new, length, 16, 2, dim, dtype, cache)
+    parts = B.pp_attention_workspace(c["q"], c["k"], c["table"], max_new=max(new), max_len=top)
+    assert (parts > 0) == (top > 300)
+    check_requests(c, range(R))

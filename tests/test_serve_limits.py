@@ -8,7 +8,7 @@ import pytest
 
 from paper_2608_01655_amd import binding as B
 from paper_2608_01655_amd import build
-from tests.test_serve_host import L, _attention, _block_args, _kv_pages  # noqa: F401
+from tests.test_serve_host import AT, L, _attention, _block_args, _kv_pages  # noqa: F401
 
 
 def workspace(L, **kw):
@@ -71,3 +71,16 @@ def test_block_tables_refuse_rows_that_overlap(L):
     for kw in (dict(row_stride=0), dict(row_stride=7), dict(requests=65536, row_stride=7)):
         assert L.pp_block_tables(ctypes.byref(_block_args(**kw)), None) == B.PP_E_ARG
         assert "overlap" in B.pp_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(max_len=30_000), dict(requests=1, tokens=600, max_new=600, max_len=30_000, max_blocks=2000)])
+def test_attention_refuses_a_workspace_that_does_not_do(L, kw):
+    """None, too little of it, and one that does not start at 256 bytes: refused before anything is enqueued."""
+    kw = dict(dict(max_blocks=2000), **kw)
+    p = _kv_pages()
+    need = L.pp_attention_workspace(ctypes.byref(p), ctypes.byref(_attention(**kw)))
+    assert need > 0
+    for at, size in ((None, need), (AT, need - 1), (AT, 0), (AT, -1), (AT + 16, need + 1024), (AT + 128, need + 1024)):
+        a = _attention(workspace=at, workspace_bytes=size, **kw)
+        assert L.pp_paged_attention(ctypes.byref(p), ctypes.byref(a), None) == B.PP_E_ARG, (at, size)
+        assert "workspace" in B.pp_last_error()
