@@ -572,7 +572,8 @@ int pp_kv_write(const pp_kv_pages *pages, int32_t tokens, int32_t dtype,
  * the last as the last; tokens past a row of the block table do not exist.
  * Scores, sums and the accumulation are held in 32 bits; weights are rounded
  * to the queries' type for the product with V.
- * max_new and max_len bound every request's new tokens and length; a request
+ * max_new and max_len bound every request's new tokens and length (parts of
+ * long requests are cut by max_len, so one far above costs time); a request
  * of more than max_new new tokens may be left unwritten, and rows of tokens
  * that no request has are.  `workspace` is device memory
  * of pp_attention_workspace bytes at least (256-byte aligned); the call

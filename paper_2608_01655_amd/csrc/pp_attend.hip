@@ -652,10 +652,11 @@ template <bool NARROW, int D>
 constexpr int kTilesLds = 2 * 2 * 64 * D * (NARROW ? 1 : 2);
 
 // 128 rows of one request and key head, and one part of its keys, a block.  Bound by the matrix
-// cores and the exponentials beside them: 4 x 2,048 new tokens behind 6,144 to 14,336 (32 heads,
-// dim 128) 1.04 to 1.08 ms, 0.99 to 1.03 PFLOP/s, matrix cores 58% busy; a product of 8,192 squared
-// reaches 1.2 to 1.3.  Two blocks of four waves share a CU, so that one's loads and joins hide
-// behind the other's products.
+// cores, the exponentials beside them and LDS, which at the matrix cores' full rate would give all it
+// has, 128 bytes a clock: every wave reads the whole tile for its 32 rows.  4 x 2,048 new tokens behind
+// 6,144 to 14,336 (32 heads, dim 128) take 1.04 to 1.12 ms from card to card, 0.95 to 1.03 PFLOP/s,
+// matrix cores 58% busy (6% longer in f16); a product of 8,192 squared reaches 1.2 to 1.3.  Two blocks
+// of four waves share a CU, so that one's loads and joins hide behind the other's products.
 template <bool F16, bool NARROW, int D>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2)
 k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
@@ -1159,8 +1160,11 @@ __global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int3
 
 // -------------------------------------------------------------- dispatch ---
 
-// Blocks of k_tiles that are resident: at dim 256 its registers leave room for one a CU (300 new tokens
-// behind 11,700 of 8-bit pages, counted as two a CU: 7% slower; 700 behind 8,300: 6% faster).
+// Blocks of k_tiles that the rule below counts on at a time.  At dim 256 its registers leave room for
+// one a CU (100 new tokens behind 15,900 in 18 parts 61 us, counted as two a CU in 25 parts 90 us; 8 x 200
+// behind up to 8,800 403 and 507 us; 3 x 700 the other way, 399 and 383).  At dim 64 three fit, but
+// counted as three the calls are not faster: 512 behind 7,680 39 and 38 us, 4 x 700 behind up to 8,300 87
+// and 103 us.
 int tile_blocks(int32_t dim) { return dim == 256 ? 256 : 512; }
 
 int64_t round_up(int64_t x, int32_t m) { return (x + m - 1) / m * m; }
@@ -1201,10 +1205,14 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Plan& pl) {
   cut(1, 128, pl.cut_rows, pl.parts_rows);
   cut(1, 128, pl.cut_tiles, pl.parts_tiles);
   if (ch.rt) {
-    // Lengths differ, so the fewer requests there are the smaller their parts have to be: 64 requests and 4
-    // heads in 31, 16 or 8 parts took 85, 92 and 107 us; 256 requests and 8 heads in 1, 2 or 4 took 550, 556
-    // and 652 us (a block that finds no keys still waits for its turn).  Below 256 keys a block's start and
-    // end are most of it: with 128, 64 requests take 90 us and not 84, one of 16,000 tokens 26 and not 18.
+    // As many parts as make 8,192 blocks (4,096 where requests times heads is 512 or more), but of 256 keys at
+    // least, rounded up to a multiple of 128: where that decides, parts of 384 keys, or of 256 where keys
+    // is a multiple of 256.  Lengths differ, so the fewer requests there are the smaller their parts have to be,
+    // and in small parts a block's start and end and the join are most of it.  In parts of 128, 256, 384,
+    // 512 and 1,024 keys 64 requests of up to 8,190 and 4 heads take 106, 90, 85, 90 and 104 us; one of
+    // 16,000 and 2 heads in the first four 25, 18, 17 and 17 us, one of 4,097 13, 13, 13 and 15.  256
+    // requests of up to 16,384 and 8 heads take 552 us whole, 555 in two parts (which the rule takes) and
+    // 652 in four: a block that finds no keys still waits for its turn.
     const int64_t base = (int64_t)a.requests * p.heads;
     int64_t n = ((base < 512 ? 8192 : 4096) + base - 1) / base;
     if (n > keys / 256) n = keys / 256;
