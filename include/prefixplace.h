@@ -452,7 +452,9 @@ int pp_backtrack_table(int32_t n, const int32_t *parent, uint32_t *table,
  * node, slot, page and token numbers out of range are treated as absent
  * where the text says so, and in no case lead out of the arrays given.
  * Row starts of queries, keys, values, outputs and pages are 16-byte
- * aligned: their pointers, and their strides times the element size.
+ * aligned: their pointers, and their strides times the element size.  Rows
+ * that are written do not overlap (a stride below dim where there are two or
+ * more is refused); rows that are only read may, of expanded tensors say.
  * ------------------------------------------------------------------------ */
 
 /* Element types of rows and pages.  PP_E4M3 is the 8-bit float of 4 exponent

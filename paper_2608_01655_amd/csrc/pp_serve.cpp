@@ -24,6 +24,9 @@ bool row_layout(const void* p, int64_t size, int64_t s0, int64_t s1, int64_t s2 
          s1 * size % 16 == 0 && s2 * size % 16 == 0;
 }
 
+// Rows that are written: those next to each other in a dimension of `count` do not overlap.
+bool apart(int64_t count, int64_t stride, int32_t dim) { return count < 2 || stride >= dim; }
+
 int64_t size_of(int32_t dtype) { return dtype == PP_E4M3 ? 1 : 2; }
 
 bool row_type(int32_t t) { return t == PP_BF16 || t == PP_F16; }
@@ -187,6 +190,10 @@ int pp_kv_write(const pp_kv_pages* pages, int32_t tokens, int32_t dtype, const v
   if (rc != PP_OK) return rc;
   if (tokens < 0) return report(PP_E_ARG, "negative size");
   if (tokens == 0) return PP_OK;
+  if (!apart(pages->n_pages, pages->page_stride, pages->dim) ||
+      !apart(pages->heads, pages->head_stride, pages->dim) ||
+      !apart(pages->page_size, pages->token_stride, pages->dim))
+    return report(PP_E_ARG, "rows of the pages overlap");
   if (!k || !v || !slot_map) return report(PP_E_ARG, "null pointer");
   if (!row_layout(k, 2, k_token_stride, k_head_stride) ||
       !row_layout(v, 2, v_token_stride, v_head_stride))
@@ -213,6 +220,8 @@ int pp_paged_attention(const pp_kv_pages* pages, const pp_attention_args* a, voi
   if (!row_layout(a->q, 2, a->q_token_stride, a->q_head_stride) ||
       !row_layout(a->out, 2, a->out_token_stride, a->out_head_stride))
     return report(PP_E_ARG, "rows start at 16-byte boundaries, at strides >= 0");
+  if (!apart(a->tokens, a->out_token_stride, pages->dim) || !apart(a->q_heads, a->out_head_stride, pages->dim))
+    return report(PP_E_ARG, "rows of out overlap");
   const int64_t need = attention_workspace(*pages, *a);
   if (need && (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need))
     return report(PP_E_ARG, "workspace too small or not 256-byte aligned");

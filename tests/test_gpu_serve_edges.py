@@ -220,3 +220,25 @@ def test_many_prompts(R, single, dim, dtype, cache, top):
     parts = B.pp_attention_workspace(c["q"], c["k"], c["table"], max_new=max(new), max_len=top)
     assert (parts > 0) == (top > 300)
     check_requests(c, range(R))
+
+
+def test_expanded_tensors_that_are_read():
+    """One row of queries, of pages and of the block table for all: the same as with copies of them."""
+    c = attend_case(15, [1, 1, 1], [70, 70, 70], 8, 2, 128, BF, BF)
+    c["table"][1:] = c["table"][:1]
+    q = c["q"][:1, :1].expand(3, 8, 128)
+    want = [x.clone() for x in attend(dict(c, q=q.contiguous()))]
+    k, v = (c[x][:, :1].expand(-1, 2, -1, -1) for x in "kv")
+    got = attend(dict(c, q=q, table=c["table"][:1].expand(3, -1)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    want = [x.clone() for x in attend(dict(c, k=k.contiguous(), v=v.contiguous()))]
+    got = attend(dict(c, k=k, v=v))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    pages = torch.zeros((2, 3, 2, 16, 128), dtype=BF, device="cuda")
+    row = torch.randn((1, 1, 128), dtype=BF, device="cuda")
+    B.pp_kv_write(row.expand(5, 2, 128), -row.expand(5, 2, 128), torch.arange(5, device="cuda"), pages[0], pages[1])
+    assert torch.equal(pages[0, 0, :, :5], row.expand(2, 5, 128)) and torch.equal(pages[1, 0, :, :5], -row.expand(2, 5, 128))
+    with pytest.raises(B.PPError):
+        B.pp_kv_write(row.expand(1, 2, 128), row.expand(1, 2, 128), torch.arange(1, device="cuda"), pages[0, :1].expand(3, -1, -1, -1), pages[1, :1].expand(3, -1, -1, -1))
+    with pytest.raises(B.PPError):
+        attend(dict(c, out=c["out"][:, :1].expand(3, 8, 128)))

@@ -84,3 +84,15 @@ def test_attention_refuses_a_workspace_that_does_not_do(L, kw):
         a = _attention(workspace=at, workspace_bytes=size, **kw)
         assert L.pp_paged_attention(ctypes.byref(p), ctypes.byref(a), None) == B.PP_E_ARG, (at, size)
         assert "workspace" in B.pp_last_error()
+
+
+def test_writes_refuse_rows_that_overlap(L):
+    """Pages of an expanded tensor, or rows closer than they are long; of one page or head its stride says nothing."""
+    rows = (3, B.PP_BF16, AT, 256, 128, AT, 256, 128, AT, None)
+    for kw in (dict(page_stride=0), dict(page_stride=64), dict(head_stride=0), dict(head_stride=120), dict(token_stride=0),
+               dict(token_stride=64), dict(n_pages=1, token_stride=0), dict(heads=1, token_stride=0)):
+        assert L.pp_kv_write(ctypes.byref(_kv_pages(**kw)), *rows) == B.PP_E_ARG
+        assert "overlap" in B.pp_last_error()
+    for kw in (dict(out_token_stride=0), dict(out_token_stride=120), dict(out_head_stride=0), dict(out_head_stride=64)):
+        assert L.pp_paged_attention(ctypes.byref(_kv_pages()), ctypes.byref(_attention(**kw)), None) == B.PP_E_ARG
+        assert "overlap" in B.pp_last_error()
