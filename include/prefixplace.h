@@ -605,6 +605,152 @@ int64_t pp_attention_workspace(const pp_kv_pages *pages, const pp_attention_args
 int pp_paged_attention(const pp_kv_pages *pages, const pp_attention_args *args,
                        void *hip_stream);
 
+/* ------------------------------------------------------------------------
+ * Around the pages: what brings rows into them, pages of latent rows, and
+ * what moves, shares and frees pages.  The same conventions hold: work is
+ * enqueued on `hip_stream`, nothing is allocated or waited for, numbers out
+ * of range in device arrays lead out of no array given.  What a call reads
+ * and what it writes do not overlap, but where the text allows it.
+ * ------------------------------------------------------------------------ */
+
+/* Host only: frequencies of rotary positions as pp_rotary_write reads them.
+ * Pair i of dim / 2 turns by w_i = base^(-2 i / dim) radians a token, or,
+ * for contexts longer than trained on, by g_i w_i + (1 - g_i) w_i / factor
+ * with g_i = (original w_i / 2 pi - slow) / (fast - slow) held to 0 .. 1:
+ * pairs that make fewer than `slow` turns in the `original` tokens slow down
+ * by `factor`, those of more than `fast` keep their pace (original = 0: all
+ * slow down; factor = 1: none).  Out, either may be NULL: radians
+ * [dim / 2] and turns [dim / 2], w / 2 pi in units of 2^-64 turns, so that
+ * position * turns modulo 2^64 is the angle at any position, exactly reduced.
+ * dim even, base > 1, factor >= 1, original >= 0, fast > slow >= 0. */
+int pp_rotary_turns(int32_t dim, double base, double factor, double original,
+                    double slow, double fast, double *radians, uint64_t *turns);
+
+/* Host only: turns [n] of any radians [n] a token (finite). */
+int pp_turns(int32_t n, const double *radians, uint64_t *turns);
+
+/* Norms of queries and keys for each head, their rotation by position, and
+ * the write into the pages, in one pass.
+ *   A row's first `norm` elements (0 = none) become
+ *     x / sqrt(mean of x^2 + eps) * weight,
+ *   then of the rot_dim elements from `first` on the pairs (a, b) become
+ *     amplitude * (a cos t - b sin t, a sin t + b cos t),
+ *   t = position[token] * frequency: elements (i, i + rot_dim / 2), or
+ *   (2 i, 2 i + 1) where `interleaved`, with turns[i].
+ * q goes to q_out.  k goes to k_out, or where pages are given to the place
+ * slot_map names, with v as it is; places and 8-bit pages as in pp_kv_write,
+ * but the one rounding is from 32 bits.  Pages without v (pages->v and v
+ * NULL) hold one row a token and head, latent rows with heads = 1 say.
+ * q_heads or k_heads = 0: no such rows.  Rows are [tokens][heads][dim];
+ * dims, firsts and norms are multiples of 8, dims at most 1,024, rot_dim is
+ * a multiple of 16 (0 = no rotation); weights are of the rows' type.
+ * An output may be its input (the same pointer and strides). */
+typedef struct {
+    int32_t tokens;
+    int32_t dtype;                 /* of all rows and weights: PP_BF16 or PP_F16 */
+    int32_t q_heads, q_dim, q_first, q_norm;
+    int32_t k_heads, k_dim, k_first, k_norm;
+    int32_t rot_dim, interleaved;
+    float eps, amplitude;
+    int64_t q_token_stride, q_head_stride;      /* elements */
+    int64_t q_out_token_stride, q_out_head_stride;
+    int64_t k_token_stride, k_head_stride;
+    int64_t k_out_token_stride, k_out_head_stride;
+    int64_t v_token_stride, v_head_stride;
+    const void *q, *k, *v;
+    void *q_out, *k_out;
+    const void *q_weight, *k_weight;            /* [q_norm], [k_norm], 16-byte aligned */
+    const int32_t *position;                    /* [tokens] */
+    const uint64_t *turns;                      /* [rot_dim / 2], 16-byte aligned */
+    const int64_t *slot_map;                    /* [tokens] */
+} pp_rotary_args;
+int pp_rotary_write(const pp_rotary_args *args, const pp_kv_pages *pages, void *hip_stream);
+
+/* Attention over pages of latent rows: one row C_j of `dim` elements a
+ * token, which every query head reads, and whose first `value_dim` elements
+ * are its value:
+ *   s_j = scale * <q, C_j>,  out = sum_j e^(s_j) C_j[0 .. value_dim) / sum_j e^(s_j).
+ * So queries are those of latent attention with the keys' expansion
+ * multiplied in, and out is yet to be multiplied by the values' expansion.
+ * Pages: k the rows, v NULL, heads 1, k_scale [1] (PP_E4M3 pages);
+ * value_dim 512 or 256, dim = value_dim + 64.  Everything else is as in
+ * pp_paged_attention; out rows are [tokens][q_heads][value_dim]. */
+int64_t pp_latent_workspace(const pp_kv_pages *pages, int32_t value_dim,
+                            const pp_attention_args *args);
+int pp_latent_attention(const pp_kv_pages *pages, int32_t value_dim,
+                        const pp_attention_args *args, void *hip_stream);
+
+/* Copies pages: move i copies page source[i] to page target[i], its first
+ * tokens[i] tokens (tokens NULL: all), in every pool (all layers' keys and
+ * values, say).  The pools' layouts are alike, in strides of elements as in
+ * pp_kv_pages.  Moves whose source or target is out of range, or which are the
+ * same page, do nothing; tokens are held to 0 .. page_size.  Moves
+ * are made at once: no target is to be named twice, or to be a source. */
+typedef struct {
+    int32_t moves;
+    int32_t n_pools;
+    int32_t dtype;                 /* PP_BF16, PP_F16 or PP_E4M3 */
+    int32_t n_pages, page_size;    /* page_size a power of two, 16 .. 1,024 */
+    int32_t heads, dim;            /* rows of dim elements are multiples of 16 bytes */
+    int64_t page_stride, head_stride, token_stride;
+    void *const *pools;            /* host array [n_pools] of device pointers */
+    const int32_t *source, *target;             /* [moves] */
+    const int32_t *tokens;                      /* [moves] or NULL */
+} pp_copy_args;
+int pp_page_copy(const pp_copy_args *args, void *hip_stream);
+
+/* Rows of block tables from their parents' (beams, several samples of a
+ * prompt).  New row r continues row parent[r] of block_table (out of range:
+ * it has no tokens and is not written): out_length[r] = length[parent[r]],
+ * and row r of out_table gets the parent's pages, ceil(length / page_size).
+ * Full pages are shared.  The page of the last block, where it is not full, is kept
+ * by the first new row of a parent; every further one takes a page off
+ * free_pages, in order of r, and the copy it needs is move r of source,
+ * target and tokens as pp_page_copy reads them (source -1, target -1, 0
+ * tokens: none).  taken[0] = pages needed; above n_free the rows that came
+ * too late have target -1 and -1 in their last block.  Blocks at or past
+ * max_blocks do not exist; negative lengths act as 0.  out_table does not
+ * overlap block_table. */
+typedef struct {
+    int32_t rows;                  /* new rows, >= 0, at most 65,536 */
+    int32_t parents;               /* rows of block_table, at most 65,536 */
+    int32_t n_free;
+    int32_t max_blocks;            /* entries a row of either table holds */
+    int32_t page_size;             /* a power of two, 16 .. 1,024 */
+    int64_t row_stride, out_row_stride;         /* entries, max_blocks at least */
+    const int32_t *parent;                      /* [rows] */
+    const int32_t *length;                      /* [parents] */
+    const int32_t *block_table;                 /* [parents][max_blocks] */
+    const int32_t *free_pages;                  /* [n_free] */
+    int32_t *out_table;                         /* [rows][max_blocks] */
+    int32_t *out_length;                        /* out [rows] */
+    int32_t *source, *target, *tokens;          /* out [rows] */
+    int32_t *taken;                             /* out [1] */
+} pp_fork_args;
+int pp_fork_tables(const pp_fork_args *args, void *hip_stream);
+
+/* The pages that no request has: numbers from `first` (past the slots'
+ * pages) to before n_pages that no row of block_table names in its
+ * ceil(length / page_size) blocks, in increasing order.  count[0] = how
+ * many; the first `room` of them are written to free_pages, whose other
+ * entries stay as they are.  marks [n_pages] is scratch memory (8-byte
+ * aligned), written before it is read.  Numbers out of range in rows name
+ * no page. */
+typedef struct {
+    int32_t requests;              /* >= 0, at most 65,536 */
+    int32_t max_blocks;
+    int32_t page_size;             /* a power of two, 16 .. 1,024 */
+    int32_t n_pages, first;        /* 0 <= first <= n_pages */
+    int32_t room;
+    int64_t row_stride;
+    const int32_t *length;                      /* [requests] */
+    const int32_t *block_table;                 /* [requests][max_blocks] */
+    int32_t *free_pages;                        /* out [room] */
+    int32_t *count;                             /* out [1] */
+    uint8_t *marks;                             /* [n_pages] */
+} pp_free_args;
+int pp_free_pages(const pp_free_args *args, void *hip_stream);
+
 /* Description of the last error on the calling thread; valid until the
  * next pp_* call on that thread. */
 const char *pp_last_error(void);

@@ -106,6 +106,44 @@ class pp_attention_args(ctypes.Structure):
                [("workspace_bytes", ctypes.c_int64)]
 
 
+class pp_rotary_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("tokens", "dtype", "q_heads", "q_dim", "q_first", "q_norm", "k_heads",
+                 "k_dim", "k_first", "k_norm", "rot_dim", "interleaved")] + \
+               [("eps", ctypes.c_float), ("amplitude", ctypes.c_float)] + \
+               [(f, ctypes.c_int64) for f in
+                ("q_token_stride", "q_head_stride", "q_out_token_stride",
+                 "q_out_head_stride", "k_token_stride", "k_head_stride",
+                 "k_out_token_stride", "k_out_head_stride", "v_token_stride",
+                 "v_head_stride")] + \
+               [(f, _P) for f in
+                ("q", "k", "v", "q_out", "k_out", "q_weight", "k_weight", "position",
+                 "turns", "slot_map")]
+
+
+class pp_copy_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("moves", "n_pools", "dtype", "n_pages", "page_size", "heads", "dim")] + \
+               [(f, ctypes.c_int64) for f in ("page_stride", "head_stride", "token_stride")] + \
+               [(f, _P) for f in ("pools", "source", "target", "tokens")]
+
+
+class pp_fork_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("rows", "parents", "n_free", "max_blocks", "page_size")] + \
+               [("row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64)] + \
+               [(f, _P) for f in
+                ("parent", "length", "block_table", "free_pages", "out_table", "out_length",
+                 "source", "target", "tokens", "taken")]
+
+
+class pp_free_args(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("requests", "max_blocks", "page_size", "n_pages", "first", "room")] + \
+               [("row_stride", ctypes.c_int64)] + \
+               [(f, _P) for f in ("length", "block_table", "free_pages", "count", "marks")]
+
+
 class PPError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"prefixplace error {code}: {msg}")
@@ -170,8 +208,19 @@ def lib() -> ctypes.CDLL:
         L.pp_attention_workspace.argtypes = [_P, _P]
         L.pp_attention_workspace.restype = i64
         L.pp_paged_attention.argtypes = [_P, _P, _P]
+        L.pp_rotary_turns.argtypes = [i32, f64, f64, f64, f64, f64, _P, _P]
+        L.pp_turns.argtypes = [i32, _P, _P]
+        L.pp_rotary_write.argtypes = [_P, _P, _P]
+        L.pp_latent_workspace.argtypes = [_P, i32, _P]
+        L.pp_latent_workspace.restype = i64
+        L.pp_latent_attention.argtypes = [_P, i32, _P, _P]
+        L.pp_page_copy.argtypes = [_P, _P]
+        L.pp_fork_tables.argtypes = [_P, _P]
+        L.pp_free_pages.argtypes = [_P, _P]
         for f in (L.pp_prefix_table, L.pp_cache_slots, L.pp_block_tables,
-                  L.pp_kv_write, L.pp_paged_attention):
+                  L.pp_kv_write, L.pp_paged_attention, L.pp_rotary_turns, L.pp_turns,
+                  L.pp_rotary_write, L.pp_latent_attention, L.pp_page_copy,
+                  L.pp_fork_tables, L.pp_free_pages):
             f.restype = ctypes.c_int
         for f in (L.pp_plan, L.pp_replan, L.pp_replan_f64, L.pp_plan_f64,
                   L.pp_plan_f64_device,
@@ -563,6 +612,10 @@ def pp_cache_slots(target, n_slots, held=None):
 _BLOCK_ARGS = struct.Struct("@9iq13P")
 _KV_PAGES = struct.Struct("@4P5i3q")
 _ATTENTION_ARGS = struct.Struct("@8if5q7Pq")
+_ROTARY_ARGS = struct.Struct("@12i2f10q10P")
+_COPY_ARGS = struct.Struct("@7i3q4P")
+_FORK_ARGS = struct.Struct("@5i2q10P")
+_FREE_ARGS = struct.Struct("@6iq5P")
 _torch = None
 _types = {}
 
@@ -597,7 +650,7 @@ def _refuse_ints(t, what, dtype, shape):
 
 def _table(torch, t, R, device):
     if t.dtype != torch.int32 or t.get_device() != device or t.dim() != 2 or t.shape[0] != R \
-            or (t.stride(1) != 1 and t.shape[1] > 1):
+            or (t.stride(1) != 1 and t.shape[1] > 1 and R):
         raise ValueError("block_table: want int32 rows, one a request, on the GPU")
     return t.data_ptr()
 
@@ -666,13 +719,14 @@ def _scale(torch, s, H, device):
 def _pages(torch, k_cache, v_cache, k_scale, v_scale, device):
     """(packed pp_kv_pages, heads, dim)."""
     strides = k_cache.stride()
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or strides != v_cache.stride() \
-            or strides[3] != 1 or k_cache.dtype != v_cache.dtype \
-            or k_cache.get_device() != device or v_cache.get_device() != device:
+    if k_cache.dim() != 4 or strides[3] != 1 or k_cache.get_device() != device \
+            or (v_cache is not None and (
+                k_cache.shape != v_cache.shape or strides != v_cache.stride()
+                or k_cache.dtype != v_cache.dtype or v_cache.get_device() != device)):
         raise ValueError("pages: want two device tensors [pages][heads][page_size][dim] "
                          "alike, dim contiguous")
     P, H, ps, D = k_cache.shape
-    return _KV_PAGES.pack(k_cache.data_ptr(), v_cache.data_ptr(), _scale(torch, k_scale, H, device),
+    return _KV_PAGES.pack(k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(), _scale(torch, k_scale, H, device),
                           _scale(torch, v_scale, H, device), _type(k_cache), P, ps, H, D,
                           *strides[:3]), H, D
 
@@ -711,10 +765,20 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
     device, st = _stream_of(torch, q, stream)
     L = lib()
     pages, _, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
+    if q.dim() == 3 and (q.shape[2] != D or out.shape != q.shape):
+        raise ValueError("shape mismatch")
+    _attend(torch, device, st, stream, L.pp_attention_workspace, L.pp_paged_attention, (pages,), q,
+            block_table, query_start, length, out, lse, scale, max_new, max_len, window, workspace)
+
+
+def _attend(torch, device, st, stream, work, call, head, q, block_table, query_start, length, out,
+            lse, scale, max_new, max_len, window, workspace):
+    """The checks and the call that attention over pages of any kind has: work and call are the C
+    entries, head their arguments before pp_attention_args."""
     (qt, qh), (ot, oh) = _rows(q, "q", device), _rows(out, "out", device)
-    T, Hq, d = q.shape
+    T, Hq, _ = q.shape
     R = length.shape[0]
-    if d != D or out.shape != q.shape or out.dtype != q.dtype:
+    if out.shape[:2] != q.shape[:2] or out.dtype != q.dtype:
         raise ValueError("shape mismatch")
     i32 = torch.int32
     if length.dtype != i32 or length.dim() != 1 or length.get_device() != device \
@@ -737,7 +801,7 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
 
     if workspace is None:
         a = args(0, 0)
-        need = L.pp_attention_workspace(pages, a)
+        need = work(*head, a)
         if need < 0:
             _check(need)
         if need:
@@ -751,7 +815,235 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace: want a contiguous tensor on the current GPU")
         a = args(workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = L.pp_paged_attention(pages, a, st)
+    rc = call(*head, a, st)
+    if rc:
+        _check(rc)
+
+
+def pp_rotary_turns(dim, base=10000.0, *, factor=1.0, original=0.0, slow=1.0, fast=32.0):
+    """Frequencies of rotary positions as pp_rotary_write reads them, int64
+    [dim / 2] (host only; see include/prefixplace.h).  factor, original, slow
+    and fast scale them for contexts longer than `original` tokens."""
+    turns = np.zeros(max(int(dim), 0) // 2, np.uint64)
+    _check(lib().pp_rotary_turns(int(dim), float(base), float(factor), float(original),
+                                 float(slow), float(fast), None, _p(turns)))
+    return turns.view(np.int64)
+
+
+def pp_turns(radians):
+    """Turns of any frequencies in radians a token, int64 [n] (host only; see
+    include/prefixplace.h)."""
+    radians = _c(radians, np.float64)
+    turns = np.zeros(radians.shape[0], np.uint64)
+    _check(lib().pp_turns(radians.shape[0], _p(radians), _p(turns)))
+    return turns.view(np.int64)
+
+
+def _weight(w, rows, device):
+    """(elements normed, address) of a norm's weights for `rows`."""
+    if w is None:
+        return 0, 0
+    if rows is None or w.dim() != 1 or w.dtype != rows.dtype or w.get_device() != device \
+            or not w.is_contiguous():
+        raise ValueError("weights: want a contiguous vector of the rows' type on the GPU")
+    return w.shape[0], w.data_ptr()
+
+
+def pp_rotary_write(position, turns, *, q=None, q_out=None, k=None, k_out=None, v=None,
+                    slot_map=None, k_cache=None, v_cache=None, k_scale=None, v_scale=None,
+                    q_weight=None, k_weight=None, eps=1e-6, q_first=0, k_first=0,
+                    interleaved=False, amplitude=1.0, stream=None):
+    """Norms of queries and keys for each head, rotation by position, and the
+    write into the pages, on torch device tensors (see
+    include/prefixplace.h).  Rows q, k, v [tokens][heads][dim]; position int32
+    [tokens] and turns int64 [pairs] (pp_rotary_turns) or None for no
+    rotation; the pairs begin at element q_first and k_first.  q_weight and
+    k_weight [n]: the first n elements are normed.  q goes to q_out (q itself
+    will do); k goes to k_out (k itself will do), or with k_cache to the places slot_map
+    names, and v with it; without v_cache the pages have keys (latent rows)
+    only."""
+    torch = _torch or _with_torch()
+    first = q if q is not None else k
+    if first is None or (q is None) != (q_out is None) or (k is None and k_cache is not None) \
+            or (k is not None and (k_out is None) == (k_cache is None)) \
+            or (v is None) != (v_cache is None) or (v is not None and k_cache is None):
+        raise ValueError("want q with q_out, k with k_out or k_cache, v with v_cache")
+    device, st = _stream_of(torch, first, stream)
+    T, dtype = first.shape[0], first.dtype
+    strides, dims = [], []
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            strides += [0, 0, 0, 0]
+            dims.append((0, 0))
+            continue
+        strides += _rows(x, what, device)
+        if x.shape[0] != T or x.dtype != dtype:
+            raise ValueError("shape mismatch")
+        if out is None:
+            strides += [0, 0]
+        else:
+            strides += _rows(out, what + "_out", device)
+            if out.shape != x.shape or out.dtype != dtype:
+                raise ValueError("shape mismatch")
+        dims.append(tuple(x.shape[1:]))
+    pages, slots = None, 0
+    if v is None:
+        strides += [0, 0]
+    else:
+        strides += _rows(v, "v", device)
+        if v.shape != k.shape or v.dtype != dtype:
+            raise ValueError("shape mismatch")
+    if k_cache is not None:
+        pages, H, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
+        if slot_map is None or slot_map.dtype != torch.int64 or slot_map.shape != (T,) \
+                or slot_map.get_device() != device or not slot_map.is_contiguous():
+            raise ValueError(f"slot_map: want a contiguous int64 tensor of shape {(T,)} on the "
+                             "current GPU")
+        if (H, D) != dims[1]:
+            raise ValueError("shape mismatch")
+        slots = slot_map.data_ptr()
+    elif k_scale is not None or v_scale is not None or slot_map is not None:
+        raise ValueError("scales and places are for pages")
+    rot = at = turning = 0
+    if turns is not None:
+        if turns.dtype != torch.int64 or turns.dim() != 1 or turns.get_device() != device \
+                or not turns.is_contiguous():
+            _refuse_ints(turns, "turns", torch.int64, ("pairs",))
+        if position is None or position.dtype != torch.int32 or position.shape != (T,) \
+                or position.get_device() != device or not position.is_contiguous():
+            raise ValueError(f"position: want a contiguous int32 tensor of shape {(T,)} on the "
+                             "current GPU")
+        rot, at, turning = 2 * turns.shape[0], position.data_ptr(), turns.data_ptr()
+    q_norm, q_w = _weight(q_weight, q, device)
+    k_norm, k_w = _weight(k_weight, k, device)
+    rc = lib().pp_rotary_write(_ROTARY_ARGS.pack(
+        T, _type(first), *dims[0], q_first, q_norm, *dims[1], k_first, k_norm, rot,
+        1 if interleaved else 0, eps, amplitude, *strides,
+        0 if q is None else q.data_ptr(), 0 if k is None else k.data_ptr(),
+        0 if v is None else v.data_ptr(), 0 if q_out is None else q_out.data_ptr(),
+        0 if k_out is None else k_out.data_ptr(), q_w, k_w, at, turning, slots), pages, st)
+    if rc:
+        _check(rc)
+
+
+def pp_latent_attention(q, cache, block_table, query_start, length, out, lse=None, *, scale,
+                        max_new, max_len, window=0, k_scale=None, workspace=None, stream=None):
+    """Attention of the batch's new tokens over pages of latent rows, on torch
+    device tensors (see include/prefixplace.h): q [tokens][q_heads][dim], cache
+    [pages][1][page_size][dim], out [tokens][q_heads][value_dim]; everything
+    else as in pp_paged_attention."""
+    torch = _torch or _with_torch()
+    device, st = _stream_of(torch, q, stream)
+    if cache.dim() != 4 or cache.shape[1] != 1:
+        raise ValueError("cache: want [pages][1][page_size][dim]")
+    pages, _, D = _pages(torch, cache, None, k_scale, None, device)
+    if q.dim() != 3 or q.shape[2] != D or out.dim() != 3:
+        raise ValueError("shape mismatch")
+    L = lib()
+    _attend(torch, device, st, stream, L.pp_latent_workspace, L.pp_latent_attention,
+            (pages, out.shape[2]), q, block_table, query_start, length, out, lse, scale, max_new,
+            max_len, window, workspace)
+
+
+def pp_latent_workspace(q, cache, block_table, value_dim, *, max_new, max_len, window=0) -> int:
+    """Bytes of workspace pp_latent_attention needs for calls of these shapes
+    (only shapes, strides and types of the tensors count)."""
+    torch = _torch or _with_torch()
+    device = q.get_device()
+    if device < 0:
+        raise ValueError("tensors must lie on the GPU")
+    pages, _, _ = _pages(torch, cache, None, None, None, device)
+    qt, qh = _rows(q, "q", device)
+    T, Hq, _ = q.shape
+    need = lib().pp_latent_workspace(pages, int(value_dim), _ATTENTION_ARGS.pack(
+        block_table.shape[0], T, Hq, _type(q), max_new, max_len, block_table.shape[1], window, 1.0,
+        qt, qh, qt, qh, block_table.stride(0), 0, 0, 0, 0, 0, 0, 0, 0))
+    if need < 0:
+        _check(need)
+    return need
+
+
+def _ints(torch, t, n, what, device):
+    if t.dtype != torch.int32 or t.shape != (n,) or t.get_device() != device \
+            or not t.is_contiguous():
+        _refuse_ints(t, what, torch.int32, (n,))
+    return t.data_ptr()
+
+
+def pp_page_copy(pools, source, target, tokens=None, *, stream=None):
+    """Copies pages source[i] to target[i], their first tokens[i] tokens (None:
+    all), in every pool: a sequence of device tensors
+    [pages][heads][page_size][dim] alike in shape, strides and type (see
+    include/prefixplace.h).  source, target and tokens int32 [moves] on the
+    GPU."""
+    torch = _torch or _with_torch()
+    device, st = _stream_of(torch, source, stream)
+    n = source.shape[0]
+    at = (_ints(torch, source, n, "source", device), _ints(torch, target, n, "target", device),
+          0 if tokens is None else _ints(torch, tokens, n, "tokens", device))
+    if not len(pools):
+        return
+    first = pools[0]
+    shape, strides, dtype = first.shape, first.stride(), first.dtype
+    for p in pools:
+        if p.dim() != 4 or p.shape != shape or p.stride() != strides or p.dtype != dtype \
+                or p.get_device() != device or strides[3] != 1:
+            raise ValueError("pools: want device tensors [pages][heads][page_size][dim] alike, "
+                             "dim contiguous")
+    P, H, ps, D = shape
+    bases = struct.pack(f"@{len(pools)}P", *[p.data_ptr() for p in pools])
+    table = ctypes.c_char_p(bases)
+    rc = lib().pp_page_copy(_COPY_ARGS.pack(
+        n, len(pools), _type(first), P, ps, H, D, *strides[:3],
+        ctypes.cast(table, _P).value, *at), st)
+    if rc:
+        _check(rc)
+
+
+def pp_fork_tables(parent, length, block_table, free_pages, out_table, out_length, source,
+                   target, tokens, taken, *, page_size, stream=None):
+    """Rows of block tables from their parents' on torch device tensors (see
+    include/prefixplace.h).  Inputs parent int32 [R], length int32 [parents],
+    block_table int32 [parents][blocks], free_pages int32 [f]; outputs
+    out_table int32 [R][blocks] (not block_table), out_length, source, target, tokens
+    int32 [R], taken int32 [1].  source, target and tokens are the copies that
+    pp_page_copy makes."""
+    torch = _torch or _with_torch()
+    device, st = _stream_of(torch, parent, stream)
+    R, P, f = parent.shape[0], length.shape[0], free_pages.shape[0]
+    rows = _table(torch, block_table, P, device)
+    out = _table(torch, out_table, R, device)
+    if out_table.shape[1] != block_table.shape[1]:
+        raise ValueError("out_table: want rows as long as block_table's")
+    at = [_ints(torch, x, n, what, device) for x, n, what in (
+        (parent, R, "parent"), (length, P, "length"), (free_pages, f, "free_pages"),
+        (out_length, R, "out_length"), (source, R, "source"), (target, R, "target"),
+        (tokens, R, "tokens"), (taken, 1, "taken"))]
+    rc = lib().pp_fork_tables(_FORK_ARGS.pack(
+        R, P, f, block_table.shape[1], page_size, block_table.stride(0), out_table.stride(0),
+        at[0], at[1], rows, at[2], out, *at[3:]), st)
+    if rc:
+        _check(rc)
+
+
+def pp_free_pages(block_table, length, free_pages, count, marks, *, page_size, first=0,
+                  stream=None):
+    """The pages that no row of block_table (int32 [R][blocks]) names in its
+    length[r] tokens, on torch device tensors (see include/prefixplace.h).
+    length int32 [R]; out free_pages int32 [room], count int32 [1]; marks uint8
+    [pages] is scratch, one byte for each page there is."""
+    torch = _torch or _with_torch()
+    device, st = _stream_of(torch, length, stream)
+    R, room = length.shape[0], free_pages.shape[0]
+    rows = _table(torch, block_table, R, device)
+    if marks.dtype != torch.uint8 or marks.dim() != 1 or marks.get_device() != device \
+            or not marks.is_contiguous():
+        _refuse_ints(marks, "marks", torch.uint8, ("pages",))
+    rc = lib().pp_free_pages(_FREE_ARGS.pack(
+        R, block_table.shape[1], page_size, marks.shape[0], first, room, block_table.stride(0),
+        _ints(torch, length, R, "length", device), rows,
+        _ints(torch, free_pages, room, "free_pages", device),
+        _ints(torch, count, 1, "count", device), marks.data_ptr()), st)
     if rc:
         _check(rc)
 

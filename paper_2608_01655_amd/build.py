@@ -45,6 +45,8 @@ def build(verbose: bool = False) -> str:
     objs = []
     for src, device in (("pp_kernels.hip", True), ("pp_reduce.hip", True),
                         ("pp_cache.hip", True), ("pp_attend.hip", True),
+                        ("pp_latent.hip", True), ("pp_rotary.hip", True),
+                        ("pp_pages.hip", True),
                         ("pp_host.cpp", False), ("pp_serve.cpp", False)):
         obj = os.path.join(BUILD_DIR, src + ".o")
         cmd = [cc, f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS, "-c",

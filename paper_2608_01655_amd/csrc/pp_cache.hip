@@ -1,7 +1,7 @@
 // pp_cache.hip -- block tables, slot maps and page writes of the prefix
 // cache (gfx950).
 
-#include "pp_serve.h"
+#include "pp_rows.h"
 
 namespace pp {
 
@@ -284,37 +284,6 @@ __global__ void __launch_bounds__(1024) k_step(pp_block_args a, int shift) {
 
 // ------------------------------------------------------------ page writes ---
 
-typedef __attribute__((__vector_size__(16))) int i32x4;
-typedef __attribute__((__vector_size__(8))) int i32x2;
-
-__device__ __forceinline__ float widen(uint16_t x, bool f16) {
-  if (f16) return (float)__builtin_bit_cast(_Float16, x);
-  return __builtin_bit_cast(float, (uint32_t)x << 16);
-}
-
-// value / scale, held to the type's range; NaN stays NaN.  The quotient is value * (1 / scale) with
-// one correction by its residual, which rounds as the division does for the scales it is used for
-// (2^-60 .. 2^60) wherever the result is not 0; the division itself took 11 instructions an element
-// and bound the kernel.
-struct Scale {
-  float s, inv;
-  bool plain;
-};
-
-__device__ __forceinline__ Scale scale_of(float s) { return {s, 1.f / s, s >= 0x1p-60f && s <= 0x1p60f}; }
-
-__device__ __forceinline__ float shrink(float x, const Scale& c) {
-  float y;
-  if (c.plain) {
-    const float q = x * c.inv;
-    y = __builtin_fmaf(__builtin_fmaf(-q, c.s, x), c.inv, q);
-    y = fabsf(q) > 512.f ? q : y;      // an infinity has no residual
-  } else {
-    y = x / c.s;
-  }
-  return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
-}
-
 // Eight elements of a row a thread, of k and of v.  Bound by what it moves:
 // a row is read and written once, 16 bytes a lane.  65,536 tokens of 8 heads,
 // dim 128 (537 MB) 104 us, 5.2 TB/s, a large copy's rate; 8,191 into 8 bits
@@ -343,13 +312,11 @@ __global__ void __launch_bounds__(256) k_write(pp_kv_pages p, int32_t tokens, bo
     } else {
       auto pack = [&](i32x4 w, const Scale& s) {
         float f[8];
-        for (int j = 0; j < 8; ++j) f[j] = shrink(widen((uint16_t)(w[j / 2] >> (16 * (j % 2))), f16), s);
-        i32x2 o;
-        for (int j = 0; j < 2; ++j) {
-          int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j], f[4 * j + 1], 0, false);
-          o[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j + 2], f[4 * j + 3], q, true);
+        for (int j = 0; j < 8; ++j) {
+          const uint16_t u = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+          f[j] = f16 ? widen1<true>(u) : widen1<false>(u);
         }
-        return o;
+        return narrow8(f, s);
       };
       *(i32x2*)((uint8_t*)p.k + to) = pack(x, scale_of(p.k_scale ? p.k_scale[h] : 1.f));
       *(i32x2*)((uint8_t*)p.v + to) = pack(y, scale_of(p.v_scale ? p.v_scale[h] : 1.f));

@@ -5,6 +5,7 @@
 #include "pp_internal.h"
 #include "pp_serve.h"
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -31,8 +32,9 @@ int64_t size_of(int32_t dtype) { return dtype == PP_E4M3 ? 1 : 2; }
 
 bool row_type(int32_t t) { return t == PP_BF16 || t == PP_F16; }
 
-int check_pages(const pp_kv_pages* p, int32_t dtype) {
-  if (!p || !p->k || !p->v) return report(PP_E_ARG, "null pages");
+// Pages of keys and values, or with `alone` of one kind of rows only; any dim.
+int check_layout(const pp_kv_pages* p, int32_t dtype, bool alone) {
+  if (!p || !p->k || (!p->v && !alone)) return report(PP_E_ARG, "null pages");
   if (!row_type(dtype)) return report(PP_E_ARG, "rows are PP_BF16 or PP_F16");
   if (p->dtype != dtype && p->dtype != PP_E4M3)
     return report(PP_E_ARG, "pages hold the rows' type or PP_E4M3");
@@ -41,11 +43,14 @@ int check_pages(const pp_kv_pages* p, int32_t dtype) {
   if (p->n_pages < 1 || p->heads < 1) return report(PP_E_ARG, "need n_pages >= 1 and heads >= 1");
   if (!pow2_page(p->page_size))
     return report(PP_E_UNSUPPORTED, "page_size is a power of two from 16 to 1,024");
-  if (p->dim != 64 && p->dim != 128 && p->dim != 256)
-    return report(PP_E_UNSUPPORTED, "dim is 64, 128 or 256");
+  return PP_OK;
+}
+
+// Strides of pages whose dim has been checked.
+int check_strides(const pp_kv_pages* p) {
   const int64_t size = size_of(p->dtype);
   if (!row_layout(p->k, size, p->page_stride, p->head_stride, p->token_stride) ||
-      !row_layout(p->v, size, p->page_stride, p->head_stride, p->token_stride))
+      (p->v && !row_layout(p->v, size, p->page_stride, p->head_stride, p->token_stride)))
     return report(PP_E_ARG, "page rows start at 16-byte boundaries, at strides >= 0");
   // kernels keep offsets inside a page in 32 bits
   if (((__int128)(p->heads - 1) * p->head_stride + (__int128)(p->page_size - 1) * p->token_stride +
@@ -54,10 +59,31 @@ int check_pages(const pp_kv_pages* p, int32_t dtype) {
   return PP_OK;
 }
 
-int check_attention(const pp_kv_pages* p, const pp_attention_args* a) {
-  if (!a) return report(PP_E_ARG, "null arguments");
-  const int rc = check_pages(p, a->dtype);
+int check_pages(const pp_kv_pages* p, int32_t dtype) {
+  const int rc = check_layout(p, dtype, false);
   if (rc != PP_OK) return rc;
+  if (p->dim != 64 && p->dim != 128 && p->dim != 256)
+    return report(PP_E_UNSUPPORTED, "dim is 64, 128 or 256");
+  return check_strides(p);
+}
+
+// Rows of `dim` elements in up to three dimensions, one inside the other: no two of them overlap.
+struct Dimension {
+  int64_t count, stride;
+};
+bool nested(int32_t dim, Dimension a, Dimension b, Dimension c = {1, 0}) {
+  Dimension d[3] = {a, b, c};
+  std::sort(d, d + 3, [](const Dimension& x, const Dimension& y) { return x.stride < y.stride; });
+  __int128 extent = dim;
+  for (const Dimension& x : d) {
+    if (x.count < 2) continue;
+    if (x.stride < extent) return false;
+    extent += (__int128)(x.count - 1) * x.stride;
+  }
+  return true;
+}
+
+int check_batch(const pp_kv_pages* p, const pp_attention_args* a) {
   if (a->requests < 0 || a->requests > 65536 || a->tokens < 0 || a->max_new < 0 ||
       a->max_len < 0 || a->max_blocks < 0 || a->window < 0 || a->row_stride < 0)
     return report(PP_E_ARG, "negative size, or more than 65,536 requests");
@@ -68,6 +94,56 @@ int check_attention(const pp_kv_pages* p, const pp_attention_args* a) {
   if ((int64_t)a->max_blocks * p->page_size > INT32_MAX)
     return report(PP_E_UNSUPPORTED, "max_blocks * page_size exceeds 2^31 - 1");
   if (!std::isfinite(a->scale)) return report(PP_E_ARG, "scale is not finite");
+  return PP_OK;
+}
+
+int check_attention(const pp_kv_pages* p, const pp_attention_args* a) {
+  if (!a) return report(PP_E_ARG, "null arguments");
+  const int rc = check_pages(p, a->dtype);
+  return rc != PP_OK ? rc : check_batch(p, a);
+}
+
+int check_latent(const pp_kv_pages* p, int32_t value_dim, const pp_attention_args* a) {
+  if (!a) return report(PP_E_ARG, "null arguments");
+  int rc = check_layout(p, a->dtype, true);
+  if (rc != PP_OK) return rc;
+  if (p->v || p->v_scale) return report(PP_E_ARG, "pages of latent rows have no v");
+  if (p->heads != 1) return report(PP_E_UNSUPPORTED, "pages of latent rows have one head");
+  if ((value_dim != 256 && value_dim != 512) || p->dim != value_dim + 64)
+    return report(PP_E_UNSUPPORTED, "value_dim is 256 or 512, dim 64 more");
+  rc = check_strides(p);
+  return rc != PP_OK ? rc : check_batch(p, a);
+}
+
+// Pointers, rows and workspace of a call that has rows; `out_dim` elements an output row.
+int check_call(const pp_attention_args* a, int32_t out_dim, int64_t need) {
+  if (!a->q || !a->out || !a->query_start || !a->length || (a->max_blocks && !a->block_table))
+    return report(PP_E_ARG, "null pointer");
+  if (!row_layout(a->q, 2, a->q_token_stride, a->q_head_stride) ||
+      !row_layout(a->out, 2, a->out_token_stride, a->out_head_stride))
+    return report(PP_E_ARG, "rows start at 16-byte boundaries, at strides >= 0");
+  if (!apart(a->tokens, a->out_token_stride, out_dim) || !apart(a->q_heads, a->out_head_stride, out_dim))
+    return report(PP_E_ARG, "rows of out overlap");
+  if (need && (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need))
+    return report(PP_E_ARG, "workspace too small or not 256-byte aligned");
+  return PP_OK;
+}
+
+// One kind of rows of pp_rotary_write; `weight` where norm is not 0.
+int check_rotary_rows(int32_t tokens, int32_t heads, int32_t dim, int32_t first, int32_t norm, int32_t rot,
+                      const void* in, int64_t token, int64_t head, const void* out, int64_t out_token,
+                      int64_t out_head, const void* weight, bool to_out) {
+  if (dim < 8 || dim > 1024 || dim % 8 || first < 0 || first % 8 || norm < 0 || norm % 8 || norm > dim ||
+      (int64_t)first + rot > dim)
+    return report(PP_E_UNSUPPORTED, "dims, firsts and norms are multiples of 8 within a dim of 1,024 at most");
+  if (!in || (to_out && !out) || (norm && !weight)) return report(PP_E_ARG, "null pointer");
+  if (!row_layout(in, 2, token, head) || (to_out && !row_layout(out, 2, out_token, out_head)) ||
+      (norm && !aligned16(weight)))
+    return report(PP_E_ARG, "rows and weights start at 16-byte boundaries, at strides >= 0");
+  if (to_out && !nested(dim, {tokens, out_token}, {heads, out_head}))
+    return report(PP_E_ARG, "rows of an output overlap");
+  if (to_out && in == out && (token != out_token || head != out_head))
+    return report(PP_E_ARG, "an output that is its input has its strides");
   return PP_OK;
 }
 
@@ -215,17 +291,175 @@ int pp_paged_attention(const pp_kv_pages* pages, const pp_attention_args* a, voi
   const int rc = check_attention(pages, a);
   if (rc != PP_OK) return rc;
   if (empty(*a)) return PP_OK;
-  if (!a->q || !a->out || !a->query_start || !a->length || (a->max_blocks && !a->block_table))
-    return report(PP_E_ARG, "null pointer");
-  if (!row_layout(a->q, 2, a->q_token_stride, a->q_head_stride) ||
-      !row_layout(a->out, 2, a->out_token_stride, a->out_head_stride))
-    return report(PP_E_ARG, "rows start at 16-byte boundaries, at strides >= 0");
-  if (!apart(a->tokens, a->out_token_stride, pages->dim) || !apart(a->q_heads, a->out_head_stride, pages->dim))
-    return report(PP_E_ARG, "rows of out overlap");
-  const int64_t need = attention_workspace(*pages, *a);
-  if (need && (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need))
-    return report(PP_E_ARG, "workspace too small or not 256-byte aligned");
+  const int bad = check_call(a, pages->dim, attention_workspace(*pages, *a));
+  if (bad != PP_OK) return bad;
   return launched(launch_attention(*pages, *a, (hipStream_t)hip_stream));
+}
+
+int pp_turns(int32_t n, const double* radians, uint64_t* turns) {
+  report(PP_OK, "");
+  if (n < 0 || (n && (!radians || !turns))) return report(PP_E_ARG, "bad arguments to pp_turns");
+  for (int32_t i = 0; i < n; ++i)
+    if (!std::isfinite(radians[i])) return report(PP_E_RANGE, "a frequency is not finite");
+  for (int32_t i = 0; i < n; ++i) {
+    const long double x = (long double)radians[i] / (2 * 3.14159265358979323846264338327950288L);
+    const long double part = x - std::floor(x);       // 0 <= part <= 1, as it is rounded
+    turns[i] = part >= 1 ? 0 : (uint64_t)std::rint(std::ldexp(part, 64));   // below 2^64: 64 bits hold it
+  }
+  return PP_OK;
+}
+
+int pp_rotary_turns(int32_t dim, double base, double factor, double original, double slow, double fast,
+                    double* radians, uint64_t* turns) {
+  report(PP_OK, "");
+  if (dim < 0 || dim % 2) return report(PP_E_ARG, "dim is even");
+  if (!(base > 1) || !(factor >= 1) || !(original >= 0) || !std::isfinite(base) || !std::isfinite(factor) ||
+      !std::isfinite(original) || !(slow >= 0) || !(fast > slow) || !std::isfinite(fast))
+    return report(PP_E_RANGE, "need base > 1, factor >= 1, original >= 0 and fast > slow >= 0");
+  for (int32_t i = 0; i < dim / 2; ++i) {
+    double w = std::pow(base, -2.0 * i / dim);
+    if (factor != 1) {
+      double keep = original > 0 ? (original * w / (2 * M_PI) - slow) / (fast - slow) : 0;
+      keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+      w = keep * w + (1 - keep) * w / factor;
+    }
+    if (radians) radians[i] = w;
+    if (turns) {
+      const int rc = pp_turns(1, &w, turns + i);
+      if (rc != PP_OK) return rc;
+    }
+  }
+  return PP_OK;
+}
+
+int pp_rotary_write(const pp_rotary_args* a, const pp_kv_pages* pages, void* hip_stream) {
+  report(PP_OK, "");
+  if (!a) return report(PP_E_ARG, "null arguments");
+  if (a->tokens < 0 || a->q_heads < 0 || a->k_heads < 0) return report(PP_E_ARG, "negative size");
+  if (!row_type(a->dtype)) return report(PP_E_ARG, "rows are PP_BF16 or PP_F16");
+  if (a->rot_dim < 0 || a->rot_dim % 16 || a->rot_dim > 1024)
+    return report(PP_E_UNSUPPORTED, "rot_dim is a multiple of 16, 1,024 at most");
+  if (!std::isfinite(a->amplitude) || !(a->eps >= 0) || !std::isfinite(a->eps))
+    return report(PP_E_ARG, "amplitude is not finite, or eps not finite and >= 0");
+  if (!a->k_heads && (pages || a->v)) return report(PP_E_ARG, "pages or values without keys");
+  if (a->k_heads && !pages && a->v) return report(PP_E_ARG, "values go to pages only");
+  if (pages) {
+    int rc = check_layout(pages, a->dtype, true);
+    if (rc != PP_OK) return rc;
+    if ((pages->v != nullptr) != (a->v != nullptr)) return report(PP_E_ARG, "values and their pages go together");
+    if (!pages->v && pages->v_scale) return report(PP_E_ARG, "a scale of no values");
+    if (pages->heads != a->k_heads || pages->dim != a->k_dim)
+      return report(PP_E_ARG, "pages have the keys' heads and dim");
+    rc = check_strides(pages);
+    if (rc != PP_OK) return rc;
+    if (!nested(pages->dim, {pages->n_pages, pages->page_stride}, {pages->heads, pages->head_stride},
+                {pages->page_size, pages->token_stride}))
+      return report(PP_E_ARG, "rows of the pages overlap");
+  }
+  if (a->tokens == 0 || (a->q_heads == 0 && a->k_heads == 0)) return PP_OK;
+  if ((int64_t)a->tokens * a->q_heads > INT32_MAX || (int64_t)a->tokens * a->k_heads > INT32_MAX)
+    return report(PP_E_UNSUPPORTED, "tokens * heads exceeds 2^31 - 1");
+  if (a->q_heads) {
+    const int rc = check_rotary_rows(a->tokens, a->q_heads, a->q_dim, a->q_first, a->q_norm, a->rot_dim, a->q,
+                                     a->q_token_stride, a->q_head_stride, a->q_out, a->q_out_token_stride,
+                                     a->q_out_head_stride, a->q_weight, true);
+    if (rc != PP_OK) return rc;
+  }
+  if (a->k_heads) {
+    const int rc = check_rotary_rows(a->tokens, a->k_heads, a->k_dim, a->k_first, a->k_norm, a->rot_dim, a->k,
+                                     a->k_token_stride, a->k_head_stride, a->k_out, a->k_out_token_stride,
+                                     a->k_out_head_stride, a->k_weight, !pages);
+    if (rc != PP_OK) return rc;
+  }
+  if (a->v && !row_layout(a->v, 2, a->v_token_stride, a->v_head_stride))
+    return report(PP_E_ARG, "rows start at 16-byte boundaries, at strides >= 0");
+  if (a->rot_dim && (!a->position || !a->turns || !aligned16(a->turns)))
+    return report(PP_E_ARG, "null position or turns, or turns not 16-byte aligned");
+  if (pages && !a->slot_map) return report(PP_E_ARG, "null pointer");
+  return launched(launch_rotary(*a, pages, (hipStream_t)hip_stream));
+}
+
+int64_t pp_latent_workspace(const pp_kv_pages* pages, int32_t value_dim, const pp_attention_args* args) {
+  report(PP_OK, "");
+  const int rc = check_latent(pages, value_dim, args);
+  if (rc != PP_OK) return rc;
+  return empty(*args) ? 0 : latent_workspace(*pages, value_dim, *args);
+}
+
+int pp_latent_attention(const pp_kv_pages* pages, int32_t value_dim, const pp_attention_args* a,
+                        void* hip_stream) {
+  report(PP_OK, "");
+  const int rc = check_latent(pages, value_dim, a);
+  if (rc != PP_OK) return rc;
+  if (empty(*a)) return PP_OK;
+  if (!nested(value_dim, {a->tokens, a->out_token_stride}, {a->q_heads, a->out_head_stride}))
+    return report(PP_E_ARG, "rows of out overlap");
+  const int bad = check_call(a, value_dim, latent_workspace(*pages, value_dim, *a));
+  if (bad != PP_OK) return bad;
+  return launched(launch_latent(*pages, value_dim, *a, (hipStream_t)hip_stream));
+}
+
+int pp_page_copy(const pp_copy_args* a, void* hip_stream) {
+  report(PP_OK, "");
+  if (!a) return report(PP_E_ARG, "null arguments");
+  if (a->moves < 0 || a->n_pools < 0) return report(PP_E_ARG, "negative size");
+  if (!row_type(a->dtype) && a->dtype != PP_E4M3) return report(PP_E_ARG, "no pages of this type");
+  if (a->n_pages < 1 || a->heads < 1 || a->dim < 1) return report(PP_E_ARG, "need n_pages, heads and dim >= 1");
+  if (!pow2_page(a->page_size)) return report(PP_E_UNSUPPORTED, "page_size is a power of two from 16 to 1,024");
+  const int64_t size = size_of(a->dtype);
+  if (a->dim * size % 16) return report(PP_E_UNSUPPORTED, "rows of pages are multiples of 16 bytes");
+  if ((__int128)a->heads * a->page_size * a->dim * size > (int64_t)1 << 31)
+    return report(PP_E_UNSUPPORTED, "one page has more than 2 GiB");
+  if (a->moves == 0 || a->n_pools == 0) return PP_OK;
+  if (!a->pools || !a->source || !a->target) return report(PP_E_ARG, "null pointer");
+  for (int32_t i = 0; i < a->n_pools; ++i)
+    if (!a->pools[i] || !row_layout(a->pools[i], size, a->page_stride, a->head_stride, a->token_stride))
+      return report(PP_E_ARG, "page rows start at 16-byte boundaries, at strides >= 0");
+  if (!nested(a->dim, {a->n_pages, a->page_stride}, {a->heads, a->head_stride}, {a->page_size, a->token_stride}))
+    return report(PP_E_ARG, "rows of the pages overlap");
+  return launched(launch_page_copy(*a, (hipStream_t)hip_stream));
+}
+
+int pp_fork_tables(const pp_fork_args* a, void* hip_stream) {
+  report(PP_OK, "");
+  if (!a) return report(PP_E_ARG, "null arguments");
+  if (a->rows < 0 || a->rows > 65536 || a->parents < 0 || a->parents > 65536 || a->n_free < 0 ||
+      a->max_blocks < 0 || a->row_stride < 0 || a->out_row_stride < 0)
+    return report(PP_E_ARG, "negative size, or more than 65,536 rows");
+  if (!pow2_page(a->page_size)) return report(PP_E_UNSUPPORTED, "page_size is a power of two from 16 to 1,024");
+  if ((int64_t)a->max_blocks * a->page_size > INT32_MAX)
+    return report(PP_E_UNSUPPORTED, "tokens of a row exceed 2^31 - 1");
+  if (!a->taken || (a->rows && (!a->parent || !a->out_length || !a->source || !a->target || !a->tokens)) ||
+      (a->parents && !a->length) || (a->parents && a->max_blocks && !a->block_table) ||
+      (a->rows && a->max_blocks && !a->out_table) || (a->n_free && !a->free_pages))
+    return report(PP_E_ARG, "null pointer");
+  if (a->rows > 1 && a->out_row_stride < a->max_blocks)
+    return report(PP_E_ARG, "rows of out_table overlap");
+  // the tables from their first entry to their last
+  if (a->rows && a->parents && a->max_blocks) {
+    const uintptr_t in = (uintptr_t)a->block_table, out = (uintptr_t)a->out_table;
+    const uintptr_t in_end = in + 4 * ((uint64_t)(a->parents - 1) * a->row_stride + a->max_blocks);
+    const uintptr_t out_end = out + 4 * ((uint64_t)(a->rows - 1) * a->out_row_stride + a->max_blocks);
+    if (in < out_end && out < in_end) return report(PP_E_ARG, "out_table overlaps block_table");
+  }
+  return launched(launch_fork_tables(*a, (hipStream_t)hip_stream));
+}
+
+int pp_free_pages(const pp_free_args* a, void* hip_stream) {
+  report(PP_OK, "");
+  if (!a) return report(PP_E_ARG, "null arguments");
+  if (a->requests < 0 || a->requests > 65536 || a->max_blocks < 0 || a->n_pages < 0 || a->first < 0 ||
+      a->first > a->n_pages || a->room < 0 || a->row_stride < 0)
+    return report(PP_E_ARG, "negative size, first past n_pages, or more than 65,536 requests");
+  if (a->n_pages > 1 << 24) return report(PP_E_UNSUPPORTED, "more than 16,777,216 pages");
+  if (!pow2_page(a->page_size)) return report(PP_E_UNSUPPORTED, "page_size is a power of two from 16 to 1,024");
+  if ((int64_t)a->max_blocks * a->page_size > INT32_MAX)
+    return report(PP_E_UNSUPPORTED, "tokens of a row exceed 2^31 - 1");
+  if (!a->count || (a->requests && !a->length) || (a->requests && a->max_blocks && !a->block_table) ||
+      (a->room && !a->free_pages) || (a->n_pages && !a->marks))
+    return report(PP_E_ARG, "null pointer");
+  if ((uintptr_t)a->marks & 7) return report(PP_E_ARG, "marks are 8-byte aligned");
+  return launched(launch_free_pages(*a, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -1,6 +1,8 @@
 // pp_serve.h -- shared declarations of the prefix cache's operators: host
 // checks and dispatch (pp_serve.cpp), block tables and page writes
-// (pp_cache.hip), attention (pp_attend.hip).  Not part of the public ABI.
+// (pp_cache.hip), attention (pp_attend.hip, pp_latent.hip), norms and rotary
+// positions (pp_rotary.hip), copies, forks and the free list of pages
+// (pp_pages.hip).  Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -36,6 +38,14 @@ hipError_t launch_block_tables(const pp_block_args& a, hipStream_t st);
 hipError_t launch_kv_write(const pp_kv_pages& p, int32_t tokens, int32_t dtype, const void* k,
                            int64_t kt, int64_t kh, const void* v, int64_t vt, int64_t vh,
                            const int64_t* slot, hipStream_t st);
+
+hipError_t launch_rotary(const pp_rotary_args& a, const pp_kv_pages* pages, hipStream_t st);
+hipError_t launch_page_copy(const pp_copy_args& a, hipStream_t st);
+hipError_t launch_fork_tables(const pp_fork_args& a, hipStream_t st);
+hipError_t launch_free_pages(const pp_free_args& a, hipStream_t st);
+
+int64_t latent_workspace(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a);
+hipError_t launch_latent(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a, hipStream_t st);
 
 int64_t attention_workspace(const pp_kv_pages& p, const pp_attention_args& a);
 hipError_t launch_attention(const pp_kv_pages& p, const pp_attention_args& a, hipStream_t st);
