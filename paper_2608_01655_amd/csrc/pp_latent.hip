@@ -359,6 +359,24 @@ struct LatentTiles : Latent<NARROW, C> {
   static constexpr int kLds = kNB * kTile + 2 * kWeights + 2 * 128 * 4 + 2 * 16;
 };
 
+// x += a b (x = a b where FIRST) with x in vector registers: left alone the compiler keeps what matrix
+// instructions write in accumulation registers, and the accumulators of 128 x 128 values take all 256 of
+// a wave.  It cannot see the instruction's timing either: s_nop 1 covers operands that the vector unit wrote
+// just before, and whoever reads x waits with settle() first.
+template <bool F16, bool FIRST>
+__device__ __forceinline__ void mfma32_vector(f32x16& x, s16x8 a, s16x8 b) {
+  if constexpr (FIRST) {
+    if constexpr (F16) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(x) : "v"(a), "v"(b));
+    else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(a), "v"(b));
+  } else {
+    if constexpr (F16) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(x) : "v"(a), "v"(b));
+    else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(a), "v"(b));
+  }
+}
+
+// 16 passes of the last instruction that wrote x are over after 19 wait states.
+__device__ __forceinline__ void settle(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x)); }
+
 // 128 rows of one request and one part of its keys a block.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
@@ -471,9 +489,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   };
   auto scores = [&](uint32_t at) -> f32x16 {       // of 32 keys
     f32x16 x;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0;
-    each<KS>([&](auto ks) { x = mfma32<F16>(k_frag(at, ks), qf[ks], x); });
+    each<KS>([&](auto ks) { mfma32_vector<F16, ks == 0>(x, k_frag(at, ks), qf[ks]); });
+    settle(x);
     return x;
   };
 
@@ -503,8 +520,12 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     for (int e = 0; e < 4; ++e) {
       if (!__builtin_amdgcn_readfirstlane(any[e])) continue;
       const float al = alphas[b * 128 + e * 32 + l32];
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d][e] *= al;
+      each<DB>([&](auto d) {
+        if constexpr (C == 512) asm volatile("" : "+a"(acc[d][e]));
+        acc[d][e] *= al;
+        if constexpr (C == 512) asm volatile("" : "+a"(acc[d][e]));
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
   };
 
@@ -556,8 +577,6 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     rescale(b);
     s16x8 f[KS], w[8], v[NV];
     f32x16 y;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = 0;
     auto read_v = [&](auto i) { v[i] = v_frag(cur + i / DB * 16 * RB, i % DB); };
     auto read_w = [&](auto i) { w[i] = p_frag(b, i % 4 * 2 + i / 4); };
     each<kAhead>([&](auto i) { f[i] = k_frag(next, i); });
@@ -565,7 +584,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       if constexpr (i + kAhead < KS) f[i + kAhead] = k_frag(next, i + kAhead);
       else read_w(std::integral_constant<int, i + kAhead - KS>());
       if constexpr (i == KS - 2) read_v(std::integral_constant<int, 0>());
-      y = mfma32<F16>(f[i], qf[i], y);
+      mfma32_vector<F16, i == 0>(y, f[i], qf[i]);
       __builtin_amdgcn_sched_barrier(0);
     });
     float mx = -INFINITY, mc = 0, sum = 0, x[16];
@@ -577,10 +596,11 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       if constexpr (DB == 2 && g == 1) read_w(std::integral_constant<int, 4 + e>());
       acc[g % DB][e] = mfma32<F16>(v[g], w[g / DB * 4 + e], acc[g % DB][e]);
       // the next step's weights, a few instructions beside each product
-      constexpr int kMax = NM / 8, kPeak = kMax, kExp = kPeak + 1, kEnd = NM - NM / 8;
-      if constexpr (i < kMax) {
+      constexpr int kWait = 4, kMax = NM / 8, kPeak = kWait + kMax, kExp = kPeak + 1, kEnd = NM - NM / 8;
+      if constexpr (i == kWait - 1) settle(y);
+      if constexpr (i >= kWait && i < kPeak) {
 #pragma unroll
-        for (int j = i * 16 / kMax; j < (i + 1) * 16 / kMax; ++j) mx = fmaxf(mx, y[j]);
+        for (int j = (i - kWait) * 16 / kMax; j < (i - kWait + 1) * 16 / kMax; ++j) mx = fmaxf(mx, y[j]);
         asm volatile("" : "+v"(mx));
       }
       if constexpr (i == kPeak) {
