@@ -752,6 +752,85 @@ k_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
   }
 }
 
+// ---------------------------------------------------------------- k_join ---
+
+// Rows of requests in several parts: a wave takes 256 / D of them, four values a lane.  Bound by the
+// chain of its loads, so eight parts are read at a time, their log sums with them.
+// few_rows: a wave's rows are some of few_rows rows of one of the key heads of a request of k_rows
+// (where no request of k_tiles is in parts); 0: they are heads of one of the call's tokens.
+template <bool F16, int D>
+__global__ void __launch_bounds__(256) k_join(pp_attention_args a, Plan pl, int32_t few_rows, int32_t heads) {
+  constexpr int kRows = 256 / D, kTurn = 8;
+  const int lane = threadIdx.x % kWave, sub = lane / (D / 4), d = lane % (D / 4) * 4;
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  int32_t t, g, r, row, h;
+  Request q;
+  bool live, few;
+  if (few_rows) {
+    const int32_t each = (few_rows + kRows - 1) / kRows;
+    if (id / each / heads >= a.requests) return;
+    r = (int32_t)(id / each / heads);
+    row = (int32_t)(id % each) * kRows + sub;
+    h = (int32_t)(id / each % heads);
+    q = request(a, pl, r);
+    const int64_t rows = (int64_t)q.count * pl.group;
+    if (rows > pl.few) return;
+    few = true;
+    live = row < few_rows && row < rows;
+    t = q.first + row / pl.group;
+    g = h * pl.group + row % pl.group;
+  } else {
+    const int32_t each = (a.q_heads + kRows - 1) / kRows;
+    if (id / each >= a.tokens) return;
+    t = (int32_t)(id / each);
+    g = (int32_t)(id % each) * kRows + sub;
+    live = g < a.q_heads;
+    r = find_last(a.requests, t, [&](int32_t i) { return a.query_start[i]; });
+    if (r < 0) return;
+    q = request(a, pl, r);
+    if (t < q.first || t >= q.first + q.count) return;
+    few = (int64_t)q.count * pl.group <= pl.few;
+    row = few ? (t - q.first) * pl.group + g % pl.group : 0;
+    h = g / pl.group;
+  }
+  const int32_t parts = few ? parts_of(q, pl.cut_rows, pl.parts_rows) : parts_of(q, pl.cut_tiles, pl.parts_tiles);
+  if (parts == 1 || !live) return;
+  const int64_t at = (int64_t)t * a.q_heads + g;
+  const int64_t own = few ? ((int64_t)r * heads + h) * pl.few + row : at;
+  const int64_t step = few ? (int64_t)a.requests * heads * pl.few : (int64_t)a.tokens * a.q_heads;
+  const float* from = (few ? pl.row_part : pl.part) + own * D + d;
+  const float* sums = (few ? pl.row_lse : pl.part_lse) + own;
+  float m = -INFINITY, sum = 0;
+  f32x4 o = {0, 0, 0, 0};
+  for (int32_t base = 0; base < parts; base += kTurn) {
+    float x[kTurn];
+    f32x4 y[kTurn];
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      const int32_t i = base + j < parts ? base + j : parts - 1;
+      x[j] = sums[i * step];
+      y[j] = *(const f32x4*)(from + i * step * D);
+    }
+    float n = m;
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) n = fmaxf(n, x[j]);
+    const float al = m == -INFINITY ? 0.f : exp2_(m - n);
+    o *= al;
+    sum *= al;
+    m = n;
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      if (base + j >= parts || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
+      const float w = x[j] == n ? 1.f : exp2_(x[j] - n);
+      sum += w;
+      o += w * y[j];
+    }
+  }
+  o *= sum == 0 ? 0.f : 1.f / sum;
+  store4<F16>(a, t, g, d, o);
+  if (a.lse && d == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
+}
+
 // -------------------------------------------------------------- dispatch ---
 
 // Blocks of k_tiles that the rule below counts on at a time.  At dim 256 its registers leave room for

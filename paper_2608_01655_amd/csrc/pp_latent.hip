@@ -18,6 +18,27 @@ namespace pp {
 
 namespace {
 
+constexpr int kFew = 16;             // rows k_latent_rows takes
+constexpr int kRowsStart = 4;        // what a request's start and end cost it, in stages, and the least a block takes
+constexpr int kRowsShare = 8;
+constexpr int kTilesStart = 8;       // the same of k_latent_tiles, in steps of 32 keys
+constexpr int kTilesShare = 12;
+constexpr int kBlocks = 256;         // resident ones: one a CU
+constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into equal shares, and requests
+
+// Rows that begin in a block and go on in the next ones up to `last`: `rows` of them from row `row` on of the request whose
+// tokens begin at `first` (rows 0: none).
+struct Cut {
+  int32_t last, first, row, rows;
+};
+
+// A call's plan, and its parts in the workspace: [2 kBlocks][rows][C], their log sums, and each block's cut.
+struct Split : Plan {
+  int32_t even;                      // k_latent_tiles cuts its slots
+  float *slot_part, *slot_lse;
+  Cut *row_cut, *slot_cut;
+};
+
 // Rows in LDS: the 16-byte unit u of a row lies at u ^ swizzle(row).  A row is 4.5 (16 bits, latent 512),
 // 2.5 (256) or half of that many times 256 bytes, so neighbouring rows are already 128 (64) bytes apart in the
 // banks, and the swizzle parts the rows that the transposing reads take together.
@@ -40,17 +61,52 @@ struct Latent {
   }
 };
 
-// What a row does not see does not touch it, whatever it holds.  In tiles that some row does not see
-// whole, elements that are not finite go into the product as 0.  A row that sees one has a score of NaN or
-// +infinity from it, and is NaN whole by its sum, or of -infinity, and then that element's weight of 0 times an
-// infinity makes it NaN: so the row's element is set to NaN.
-template <bool F16>
-__device__ __forceinline__ s16x8 odd_ones(s16x8 v) {      // 1 where v is not finite
-  s16x8 o;
-  const uint16_t top = F16 ? 0x7c00 : 0x7f80;
+// What a row does not see does not touch it, whatever it holds.  In tiles that some row does not see whole, elements
+// that are not finite are set to 0 in LDS between the scores and the values.  A row that sees one has a score of
+// NaN or +infinity from it, and is NaN whole by its sum, or of -infinity, and then that element's weight of 0
+// times an infinity makes it NaN: so mark_odd sets the row's element to NaN once it is stored.
+template <bool F16, bool NARROW>
+__device__ __forceinline__ bool clean16(uint32_t at) {
+  u32x4 x = *LDS_PTR(u32x4, at);
+  uint32_t any = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = ((uint16_t)v[j] & top) == top ? (short)(F16 ? 0x3c00 : 0x3f80) : (short)0;
-  return o;
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (NARROW) {
+      const uint32_t n = ((x[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      any |= n;
+      x[j] &= ~((n >> 7) * 0xffu);
+    } else {
+      const uint32_t n = not_finite<F16>(x[j]);
+      any |= n;
+      x[j] &= ~((n >> 15) * 0xffffu);
+    }
+  }
+  if (any) *LDS_PTR(u32x4, at) = x;
+  return any != 0;
+}
+
+// Rows row0 .. row0 + count - 1 of request r, keys k0 .. k1 - 1; sums: the rows' sums, 0 where nothing is seen.
+// `put` sets a row's element d to NaN.  All threads of the block, behind the rows' stores.
+template <bool F16, bool NARROW, int C, class Put>
+__device__ __forceinline__ void mark_odd(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, int32_t r, int32_t start,
+                                         int32_t row0, int32_t count, int32_t k0, int32_t k1, const float* sums, Put&& put) {
+  const int32_t* blocks = a.block_table + r * a.row_stride;
+  const int64_t es = NARROW ? 1 : 2;
+#pragma unroll 1
+  for (int32_t key = k0; key < k1; ++key) {
+    const char* from = (const char*)p.k + page_of(p, a, pl, blocks, key) * p.page_stride * es +
+                       (int64_t)(key & (p.page_size - 1)) * p.token_stride * es;
+#pragma unroll 1
+    for (int32_t d = threadIdx.x; d < C; d += 256) {
+      uint32_t y;
+      if constexpr (NARROW) y = (((const uint8_t*)from)[d] & 0x7f) == 0x7f;
+      else y = not_finite<F16>(((const uint16_t*)from)[d]) & 0x8000u;
+      if (!y) continue;
+#pragma unroll 1
+      for (int32_t i = 0; i < count; ++i)
+        if (sees(start + (row0 + i) / pl.group, key, a.window) && sums[i] != 0) put(i, d);
+    }
+  }
 }
 
 // -------------------------------------------------------- k_latent_rows ---
@@ -62,7 +118,7 @@ struct LatentRows : Latent<NARROW, C> {
   static constexpr int kNS = C == 512 ? 2 : 3;              // stages of a wave's ring
   static constexpr int kRing = kNW * kNS * L::kStage;
   static constexpr int kRow = C + 4;                        // floats of a joined row
-  static constexpr int kJoin = kNW * 16 * (kRow + 2) * 4;
+  static constexpr int kJoin = kNW * 16 * (kRow + 3) * 4;
   static constexpr int kLds = kRing > kJoin ? kRing : kJoin;
 };
 
@@ -75,51 +131,109 @@ __device__ __forceinline__ f32x4 mfma16x16(s16x4 a, s16x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
 
-template <bool F16, bool NARROW, int C, int RT>
-__global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attention_args a, Plan pl) {
+// A value that all lanes have, where the compiler cannot know it.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// Sums over the 256 threads of a block: before this one, and of all.
+__device__ __forceinline__ int64_t before(int64_t x, int64_t& all, int64_t* sums) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int64_t up = x;
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t y = __shfl_up(up, o);
+    if (lane >= o) up += y;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) sums[wave] = up;
+  __syncthreads();
+  int64_t base = 0;
+  all = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) base += sums[w];
+    all += sums[w];
+  }
+  return base + up - x;
+}
+
+// All blocks together take the tiles of all items in order, `share` of the items' costs each.  An item at `at`
+// in the row of costs has `start` for its start and end and then its tiles; block b has tiles from .. to - 1 of
+// them (an item without tiles is whole in the block where it begins).  An item in several blocks leaves parts:
+// that of its first block b is number 2 b + 1, the others 2 b, and a block has one of either at most.
+struct Piece {
+  int32_t from, to;
+  bool here, first, last;
+};
+
+__device__ __forceinline__ Piece piece_of(int64_t at, int32_t start, int32_t tiles, int64_t share, int32_t b) {
+  const int64_t lo = b * share - at - (tiles ? start : 0), hi = lo + share;
+  Piece x;
+  x.from = (int32_t)(lo > 0 ? lo : 0);
+  x.to = (int32_t)(hi < tiles ? hi : tiles);
+  x.first = lo <= 0;
+  x.last = hi >= tiles;
+  x.here = tiles ? x.from < x.to : lo <= 0 && hi > 0;
+  return x;
+}
+
+// Requests of up to 16 rows.  All blocks together take the tiles of all requests in order, an equal share
+// each, whatever the lengths: a block's share is of one request or of several.  Each wave has a ring of its own and
+// keeps a stage in flight while it works on another, without a barrier.
+template <bool F16, bool NARROW, int C>
+__global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attention_args a, Split pl) {
   using Sh = LatentRows<NARROW, C>;
   constexpr int RB = Sh::kRB, NW = Sh::kNW, NS = Sh::kNS, KEYS = Sh::kKeys, KB = KEYS / 16;
   constexpr int DB = C / 16, KS = Sh::kKS16;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int part = blockIdx.x % pl.parts_rows;
-  const int32_t r = blockIdx.x / pl.parts_rows;
-  const Request q = request(a, pl, r);
-  const int G = pl.group;
-  const int64_t rows64 = (int64_t)q.count * G;
-  if (rows64 == 0 || rows64 > pl.few) return;
-  const int32_t rows = (int32_t)rows64;
-  const int32_t parts = parts_of(q, pl.cut_rows, pl.parts_rows);
-  if (part >= parts) return;
-  int64_t k0 = q.lo + (int64_t)part * pl.cut_rows;
-  int64_t k1 = part + 1 < parts ? k0 + pl.cut_rows : q.hi;
-  if (k1 > q.hi) k1 = q.hi;
-  const int32_t tiles = k1 > k0 ? (int32_t)((k1 - k0 + KEYS - 1) / KEYS) : 0;
-  const int32_t share = (tiles + NW - 1) / NW;
-  const int32_t t0 = wave * share < tiles ? wave * share : tiles;
-  const int32_t nt = t0 + share < tiles ? share : tiles - t0;
-  const int32_t kbase = (int32_t)k0 + t0 * KEYS;
-  const int grp = lane / 16, i16 = lane % 16;
+  const int grp = lane / 16, i16 = lane % 16, G = pl.group;
+  if (threadIdx.x == 0) pl.row_cut[blockIdx.x].rows = 0;
 
-  // this lane's row of each tile of rows: its token's position, or -1
-  int32_t pos[RT];
-  s16x8 qf[RT][KS];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int32_t row = rt * 16 + i16;
-    const int32_t tok = row / G, g = row % G;
-    pos[rt] = row < rows ? q.start + tok : -1;
-    const uint16_t* src = (const uint16_t*)a.q + (q.first + (row < rows ? tok : 0)) * a.q_token_stride +
-                          (row < rows ? g : 0) * a.q_head_stride + grp * 8;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      i32x4 x = *(const i32x4*)(src + ks * 32);
-      if (pl.negative) x ^= (int)0x80008000;
-      qf[rt][ks] = __builtin_bit_cast(s16x8, x);
+  // what a request costs: its tiles and its start and end, nothing where it is not this kernel's
+  struct Item {
+    Request q;
+    int32_t rows, tiles, cost;
+  };
+  auto item = [&](int32_t r) -> Item {
+    Item x;
+    x.q = request(a, pl, r);
+    const int64_t rows = (int64_t)x.q.count * G;
+    x.rows = rows <= kFew ? (int32_t)rows : 0;
+    x.tiles = x.q.hi > x.q.lo ? (int32_t)(((int64_t)x.q.hi - x.q.lo + KEYS - 1) / KEYS) : 0;
+    x.cost = x.rows ? x.tiles + kRowsStart : 0;
+    return x;
+  };
+  int64_t share, at;
+  int32_t r;
+  {
+    // thread i has requests i * each .. of them; the one whose costs hold the block's first looks it up
+    int64_t* const sums = (int64_t*)g_lds;               // [4], then the block's first request and its place
+    const int32_t each = (a.requests + 255) / 256, r0 = threadIdx.x * each;
+    const int32_t r1 = r0 + each < a.requests ? r0 + each : a.requests;
+    int64_t mine = 0, all;
+    for (int32_t i = r0; i < r1; ++i) mine += item(i).cost;
+    int64_t from = before(mine, all, sums);
+    share = uniform((all + gridDim.x - 1) / gridDim.x);
+    if (share < kRowsShare) share = kRowsShare;
+    const int64_t x0 = blockIdx.x * share;
+    if (x0 >= all) return;
+    if (from <= x0 && x0 < from + mine) {
+      int32_t i = r0;
+      for (;; ++i) {
+        const int32_t cost = item(i).cost;
+        if (x0 < from + cost) break;
+        from += cost;
+      }
+      sums[4] = i;
+      sums[5] = from;
     }
+    __syncthreads();
+    r = __builtin_amdgcn_readfirstlane((int32_t)sums[4]);
+    at = uniform(sums[5]);
   }
+
   const float vs = NARROW && p.k_scale ? p.k_scale[0] : 1.f;
   const float c = pl.c * vs;
-
   const int64_t es = NARROW ? 1 : 2;
   const int64_t page_b = p.page_stride * es;
   const uint32_t tok_b = (uint32_t)(p.token_stride * es);
@@ -128,29 +242,6 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
   uint32_t off[Sh::kHalf];
 #pragma unroll
   for (int i = 0; i < Sh::kHalf; ++i) off[i] = Sh::source(i, lane, tok_b);
-  const int32_t* blocks = a.block_table + r * a.row_stride;
-  int32_t held = 0;
-  auto issue = [&](int32_t t) {
-    const uint32_t to = __builtin_amdgcn_readfirstlane(ring + (t % NS) * Sh::kStage);
-    if ((t * KB & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + ((int64_t)t * KB + lane) * 16);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int32_t key = kbase + t * KEYS + half * (KEYS / 2);
-      const int64_t page = __builtin_amdgcn_readlane(held, (t * KB + (KB - 1) * half) & 63);
-      const char* from = rows_at + page * page_b + (int64_t)(key & (p.page_size - 1)) * tok_b;
-      each<Sh::kHalf>([&](auto i) { load_lds(to + (half * Sh::kHalf + i) * 1024, off[i], from); });
-    }
-  };
-
-  f32x4 acc[RT][DB];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = -INFINITY;
-    l[rt] = 0;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) acc[rt][d] = f32x4{0, 0, 0, 0};
-  }
   // reads along a row: row i16, its units grp + 4 ks (16 bits) or grp / 2 + 2 ks; transposed ones: four
   // keys a 16-lane group, or eight.  The swizzle meets the steps' low bits only, the rest are offsets.
   const uint32_t kx = NARROW ? ((grp / 2) ^ Sh::swizzle(i16)) * 16 + (grp % 2) * 8 : (grp ^ Sh::swizzle(i16)) * 16;
@@ -162,188 +253,208 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
   for (int i = 0; i < 2; ++i) k_at[i] = i16 * RB + (kx ^ (i * (NARROW ? 32 : 64)));
 #pragma unroll
   for (int i = 0; i < 4; ++i) v_at[i] = vrow * RB + (vx ^ (i * (NARROW ? 16 : 32)));
-  const int32_t pos_lo = q.start;   // the first row's; rows of -1 see nothing in any case
-  const int32_t pos_hi = q.start + q.count - 1;
 
-  auto tile = [&](int32_t t, auto masked) {
-    constexpr bool kMasked = decltype(masked)::value;   // some row does not see all of it
-    if (t + NS - 1 < nt) {
-      issue(t + NS - 1);
-      wait_loads<(NS - 1) * Sh::kLoads>();
-    } else if (NS > 2 && t + NS - 2 < nt) {
-      wait_loads<(NS > 2 ? NS - 2 : 0) * Sh::kLoads>();
-    } else {
-      wait_loads<0>();
-    }
-    const uint32_t at = ring + (t % NS) * Sh::kStage;
-    f32x4 s[RT][KB];
+#pragma unroll 1
+  for (; r < a.requests && at < (blockIdx.x + 1) * share; ++r) {
+    const Item x = item(r);
+    const Request q = x.q;
+    const int32_t rows = x.rows;
+    const int64_t place = at;
+    at += x.cost;
+    const int32_t b = blockIdx.x;
+    const Piece piece = piece_of(place, kRowsStart, x.tiles, share, b);
+    if (!rows || !piece.here) continue;
+    const bool parts = !piece.first || !piece.last;
+    const int64_t to = 2 * b + piece.first;
+    if (piece.first && parts && threadIdx.x == 0)
+      pl.row_cut[b] = {(int32_t)((place + x.cost - 1) / share), q.first, 0, rows};
+    const int32_t k0 = q.lo + piece.from * KEYS;
+    const int64_t end = (int64_t)q.lo + (int64_t)piece.to * KEYS;
+    const int32_t k1 = end < q.hi ? (int32_t)end : q.hi;
+    const int32_t tiles = piece.to - piece.from;
+    const int32_t share_w = (tiles + NW - 1) / NW;
+    const int32_t t0 = wave * share_w < tiles ? wave * share_w : tiles;
+    const int32_t nt = t0 + share_w < tiles ? share_w : tiles - t0;
+    const int32_t kbase = k0 + t0 * KEYS;
+    const int32_t* blocks = a.block_table + r * a.row_stride;
+    int32_t held = 0;
+    auto issue = [&](int32_t t) {
+      const uint32_t into = __builtin_amdgcn_readfirstlane(ring + (t % NS) * Sh::kStage);
+      if ((t * KB & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + ((int64_t)t * KB + lane) * 16);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt][kb] = f32x4{0, 0, 0, 0};
+      for (int half = 0; half < 2; ++half) {
+        const int32_t key = kbase + t * KEYS + half * (KEYS / 2);
+        const int64_t page = __builtin_amdgcn_readlane(held, (t * KB + (KB - 1) * half) & 63);
+        const char* from = rows_at + page * page_b + (int64_t)(key & (p.page_size - 1)) * tok_b;
+        each<Sh::kHalf>([&](auto i) { load_lds(into + (half * Sh::kHalf + i) * 1024, off[i], from); });
+      }
+    };
+    __syncthreads();                  // the ring was the last piece's join
+    for (int32_t t = 0; t < NS - 1 && t < nt; ++t) issue(t);
+
+    // this lane's row: its token's position, or -1
+    const bool live = i16 < rows;
+    const int32_t pos = live ? q.start + i16 / G : -1;
+    s16x8 qf[KS];
+    {
+      const uint16_t* src = (const uint16_t*)a.q + (q.first + (live ? i16 / G : 0)) * a.q_token_stride +
+                            (live ? i16 % G : 0) * a.q_head_stride + grp * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s16x8 f;
-        const uint32_t from = at + kb * 16 * RB + k_at[ks % 2] + ks / 2 * (NARROW ? 64 : 128);
-        if constexpr (NARROW) f = widen8<F16>(*LDS_PTR(i32x2, from));
-        else f = *LDS_PTR(s16x8, from);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][kb] = mfma16<F16>(f, qf[rt][ks], s[rt][kb]);
+        i32x4 y = *(const i32x4*)(src + ks * 32);
+        if (pl.negative) y ^= (int)0x80008000;
+        qf[ks] = __builtin_bit_cast(s16x8, y);
       }
     }
-    const int32_t key0 = kbase + t * KEYS + 4 * grp;   // of s[.][0][0]; + 16 kb + i
-    s16x8 pf[RT];                                      // of 16 keys: its first half
-    uint32_t seen[RT];
+    f32x4 acc[DB];
+    float m = -INFINITY, l = 0;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float x[4 * KB], w[8];
-      seen[rt] = 0xff;
+    for (int d = 0; d < DB; ++d) acc[d] = f32x4{0, 0, 0, 0};
+    const int32_t pos_lo = q.start;   // the first row's; rows of -1 see nothing in any case
+    const int32_t pos_hi = q.start + q.count - 1;
+
+    const Span3 sp = spans<KEYS>(kbase, nt, pos_lo, pos_hi, k1, a.window);
+    bool odd = false;
+    // One body for all tiles: a launch runs through little more than this once, and fetching code took
+    // longer than its products (with a body each for tiles seen whole and in part a lone short request
+    // took 16 us).
+#pragma unroll 1
+    for (int32_t t = 0; t < nt; ++t) {
+      const bool masked = t < sp.whole || t >= sp.tail;   // some row does not see all of it
+      if (t + NS - 1 < nt) {
+        issue(t + NS - 1);
+        wait_loads<(NS - 1) * Sh::kLoads>();
+      } else if (NS > 2 && t + NS - 2 < nt) {
+        wait_loads<(NS > 2 ? NS - 2 : 0) * Sh::kLoads>();
+      } else {
+        wait_loads<0>();
+      }
+      const uint32_t in = ring + (t % NS) * Sh::kStage;
+      f32x4 s[KB];
 #pragma unroll
-      for (int j = 0; j < 4 * KB; ++j) x[j] = s[rt][j / 4][j % 4];
-      if constexpr (kMasked) {
-        seen[rt] = 0;
+      for (int kb = 0; kb < KB; ++kb) {
+        s[kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          s16x8 f;
+          const uint32_t from = in + kb * 16 * RB + k_at[ks % 2] + ks / 2 * (NARROW ? 64 : 128);
+          if constexpr (NARROW) f = widen8<F16>(*LDS_PTR(i32x2, from));
+          else f = *LDS_PTR(s16x8, from);
+          s[kb] = mfma16<F16>(f, qf[ks], s[kb]);
+        }
+      }
+      float y[4 * KB], w[8];
+#pragma unroll
+      for (int j = 0; j < 4 * KB; ++j) y[j] = s[j / 4][j % 4];
+      if (masked) {
+        const int32_t key0 = kbase + t * KEYS + 4 * grp;   // of s[0][0]; + 16 kb + i
 #pragma unroll
         for (int j = 0; j < 4 * KB; ++j) {
           const int32_t key = key0 + (j / 4) * 16 + j % 4;
-          const bool ok = sees(pos[rt], key, a.window) && key < k1;
-          seen[rt] |= ok ? 1u << j : 0;
-          if (!ok) x[j] = -INFINITY;
+          if (!(sees(pos, key, a.window) && key < k1)) y[j] = -INFINITY;
         }
+        wait_lds();
+#pragma unroll 1
+        for (int i = lane; i < KEYS * (C * (int)es / 16); i += kWave)
+          odd |= clean16<F16, NARROW>(in + i / (C * (int)es / 16) * RB + i % (C * (int)es / 16) * 16);
+        wait_lds();
       }
-      float mx = x[0];
+      float mx = y[0];
 #pragma unroll
-      for (int j = 1; j < 4 * KB; ++j) mx = fmaxf(mx, x[j]);
+      for (int j = 1; j < 4 * KB; ++j) mx = fmaxf(mx, y[j]);
       mx = over_halves(over_rows(mx, Max()), Max());
-      const bool grow = mx > m[rt] && (m[rt] == -INFINITY || (mx - m[rt]) * c > kLag<F16>);
+      const bool grow = mx > m && (m == -INFINITY || (mx - m) * c > kLag<F16>);
       if (__any(grow)) {
-        const float n = fmaxf(m[rt], mx);
-        const float al = m[rt] == -INFINITY ? 0.f : exp2_((m[rt] - n) * c);
-        l[rt] *= al;
+        const float n = fmaxf(m, mx);
+        const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
+        l *= al;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) acc[rt][d] *= al;
-        m[rt] = n;
+        for (int d = 0; d < DB; ++d) acc[d] *= al;
+        m = n;
       }
-      const float mc = top_of<F16>(m[rt], c);
+      const float mc = top_of<F16>(m, c);
       float sum = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        w[j] = 0;
-        if (j >= 4 * KB) continue;
-        w[j] = exp2_(__builtin_fmaf(x[j], c, -mc));
-        if (kMasked && !(seen[rt] >> j & 1)) w[j] = 0;
+        w[j] = j < 4 * KB ? exp2_(__builtin_fmaf(y[j < 4 * KB ? j : 0], c, -mc)) : 0.f;
         sum += w[j];
       }
-      l[rt] += sum;
-      pf[rt] = pack8<F16>(w);
-    }
-    // the values of 32 (16 bits: two blocks of 16) elements of the latent
-    auto v_frag = [&](int db) -> s16x8 {
-      if constexpr (NARROW) {
-        return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            LDS_PTR(i32x2, at + v_at[db % 4] + db / 4 * 64))));
-      } else {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + v_at[2 * db % 4] + 2 * db / 4 * 128));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + v_at[(2 * db + 1) % 4] + 2 * db / 4 * 128));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    };
-    constexpr int kPer = NARROW ? 1 : 2, NB = DB / kPer;
-    auto product = [&](s16x8 v, s16x8 w, f32x4* o) {
-      if constexpr (NARROW) {
-        o[0] = mfma16<F16>(v, w, o[0]);
-      } else {
-        const s16x4 lo = __builtin_shufflevector(w, w, 0, 1, 2, 3);
-        o[0] = mfma16x16<F16>(__builtin_shufflevector(v, v, 0, 1, 2, 3), lo, o[0]);
-        o[1] = mfma16x16<F16>(__builtin_shufflevector(v, v, 4, 5, 6, 7), lo, o[1]);
-      }
-    };
-    if constexpr (!kMasked) {
+      l += sum;
+      const s16x8 pf = pack8<F16>(w);                    // of 16 keys: its first half
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const s16x8 f = v_frag(b);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) product(f, pf[rt], &acc[rt][b * kPer]);
-      }
-    } else {
-      uint32_t odd = 0;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const s16x8 f = only_finite<F16>(v_frag(b), odd);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) product(f, pf[rt], &acc[rt][b * kPer]);
-      }
-      if (__any(odd != 0)) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const s16x8 f = odd_ones<F16>(v_frag(b));
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            f32x4 n[kPer];
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) n[e] = f32x4{0, 0, 0, 0};
-            product(f, ones8<F16>(seen[rt]), n);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[rt][b * kPer + e][i] = n[e][i] != 0 ? __builtin_nanf("") : acc[rt][b * kPer + e][i];
-          }
+      for (int db = 0; db < DB; ++db) {
+        if constexpr (NARROW) {
+          acc[db] = mfma16<F16>(widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                    LDS_PTR(i32x2, in + v_at[db % 4] + db / 4 * 64)))), pf, acc[db]);
+        } else {
+          acc[db] = mfma16x16<F16>(__builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, in + v_at[db % 4] + db / 4 * 128)),
+                                   __builtin_shufflevector(pf, pf, 0, 1, 2, 3), acc[db]);
         }
       }
+      wait_lds();   // this stage's reads are done before its next load is issued
     }
-    wait_lds();   // this stage's reads are done before its next load is issued
-  };
-  const Span3 sp = spans<KEYS>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
-  for (int32_t t = 0; t < NS - 1 && t < nt; ++t) issue(t);
-  int32_t t = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (const int32_t e = pass ? nt : sp.whole; t < e; ++t) tile(t, std::true_type());
-    if (pass == 0)
-      for (; t < sp.tail; ++t) tile(t, std::false_type());
-  }
 
-  // the waves' parts of 16 rows at a time are joined in LDS
-  float* js = (float*)g_lds;                       // [NW][16][kRow]
-  float* jm = js + NW * 16 * Sh::kRow;             // [NW][16]
-  float* jl = jm + NW * 16;
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    __syncthreads();
-    const float ls = over_halves(over_rows(l[rt], Sum()), Sum());
+    // the waves' parts of the rows are joined in LDS
+    float* js = (float*)g_lds;                       // [NW][16][kRow]
+    float* jm = js + NW * 16 * Sh::kRow;             // [NW][16]
+    float* jl = jm + NW * 16;
+    const int any_odd = __syncthreads_or(odd);
+    const float ls = over_halves(over_rows(l, Sum()), Sum());
     if (grp == 0) {
-      jm[wave * 16 + i16] = m[rt];
+      jm[wave * 16 + i16] = m;
       jl[wave * 16 + i16] = ls;
     }
 #pragma unroll
-    for (int db = 0; db < DB; ++db) *(f32x4*)&js[(wave * 16 + i16) * Sh::kRow + db * 16 + grp * 4] = acc[rt][db];
+    for (int db = 0; db < DB; ++db) *(f32x4*)&js[(wave * 16 + i16) * Sh::kRow + db * 16 + grp * 4] = acc[db];
     __syncthreads();
-    const int left = rows - rt * 16 < 16 ? rows - rt * 16 : 16;
-    for (int i = threadIdx.x; i < left * (C / 4); i += NW * kWave) {
-      const int row = i / (C / 4), d = i % (C / 4) * 4;
+    // a factor for each wave's part of each row, 0 where it saw nothing
+    float* const jf = jl + NW * 16;                  // [16][NW]
+    if (threadIdx.x < NW * 16) {
+      const int w = threadIdx.x / 16, row = i16;
       float mm = -INFINITY, ll = 0;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, jm[w * 16 + row]);
+      for (int v = 0; v < NW; ++v) mm = fmaxf(mm, jm[v * 16 + row]);
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float mv = jm[v * 16 + row], lv = jl[v * 16 + row];
+        if (lv != 0) ll += (mv == mm ? 1.f : exp2_((mv - mm) * c)) * lv;
+      }
+      const float mw = jm[w * 16 + row];
+      jf[row * NW + w] = jl[w * 16 + row] == 0 ? 0.f : (mw == mm ? 1.f : exp2_((mw - mm) * c)) * (vs / ll);
+      if (w == 0 && row < rows) {
+        const float lse = ll == 0 ? -INFINITY : mm * c + (__log2f(ll) - kLift<F16>);
+        if (parts) pl.row_lse[to * kFew + row] = lse;
+        else if (a.lse) a.lse[(int64_t)(q.first + row / G) * a.q_heads + row % G] = lse / kLog2e;
+      }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rows * (C / 4); i += NW * kWave) {
+      const int row = i / (C / 4), d = i % (C / 4) * 4;
+      const f32x4 f = *(const f32x4*)&jf[row * NW];
       f32x4 o = {0, 0, 0, 0};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float mw = jm[w * 16 + row], lw = jl[w * 16 + row];
-        if (lw == 0) continue;      // it saw nothing
-        const float f = mw == mm ? 1.f : exp2_((mw - mm) * c);
-        ll += f * lw;
-        o += f * *(const f32x4*)&js[(w * 16 + row) * Sh::kRow + d];
+        // a wave that saw nothing may hold anything
+        const f32x4 y = *(const f32x4*)&js[(w * 16 + row) * Sh::kRow + d];
+        o += f[w] == 0 ? f32x4{0, 0, 0, 0} : f[w] * y;
       }
-      const float inv = ll == 0 ? 0.f : vs / ll;
-      o *= inv;
-      const float lse = ll == 0 ? -INFINITY : mm * c + (__log2f(ll) - kLift<F16>);
-      const int32_t tk = q.first + (rt * 16 + row) / G, g = (rt * 16 + row) % G;
-      if (parts == 1) {
-        store4<F16>(a, tk, g, d, o);
-        if (a.lse && d == 0) a.lse[(int64_t)tk * a.q_heads + g] = lse / kLog2e;
-      } else {
-        const int64_t to = ((int64_t)part * a.requests + r) * pl.few + rt * 16 + row;
-        *(f32x4*)&pl.row_part[to * C + d] = o;
-        if (d == 0) pl.row_lse[to] = lse;
-      }
+      if (parts) *(f32x4*)&pl.row_part[(to * kFew + row) * C + d] = o;
+      else store4<F16>(a, q.first + row / G, row % G, d, o);
     }
+    if (!any_odd) continue;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+      float sum = 0;
+      for (int w = 0; w < NW; ++w) sum += jl[w * 16 + threadIdx.x];
+      js[threadIdx.x] = sum;
+    }
+    __threadfence_block();
+    __syncthreads();
+    mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, 0, rows, k0, k1, js, [&](int32_t i, int32_t d) {
+      if (parts) pl.row_part[(to * kFew + i) * C + d] = __builtin_nanf("");
+      else ((uint16_t*)a.out)[(q.first + i / G) * a.out_token_stride + i % G * a.out_head_stride + d] = F16 ? 0x7e00 : 0x7fc0;
+    });
   }
 }
 
@@ -356,7 +467,9 @@ struct LatentTiles : Latent<NARROW, C> {
   static constexpr int kKeysTile = 2 * L::kKeys, kSubs = kKeysTile / 32;
   static constexpr int kNB = 3;                             // tiles in LDS
   static constexpr int kWeights = 4 * 2 * 1024;             // of 128 rows and 32 keys, as the products take them
-  static constexpr int kLds = kNB * kTile + 2 * kWeights + 2 * 128 * 4 + 2 * 16;
+  static constexpr int kOffsets = kNB * kTile + 2 * kWeights + 2 * 128 * 4 + 2 * 16;
+  static constexpr int kTables = kOffsets + (L::kHalf + 3) / 4 * 1024;   // of the even split
+  static constexpr int kLds = kTables + kSlots * 16;
 };
 
 // x += a b (x = a b where FIRST) with x in vector registers: left alone the compiler keeps what matrix
@@ -379,42 +492,208 @@ __device__ __forceinline__ void settle(f32x16& x) { asm volatile("s_nop 15\n\ts_
 
 // 128 rows of one request and one part of its keys a block.
 template <bool F16, bool NARROW, int C>
-__global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Plan pl) {
+__global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Split pl) {
   using Sh = LatentTiles<NARROW, C>;
   constexpr int RB = Sh::kRB, KS = Sh::kKS32, SUBS = Sh::kSubs, TK = Sh::kKeysTile, NB = Sh::kNB;
   constexpr int DB = C / 128;                               // blocks of 32 of a wave's quarter of the latent
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int part = blockIdx.x % pl.parts_tiles;
-  const int32_t slot = blockIdx.x / pl.parts_tiles;
   const int G = pl.group;
-  const Slot at_slot = slot_of(a, pl, slot);
-  const int32_t r = at_slot.r;
-  if (r < 0) return;
-  const Request q = request(a, pl, r);
-  const int64_t rows = (int64_t)q.count * G;
-  const int64_t row0 = (int64_t)(slot - at_slot.first) * 128;
-  if (rows <= pl.few || row0 >= rows) return;
-  const int32_t parts = parts_of(q, pl.cut_tiles, pl.parts_tiles);
-  if (part >= parts) return;
+
+  // keys that the 128 rows of a request from row0 on see (there are less than 2^31 rows in all)
+  struct Item {
+    int32_t pos_lo, pos_hi, k0, k1, tiles;
+  };
+  auto item = [&](int32_t start, int32_t rows, int32_t lo, int32_t hi, int32_t row0) -> Item {
+    Item x;
+    const int32_t last = row0 + 127 < rows ? row0 + 127 : rows - 1;
+    x.pos_lo = start + row0 / G;
+    x.pos_hi = start + last / G;
+    x.k0 = lo;
+    if (a.window && (int64_t)x.pos_lo - a.window + 1 > x.k0) x.k0 = (x.pos_lo - a.window + 1) & ~63;
+    x.k1 = x.pos_hi < hi ? x.pos_hi + 1 : hi;
+    x.tiles = x.k1 > x.k0 ? (int32_t)(((int64_t)x.k1 - x.k0 + TK - 1) / TK) : 0;
+    return x;
+  };
+  // Few slots of 128 rows: all blocks together take the tiles of all slots in order, an equal share each.
+  // places: where slots begin in the row of costs; owners: their requests and their first rows.
+  struct Owner {
+    int32_t r, row;
+  };
+  int64_t* const places = (int64_t*)(g_lds + Sh::kTables);
+  Owner* const owners = (Owner*)(places + kSlots);
+  int64_t share = 1;
+  int32_t slot = blockIdx.x, slots = blockIdx.x + 1;
+  constexpr int kStart = kTilesStart / SUBS;
+  if (pl.even) {
+    if (threadIdx.x == 0) pl.slot_cut[blockIdx.x].rows = 0;
+    int64_t* const sums = (int64_t*)g_lds;                      // in the ring, as are
+    int32_t* const begins = (int32_t*)(g_lds + 64);            // [kSlots]: the request that begins at a slot
+    i32x4* const requests = (i32x4*)(g_lds + 64 + 4 * kSlots); // [kSlots]
+    const int32_t most = a.requests > pl.slots ? a.requests : pl.slots, each = (most + 255) / 256;
+    const int32_t i0 = threadIdx.x * each;
+    int64_t all, sum = 0;
+#pragma unroll 1
+    for (int32_t i = i0; i < i0 + each; ++i) {
+      begins[i] = 0;
+      if (i >= a.requests) continue;
+      const Request q = request(a, pl, i);
+      requests[i] = i32x4{q.start, q.count * G, q.lo, q.hi};
+      sum += q.count * G > pl.few ? (q.count * G + 127) / 128 : 0;
+    }
+    int32_t from = (int32_t)before(sum, all, sums);
+    slots = (int32_t)uniform(all < kSlots ? all : kSlots);
+#pragma unroll 1
+    for (int32_t i = i0; i < i0 + each && i < a.requests; ++i) {
+      const int32_t rows = requests[i][1];
+      if (rows <= pl.few) continue;
+      if (from < kSlots) begins[from] = i;   // overlapping requests may have more slots than there can be
+      owners[i].row = from;                 // for now: the request's first slot
+      from += (rows + 127) / 128;
+    }
+    __syncthreads();
+    // the last request that begins at or before a slot
+    int32_t last = 0;
+    for (int32_t i = i0; i < i0 + each; ++i) last = begins[i] > last ? begins[i] : last;
+    int32_t up = last;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int32_t y = __shfl_up(up, o);
+      if (lane >= o && y > up) up = y;
+    }
+    if (lane == kWave - 1) ((int32_t*)sums)[8 + wave] = up;
+    up = __shfl_up(up, 1);
+    if (lane == 0) up = 0;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+      const int32_t y = ((int32_t*)sums)[8 + w];
+      up = y > up ? y : up;
+    }
+    sum = 0;
+    Owner mine[kSlots / 256];
+    int32_t cost[kSlots / 256];
+#pragma unroll
+    for (int e = 0; e < kSlots / 256; ++e) {
+      const int32_t i = i0 + e;
+      if (e >= each || i >= slots) continue;
+      up = begins[i] > up ? begins[i] : up;
+      const i32x4 q = requests[up];
+      mine[e] = {up, (i - owners[up].row) * 128};
+      cost[e] = item(q[0], q[1], q[2], q[3], mine[e].row).tiles + kStart;
+      sum += cost[e];
+    }
+    int64_t at = before(sum, all, sums);       // and every first slot is read
+#pragma unroll
+    for (int e = 0; e < kSlots / 256; ++e) {
+      const int32_t i = i0 + e;
+      if (e >= each || i >= slots) continue;
+      places[i] = at;
+      owners[i] = mine[e];
+      at += cost[e];
+    }
+    __syncthreads();
+    share = uniform((all + gridDim.x - 1) / gridDim.x);
+    if (share < kTilesShare / SUBS) share = kTilesShare / SUBS;
+    const int64_t x0 = blockIdx.x * share;
+    if (x0 >= all) return;
+    int32_t lo = 0, hi = slots - 1;         // the last slot at or before x0
+    while (lo < hi) {
+      const int32_t mid = (lo + hi + 1) / 2;
+      if (places[mid] <= x0) lo = mid;
+      else hi = mid - 1;
+    }
+    slot = __builtin_amdgcn_readfirstlane(lo);
+  }
 
   const int half = lane / 32, l32 = lane % 32, i16 = lane % 16, dh = (lane / 16) % 2;
-  const int64_t row = row0 + wave * 32 + l32;
+#pragma unroll 1
+  for (; slot < slots; ++slot) {
+  int32_t r, row0;
+  int64_t place = 0;
+  if (pl.even) {
+    place = uniform(places[slot]);
+    if (place >= (blockIdx.x + 1) * share) return;
+    r = __builtin_amdgcn_readfirstlane(owners[slot].r);
+    row0 = __builtin_amdgcn_readfirstlane(owners[slot].row);
+  } else {
+    const Slot s = slot_of(a, pl, slot);
+    r = s.r;
+    row0 = (slot - s.first) * 128;
+    if (r < 0) return;
+  }
+  const Request q = request(a, pl, r);
+  const int32_t rows = q.count * G;
+  if (!pl.even && (rows <= pl.few || row0 >= rows)) return;
+  const Item x = item(q.start, rows, q.lo, q.hi, row0);
+  int32_t k0 = x.k0, k1 = x.k1;
+  bool parts = false;
+  int64_t to = 0;
+  const int32_t count = rows - row0 < 128 ? rows - row0 : 128;
+  if (pl.even) {
+    const int32_t b = blockIdx.x;
+    const Piece piece = piece_of(place, kStart, x.tiles, share, b);
+    if (!piece.here) continue;
+    const int64_t end = (int64_t)k0 + (int64_t)piece.to * TK;
+    if (end < k1) k1 = (int32_t)end;
+    k0 += piece.from * TK;
+    parts = !piece.first || !piece.last;
+    to = 2 * b + piece.first;
+    if (piece.first && parts && threadIdx.x == 0)
+      pl.slot_cut[b] = {(int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, count};
+  }
+  k0 = __builtin_amdgcn_readfirstlane(k0);
+  k1 = __builtin_amdgcn_readfirstlane(k1);
+  const int32_t nt = k1 > k0 ? (int32_t)(((int64_t)k1 - k0 + TK - 1) / TK) : 0;
+  const int32_t kbase = k0, pos_lo = x.pos_lo, pos_hi = x.pos_hi;
+  const int32_t row = row0 + wave * 32 + l32;
   const bool live = row < rows;
-  const int32_t tok = (int32_t)((live ? row : 0) / G), g = (int32_t)((live ? row : 0) % G);
+  const int32_t tok = (live ? row : 0) / G, g = (live ? row : 0) % G;
   const int32_t pos = live ? q.start + tok : -1;
+  barrier();                          // the last piece's sums are read
 
-  // keys of this part that the tile's rows see
-  const int32_t tok_lo = (int32_t)(row0 / G);
-  const int64_t last = row0 + 127 < rows ? row0 + 127 : rows - 1;
-  const int32_t pos_lo = q.start + tok_lo, pos_hi = q.start + (int32_t)(last / G);
-  int64_t k0 = q.lo + (int64_t)part * pl.cut_tiles;
-  int64_t k1 = part + 1 < parts ? k0 + pl.cut_tiles : q.hi;
-  if (k1 > (int64_t)pos_hi + 1) k1 = (int64_t)pos_hi + 1;
-  if (k1 > q.hi) k1 = q.hi;
-  if (a.window && (int64_t)pos_lo - a.window + 1 > k0) k0 = (pos_lo - a.window + 1) & ~63;
-  const int32_t nt = k1 > k0 ? (int32_t)((k1 - k0 + TK - 1) / TK) : 0;
-  const int32_t kbase = (int32_t)k0;
+  const float vs = NARROW && p.k_scale ? p.k_scale[0] : 1.f;
+  const float c = pl.c * vs;
 
+  const int64_t es = NARROW ? 1 : 2;
+  const int64_t page_b = p.page_stride * es;
+  const uint32_t tok_b = (uint32_t)(p.token_stride * es);
+  const uint32_t lds = lds_base(), weights = lds + NB * Sh::kTile, offsets = lds + Sh::kOffsets;
+  float* const alphas = (float*)(g_lds + NB * Sh::kTile + 2 * Sh::kWeights);     // [2][128]
+  int32_t* const grown = (int32_t*)(alphas + 2 * 128);                          // [2][4]
+  // wave w brings a quarter of a tile's keys
+  constexpr int kMine = TK / 4;
+  const uint32_t own = __builtin_amdgcn_readfirstlane(lds + wave * kMine * RB);
+  const int32_t* blocks = a.block_table + r * a.row_stride;
+  int32_t held = 0;
+  // where tile t comes from and goes to, or the last one again where there are no more
+  struct Move {
+    const char* from;
+    uint32_t to;
+  };
+  auto move_of = [&](int32_t t) -> Move {
+    const uint32_t to = own + t % NB * Sh::kTile;
+    if (t < nt && (t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (int64_t)(t + lane) * TK + wave * kMine);
+    if (t >= nt) t = nt - 1;
+    const int64_t page = __builtin_amdgcn_readlane(held, t & 63);
+    const char* from = (const char*)p.k + page * page_b + (int64_t)((kbase + t * TK + wave * kMine) & (p.page_size - 1)) * tok_b;
+    return {(const char*)uniform((int64_t)from), (uint32_t)__builtin_amdgcn_readfirstlane(to)};
+  };
+  // this lane's sources wait in LDS: registers are short
+  auto sources = [&](auto i) { return *LDS_PTR(u32x4, offsets + i * 1024 + lane * 16); };
+  auto bring = [&](auto i, u32x4 off, const Move& x) { load_lds_at<i * 1024>(x.to, off[i % 4], x.from); };
+
+  // the first tiles are on their way before the queries are read
+  if (nt) {
+    if (threadIdx.x < kWave)
+      each<(Sh::kHalf + 3) / 4>([&](auto i) {
+        *LDS_PTR(u32x4, offsets + i * 1024 + lane * 16) = u32x4{Sh::source(i * 4, lane, tok_b), Sh::source(i * 4 + 1, lane, tok_b),
+                                                                Sh::source(i * 4 + 2, lane, tok_b), Sh::source(i * 4 + 3, lane, tok_b)};
+      });
+    barrier();
+#pragma unroll 1
+    for (int32_t t = 0; t < 2; ++t) {
+      const Move x = move_of(t);
+      each<Sh::kHalf>([&](auto i) { bring(i, sources(std::integral_constant<int, i / 4>()), x); });
+    }
+  }
   s16x8 qf[KS];
   {
     const uint16_t* src = (const uint16_t*)a.q + (q.first + tok) * a.q_token_stride + g * a.q_head_stride + half * 8;
@@ -425,31 +704,6 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       qf[ks] = __builtin_bit_cast(s16x8, x);
     }
   }
-  const float vs = NARROW && p.k_scale ? p.k_scale[0] : 1.f;
-  const float c = pl.c * vs;
-
-  const int64_t es = NARROW ? 1 : 2;
-  const int64_t page_b = p.page_stride * es;
-  const uint32_t tok_b = (uint32_t)(p.token_stride * es);
-  const uint32_t lds = lds_base(), weights = lds + NB * Sh::kTile;
-  float* const alphas = (float*)(g_lds + NB * Sh::kTile + 2 * Sh::kWeights);     // [2][128]
-  int32_t* const grown = (int32_t*)(alphas + 2 * 128);                          // [2][4]
-  // wave w brings a quarter of a tile's keys
-  constexpr int kMine = TK / 4;
-  const uint32_t own = __builtin_amdgcn_readfirstlane(lds + wave * kMine * RB);
-  uint32_t off[Sh::kHalf];
-#pragma unroll
-  for (int i = 0; i < Sh::kHalf; ++i) off[i] = Sh::source(i, lane, tok_b);
-  const int32_t* blocks = a.block_table + r * a.row_stride;
-  int32_t held = 0;
-  auto issue = [&](int32_t t) {
-    if (t >= nt) return;
-    if ((t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (int64_t)(t + lane) * TK + wave * kMine);
-    const int64_t page = __builtin_amdgcn_readlane(held, t & 63);
-    const char* from = (const char*)p.k + page * page_b + (int64_t)((kbase + t * TK + wave * kMine) & (p.page_size - 1)) * tok_b;
-    const uint32_t to = own + t % NB * Sh::kTile;
-    each<Sh::kHalf>([&](auto i) { load_lds_at<i * 1024>(to, off[i], from); });
-  };
 
   f32x16 acc[DB][4];
 #pragma unroll
@@ -487,13 +741,6 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   };
-  auto scores = [&](uint32_t at) -> f32x16 {       // of 32 keys
-    f32x16 x;
-    each<KS>([&](auto ks) { mfma32_vector<F16, ks == 0>(x, k_frag(at, ks), qf[ks]); });
-    settle(x);
-    return x;
-  };
-
   auto p_frag = [&](int b, int i) -> s16x8 {       // weights of rows 32 (i / 2) .., keys 16 (i % 2) ..
     return *LDS_PTR(s16x8, weights + b * Sh::kWeights + i * 1024 + lane * 16);
   };
@@ -529,54 +776,23 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     }
   };
 
-  // A step's scores and weights, and its values, of 32 keys that some row may not see whole.
-  uint32_t odd = 0;
-  auto weigh = [&](uint32_t at, int32_t key0, int b) {
-    f32x16 s = scores(at);
-    uint32_t seen = 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int32_t key = key0 + 4 * half + (j / 4) * 8 + j % 4;
-      const bool ok = sees(pos, key, a.window) && key < k1;
-      seen |= ok ? 1u << j : 0;
-      if (!ok) s[j] = -INFINITY;
-    }
-    float mx = s[0];
-#pragma unroll
-    for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[j]);
-    peak(mx, b);
-    const float mc = top_of<F16>(m, c);
-    float w[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      w[j] = (seen >> j & 1) ? exp2_(__builtin_fmaf(s[j], c, -mc)) : 0.f;
-      l += w[j];
-    }
-    put_weights(b, 0, pack8<F16>(w));
-    put_weights(b, 1, pack8<F16>(w + 8));
-  };
-  auto values = [&](uint32_t at, int b) {
-    rescale(b);
-    each<2>([&](auto k) {
-      s16x8 w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = p_frag(b, e * 2 + k);
-      each<DB>([&](auto d) {
-        const s16x8 f = only_finite<F16>(v_frag(at + k * 16 * RB, d), odd);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[d][e] = mfma32<F16>(f, w[e], acc[d][e]);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    });
+  // Between a step's scores and its values, this wave's quarter of keys that some row does not see whole.
+  constexpr int kQuarter = C / 4 * (NARROW ? 1 : 2) / 16;      // units
+  bool odd = false;
+  auto clean = [&](uint32_t at) {
+#pragma unroll 1
+    for (int i = lane; i < 32 * kQuarter; i += kWave)
+      odd |= clean16<F16, NARROW>(lds + at + i / kQuarter * RB + (wave * kQuarter + i % kQuarter) * 16);
+    wait_lds();
   };
 
-  // The values of one step (at `cur`, weights in buffer b) and the scores and weights of the next, of keys
-  // that every row sees.
+  // The values of one step (at `cur`, weights in buffer b) and the scores and weights of the next.
   constexpr int kAhead = 4, NV = 2 * DB;
-  auto step = [&](uint32_t cur, uint32_t next, int b) {
+  auto step = [&](uint32_t cur, uint32_t next, int b, int32_t key0, bool masked, bool more, const Move& tile) {
     rescale(b);
     s16x8 f[KS], w[8], v[NV];
     f32x16 y;
+    u32x4 off[(Sh::kHalf + 3) / 4];
     auto read_v = [&](auto i) { v[i] = v_frag(cur + i / DB * 16 * RB, i % DB); };
     auto read_w = [&](auto i) { w[i] = p_frag(b, i % 4 * 2 + i / 4); };
     each<kAhead>([&](auto i) { f[i] = k_frag(next, i); });
@@ -585,6 +801,9 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       else read_w(std::integral_constant<int, i + kAhead - KS>());
       if constexpr (i == KS - 2) read_v(std::integral_constant<int, 0>());
       mfma32_vector<F16, i == 0>(y, f[i], qf[i]);
+      if constexpr (i % 8 == 0 && i / 8 < (Sh::kHalf + 3) / 4) off[i / 8] = sources(std::integral_constant<int, i / 8>());
+      if constexpr (i >= 4 && i % 2 == 0 && i / 2 - 2 < Sh::kHalf)
+        if (more) bring(std::integral_constant<int, i / 2 - 2>(), off[(i / 2 - 2) / 4], tile);
       __builtin_amdgcn_sched_barrier(0);
     });
     float mx = -INFINITY, mc = 0, sum = 0, x[16];
@@ -597,7 +816,16 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       acc[g % DB][e] = mfma32<F16>(v[g], w[g / DB * 4 + e], acc[g % DB][e]);
       // the next step's weights, a few instructions beside each product
       constexpr int kWait = 4, kMax = NM / 8, kPeak = kWait + kMax, kExp = kPeak + 1, kEnd = NM - NM / 8;
-      if constexpr (i == kWait - 1) settle(y);
+      if constexpr (i == kWait - 1) {
+        settle(y);
+        if (masked) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int32_t key = key0 + 4 * half + (j / 4) * 8 + j % 4;
+            if (!(sees(pos, key, a.window) && key < k1)) y[j] = -INFINITY;
+          }
+        }
+      }
       if constexpr (i >= kWait && i < kPeak) {
 #pragma unroll
         for (int j = (i - kWait) * 16 / kMax; j < (i - kWait + 1) * 16 / kMax; ++j) mx = fmaxf(mx, y[j]);
@@ -624,229 +852,218 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     l += sum;
   };
 
-  const Span3 sp = spans<TK>(kbase, nt, pos_lo, pos_hi, (int32_t)k1, a.window);
-  issue(0);
-  issue(1);
   // One barrier a step of 32 keys.  Before it the step's weights are written and the next step's keys
   // waited for; behind it every wave is past the values of the step before, whose tile is brought anew.
-  if (nt > 1) wait_loads<Sh::kHalf>();
-  else wait_loads<0>();
+  // There is one body for all steps, since fetching code takes longer than running it: the first has the values of no
+  // keys (zeros in the third tile and the second weights), the last the scores of keys that no row sees.
+  const Span3 sp = spans<TK>(kbase, nt, pos_lo, pos_hi, k1, a.window);
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x * 16; i < Sh::kTile; i += 4096) *LDS_PTR(i32x4, lds + 2 * Sh::kTile + i) = i32x4{0, 0, 0, 0};
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x * 16; i < Sh::kWeights; i += 4096) *LDS_PTR(i32x4, weights + Sh::kWeights + i) = i32x4{0, 0, 0, 0};
+  if (threadIdx.x < 4) grown[4 + threadIdx.x] = 0;
+  wait_loads<0>();
   barrier();
   const int32_t steps = nt * SUBS, whole = sp.whole * SUBS, tail = sp.tail * SUBS;
-  auto turn = [&](int32_t u) {       // step u's weights are on their way
-    const bool end = SUBS == 1 || (u & 1);
-    if (end) wait_loads<0>();
+  uint32_t cur = 2 * Sh::kTile;
+#pragma unroll 1
+  for (int32_t u = 0;; ++u) {
+    const uint32_t next = u / SUBS % NB * Sh::kTile + u % SUBS * 32 * RB;
+    const bool masked = u < whole || u >= tail;
+    const bool more = u && (SUBS == 1 || !(u & 1));    // a tile's last step is over: two tiles on
+    step(cur, next, (u & 1) ^ 1, kbase + u * 32, masked, more, move_of(u / SUBS + 1));
+    if (u == steps) break;
+    if (SUBS == 1 || (u & 1)) wait_loads<0>();
     barrier();
-    if (end) issue(u / SUBS + 2);
-  };
-  auto place = [&](int32_t u) -> uint32_t { return u / SUBS % NB * Sh::kTile + u % SUBS * 32 * RB; };
-  int32_t u = 0;
-#pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-    for (const int32_t e = pass ? steps : whole; u < e; ++u) {
-      weigh(place(u), kbase + u * 32, u & 1);
-      turn(u);
-      values(place(u), u & 1);
-    }
-    if (pass || u >= tail) continue;
-    weigh(place(u), kbase + u * 32, u & 1);
-    turn(u);
-    uint32_t cur = place(u);
-#pragma unroll 1
-    for (; u + 1 < tail; ++u) {
-      const uint32_t next = place(u + 1);
-      step(cur, next, u & 1);
-      turn(u + 1);
-      cur = next;
-    }
-    values(cur, u & 1);
-    ++u;
+    if (masked) clean(next);
+    cur = next;
   }
+  wait_loads<0>();
 
-  // sums and log sums from the rows' waves to all
+  // The rows' sums and where they go, from their waves to all; then 32 rows at a time through LDS, so that
+  // whole lines are written.
   l = over_halves(l, Sum());
-  barrier();
-  if (half == 0) alphas[wave * 32 + l32] = l;
-  if (half == 0 && live) {
-    const float lse = l == 0 ? -INFINITY : m * c + (__log2f(l) - kLift<F16>);
-    const int64_t at = (int64_t)(q.first + tok) * a.q_heads + g;
-    if (parts > 1) pl.part_lse[(int64_t)part * a.tokens * a.q_heads + at] = lse;
-    else if (a.lse) a.lse[at] = lse / kLog2e;
-  }
-  barrier();
-  each<4>([&](auto e) {
-    const int64_t other = row0 + e * 32 + l32;
-    if (other >= rows) return;
-    const int32_t tk = q.first + (int32_t)(other / G), og = (int32_t)(other % G);
-    const float le = alphas[e * 32 + l32], inv = vs / le;
-    const int64_t at = ((int64_t)part * a.tokens + tk) * a.q_heads + og;
-    each<DB>([&](auto db) {
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        f32x4 o = {acc[db][e][4 * b], acc[db][e][4 * b + 1], acc[db][e][4 * b + 2], acc[db][e][4 * b + 3]};
-        // where l is 0 the products may still hold 0 times an infinity
-        o = le == 0 ? f32x4{0, 0, 0, 0} : o * inv;
-        const int d = (wave * DB + db) * 32 + b * 8 + half * 4;
-        if (parts == 1) store4<F16>(a, tk, og, d, o);
-        else *(f32x4*)&pl.part[at * C + d] = o;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    });
-  });
-  if (!__any(odd != 0)) return;
-  // Elements that are not finite, in keys that some row does not see: a wave marks its own quarter of
-  // the rows that see them, behind its own stores.
-  __threadfence_block();
-  const int32_t all = (int32_t)(rows - row0 < 128 ? rows - row0 : 128);
-#pragma unroll 1
-  for (int32_t v = 0; v < steps; ++v) {
-    if (v >= whole && v < tail) continue;
-#pragma unroll 1
-    for (int32_t key = kbase + v * 32; key < kbase + v * 32 + 32 && key < k1; ++key) {
-      const char* from = (const char*)p.k + page_of(p, a, pl, blocks, key) * page_b + (int64_t)(key & (p.page_size - 1)) * tok_b;
-#pragma unroll 1
-      for (int32_t d = wave * DB * 32 + lane; d < (wave + 1) * DB * 32; d += kWave) {
-        uint32_t x;
-        if constexpr (NARROW) x = (((const uint8_t*)from)[d] & 0x7f) == 0x7f;
-        else x = not_finite<F16>(((const uint16_t*)from)[d]) & 0x8000u;
-        if (!x) continue;
-#pragma unroll 1
-        for (int32_t i = 0; i < all; ++i) {
-          const int32_t tk = (int32_t)((row0 + i) / G), og = (int32_t)((row0 + i) % G);
-          if (!sees(q.start + tk, key, a.window) || alphas[i] == 0) continue;
-          if (parts == 1)
-            ((uint16_t*)a.out)[(q.first + tk) * a.out_token_stride + og * a.out_head_stride + d] = F16 ? 0x7e00 : 0x7fc0;
-          else
-            pl.part[(((int64_t)part * a.tokens + q.first + tk) * a.q_heads + og) * C + d] = __builtin_nanf("");
-        }
-      }
+  const int any_odd = __syncthreads_or(odd);
+  int64_t* const goes = (int64_t*)(g_lds + NB * Sh::kTile);          // [128], in place of the weights
+  float* const inverse = (float*)(goes + 128);                       // [128]
+  if (half == 0) {
+    alphas[wave * 32 + l32] = l;
+    inverse[wave * 32 + l32] = l == 0 ? 0.f : vs / l;
+    goes[wave * 32 + l32] = parts ? (to * 128 + wave * 32 + l32) * C
+                                  : (q.first + tok) * a.out_token_stride + g * a.out_head_stride;
+    if (live) {
+      const float lse = l == 0 ? -INFINITY : m * c + (__log2f(l) - kLift<F16>);
+      if (parts) pl.slot_lse[to * 128 + wave * 32 + l32] = lse;
+      else if (a.lse) a.lse[(int64_t)(q.first + tok) * a.q_heads + g] = lse / kLog2e;
     }
   }
+  constexpr int kRow = C + 4;         // floats
+#pragma unroll 1
+  for (int32_t e = 0; e < 4 && e * 32 < count; ++e) {
+    each<4>([&](auto i) {
+      if (i != e) return;
+      each<DB>([&](auto db) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *LDS_PTR(f32x4, lds + (l32 * kRow + (wave * DB + db) * 32 + b * 8 + half * 4) * 4) =
+              f32x4{acc[db][i][4 * b], acc[db][i][4 * b + 1], acc[db][i][4 * b + 2], acc[db][i][4 * b + 3]};
+      });
+    });
+    barrier();
+#pragma unroll 4
+    for (int i = 0; i < C / 32; ++i) {
+      const int lane_row = (i * 256 + threadIdx.x) / (C / 4), d = threadIdx.x % (C / 4) * 4, at = e * 32 + lane_row;
+      const float inv = inverse[at];
+      const int64_t put = goes[at] + d;
+      f32x4 o = *LDS_PTR(f32x4, lds + (lane_row * kRow + d) * 4);
+      o = inv == 0 ? f32x4{0, 0, 0, 0} : o * inv;   // where nothing is seen the products may hold 0 times an infinity
+      if (at >= count) continue;
+      if (parts) *(f32x4*)&pl.slot_part[put] = o;
+      else *(i32x2*)((uint16_t*)a.out + put) = i32x2{pack2<F16>(o[0], o[1]), pack2<F16>(o[2], o[3])};
+    }
+    barrier();
+  }
+  if (!any_odd) continue;
+  __threadfence_block();
+  __syncthreads();
+  mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, row0, count, kbase, k1, alphas, [&](int32_t i, int32_t d) {
+    if (parts) pl.slot_part[goes[i] + d] = __builtin_nanf("");
+    else ((uint16_t*)a.out)[goes[i] + d] = F16 ? 0x7e00 : 0x7fc0;
+  });
+  }
+}
+
+// --------------------------------------------------------- k_latent_join ---
+
+// Rows in several parts: a wave takes 256 elements of one of the `each` rows at most of a block's cut.  Bound by the
+// chain of its loads, so eight parts are read at a time, their log sums with them.
+template <bool F16, int C, int ROWS>
+__global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split pl, int32_t each) {
+  constexpr int kTurn = 8, kHalves = C / 256;
+  const int lane = threadIdx.x % kWave;
+  const int32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t first = id / kHalves / each, row = id / kHalves % each, d = id % kHalves * 256 + lane * 4;
+  const int32_t G = pl.group;
+  if (first >= kBlocks) return;
+  const Cut at = (ROWS == kFew ? pl.row_cut : pl.slot_cut)[first];
+  if (row >= at.rows) return;
+  const float* const from = ROWS == kFew ? pl.row_part : pl.slot_part;
+  const float* const sums = ROWS == kFew ? pl.row_lse : pl.slot_lse;
+  float m = -INFINITY, sum = 0;
+  f32x4 o = {0, 0, 0, 0};
+  for (int32_t base = first; base <= at.last; base += kTurn) {
+    float x[kTurn];
+    f32x4 y[kTurn];
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      const int32_t i = base + j < at.last ? base + j : at.last;
+      const int64_t part = (2 * (int64_t)i + (i == first)) * ROWS + row;
+      x[j] = sums[part];
+      y[j] = *(const f32x4*)(from + part * C + d);
+    }
+    float n = m;
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) n = fmaxf(n, x[j]);
+    const float al = m == -INFINITY ? 0.f : exp2_(m - n);
+    o *= al;
+    sum *= al;
+    m = n;
+#pragma unroll
+    for (int j = 0; j < kTurn; ++j) {
+      if (base + j > at.last || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
+      const float w = x[j] == n ? 1.f : exp2_(x[j] - n);
+      sum += w;
+      o += w * y[j];
+    }
+  }
+  o *= sum == 0 ? 0.f : 1.f / sum;
+  const int32_t t = at.first + (at.row + row) / G, g = (at.row + row) % G;
+  store4<F16>(a, t, g, d, o);
+  if (a.lse && d == 0) a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }
 
 // -------------------------------------------------------------- dispatch ---
 
-int64_t round_up(int64_t x, int32_t m) { return (x + m - 1) / m * m; }
-
 struct Choice {
-  int rt;                       // tiles of 16 rows in k_latent_rows, 0 = not launched
-  bool tiles, join;
+  bool rows, tiles;
 };
 
 // Every rule here goes by sizes the host knows, so the workspace is known before the call.
-Choice choose(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a, Plan& pl) {
+Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Split& pl) {
   Choice ch{};
   pl.group = a.q_heads;
   pl.shift = __builtin_ctz(p.page_size);
-  constexpr int kMost = 32;                     // rows k_latent_rows has registers for
-  const int64_t rows = (int64_t)a.max_new * pl.group;
-  if (rows <= kMost) {
-    ch.rt = rows <= 16 ? 1 : 2;
+  if ((int64_t)a.max_new * pl.group <= kFew) {
+    ch.rows = true;
   } else {
     ch.tiles = true;
     // single tokens apart, unless every request has max_new tokens
-    if (pl.group <= kMost && (int64_t)a.requests * a.max_new != a.tokens) ch.rt = pl.group <= 16 ? 1 : 2;
+    ch.rows = pl.group <= kFew && (int64_t)a.requests * a.max_new != a.tokens;
   }
-  pl.few = ch.rt * 16;
-  // keys that a request's rows see, at most; tokens past a row of the block table do not exist
-  int64_t keys = (int64_t)a.max_blocks * p.page_size;
-  if (a.max_len < keys) keys = a.max_len;
-  if (keys < 1) keys = 1;
-  if (a.window && (int64_t)a.window + a.max_new + 64 < keys) keys = (int64_t)a.window + a.max_new + 64;
-  // n parts at most; the last one is open, so a size held to 31 bits loses no key
-  auto cut = [&](int64_t n, int32_t& size, int32_t& parts) {
-    const int64_t x = round_up((keys + n - 1) / n, 128), most = INT32_MAX / 128 * 128;
-    size = (int32_t)(x < most ? x : most);
-    const int64_t count = (keys + size - 1) / size;
-    parts = (int32_t)(count < n ? count : n);
-  };
-  cut(1, pl.cut_rows, pl.parts_rows);
-  cut(1, pl.cut_tiles, pl.parts_tiles);
-  if (ch.rt) {
-    int64_t n = (2048 + a.requests - 1) / a.requests;
-    if (n > keys / 256) n = keys / 256;
-    cut(n > 1 ? n : 1, pl.cut_rows, pl.parts_rows);
-  }
-  pl.slots = (int32_t)((int64_t)a.tokens * pl.group / 128) + a.requests;
-  if (ch.tiles) {
-    // as many parts as end soonest: rounds of resident blocks, each of its share of the tiles and some
-    // tiles' time to start and end, and the join's reading and writing of every part
-    const double blocks = (double)a.tokens * pl.group / 128 + 1, tiles = keys / 32.0;
-    const double tile_us = 1.5 * value_dim / 512;
-    const double part_us = (double)a.tokens * a.q_heads * value_dim * 8 / 4e6;
-    double best = 0;
-    int32_t n = 1;
-    const double part_bytes = (double)a.tokens * a.q_heads * value_dim * 4;
-    // 512 MiB of parts at most
-    for (int32_t i = 1; i <= 64 && (i == 1 || (tiles / i >= 8 && i * part_bytes <= 0x1p29)); ++i) {
-      const double t = std::ceil(blocks * i / 256) * (tiles / i + 6) * tile_us + (i > 1 ? 4 + i * part_us : 0);
-      if (i == 1 || t < best) {
-        best = t;
-        n = i;
-      }
-    }
-    cut(n, pl.cut_tiles, pl.parts_tiles);
-  }
-  ch.join = (ch.rt && pl.parts_rows > 1) || (ch.tiles && pl.parts_tiles > 1);
+  pl.few = ch.rows ? kFew : 0;
+  const int64_t slots = (int64_t)a.tokens * pl.group / 128 + a.requests;
+  pl.slots = slots < INT32_MAX ? (int32_t)slots : INT32_MAX;
+  pl.even = slots <= kSlots;
   return ch;
 }
 
-// Rows of the two regions of parts.
-struct PartRows {
-  int64_t tiles, rows;
-};
-
-PartRows part_rows(const pp_attention_args& a, const Plan& pl, const Choice& ch) {
-  PartRows n{0, 0};
-  if (ch.tiles && pl.parts_tiles > 1) n.tiles = (int64_t)pl.parts_tiles * a.tokens * a.q_heads;
-  if (ch.rt && pl.parts_rows > 1) n.rows = (int64_t)pl.parts_rows * a.requests * pl.few;
-  return n;
-}
-
-template <bool F16, bool NARROW, int C, int RT>
-hipError_t go_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, hipStream_t st) {
-  constexpr int lds = LatentRows<NARROW, C>::kLds;
-  static OnEachGpu once;
-  const hipError_t ok = allow_lds(once, &k_latent_rows<F16, NARROW, C, RT>, lds);
-  if (ok != hipSuccess) return ok;
-  const int64_t grid = (int64_t)a.requests * pl.parts_rows;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_latent_rows<F16, NARROW, C, RT><<<(unsigned)grid, 256, lds, st>>>(p, a, pl);
-  return hipGetLastError();
+// Bytes of the workspace; its regions where `pl` is given one.
+int64_t regions(int32_t value_dim, const pp_attention_args& a, const Choice& ch, Split& pl) {
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    char* const x = (char*)a.workspace + at;
+    at += (bytes + 255) / 256 * 256;
+    return x;
+  };
+  if (ch.rows) {
+    pl.row_part = (float*)take((int64_t)2 * kBlocks * kFew * value_dim * 4);
+    pl.row_lse = (float*)take((int64_t)2 * kBlocks * kFew * 4);
+    pl.row_cut = (Cut*)take(kBlocks * sizeof(Cut));
+  }
+  if (ch.tiles && pl.even) {
+    pl.slot_part = (float*)take((int64_t)2 * kBlocks * 128 * value_dim * 4);
+    pl.slot_lse = (float*)take((int64_t)2 * kBlocks * 128 * 4);
+    pl.slot_cut = (Cut*)take(kBlocks * sizeof(Cut));
+  }
+  return at;
 }
 
 template <bool F16, bool NARROW, int C>
-hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, const Choice& ch, hipStream_t st) {
+hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl, const Choice& ch, hipStream_t st) {
   if (ch.tiles) {
     constexpr int lds = LatentTiles<NARROW, C>::kLds;
     static OnEachGpu once;
     const hipError_t ok = allow_lds(once, &k_latent_tiles<F16, NARROW, C>, lds);
     if (ok != hipSuccess) return ok;
-    const int64_t grid = (int64_t)pl.slots * pl.parts_tiles;
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    k_latent_tiles<F16, NARROW, C><<<(unsigned)grid, 256, lds, st>>>(p, a, pl);
+    k_latent_tiles<F16, NARROW, C><<<pl.even ? kBlocks : pl.slots, 256, lds, st>>>(p, a, pl);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-  }
-  hipError_t e = hipSuccess;
-  if (ch.rt == 1) e = go_rows<F16, NARROW, C, 1>(p, a, pl, st);
-  if (ch.rt == 2) e = go_rows<F16, NARROW, C, 2>(p, a, pl, st);
-  if (e != hipSuccess) return e;
-  if (ch.join) {
-    int64_t few_rows = 0, waves = (int64_t)a.tokens * a.q_heads;
-    if (pl.parts_tiles == 1) {
-      few_rows = (int64_t)a.max_new * pl.group < pl.few ? (int64_t)a.max_new * pl.group : pl.few;
-      waves = (int64_t)a.requests * few_rows;
+    if (pl.even) {
+      const int64_t most = (int64_t)a.max_new * pl.group, each = most < 128 ? most : 128;
+      const int64_t waves = kBlocks * each * (C / 256);
+      k_latent_join<F16, C, 128><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)each);
+      const hipError_t e2 = hipGetLastError();
+      if (e2 != hipSuccess) return e2;
     }
-    k_join<F16, C><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)few_rows, 1);
-    e = hipGetLastError();
   }
-  return e;
+  if (ch.rows) {
+    constexpr int lds = LatentRows<NARROW, C>::kLds;
+    static OnEachGpu once;
+    const hipError_t ok = allow_lds(once, &k_latent_rows<F16, NARROW, C>, lds);
+    if (ok != hipSuccess) return ok;
+    k_latent_rows<F16, NARROW, C><<<kBlocks, 256, lds, st>>>(p, a, pl);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t most = (int64_t)a.max_new * pl.group, each = most < kFew ? most : kFew;
+    const int64_t waves = kBlocks * each * (C / 256);
+    k_latent_join<F16, C, kFew><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)each);
+    return hipGetLastError();
+  }
+  return hipSuccess;
 }
 
 template <bool F16, bool NARROW>
-hipError_t go_dim(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a, const Plan& pl, const Choice& ch,
+hipError_t go_dim(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a, const Split& pl, const Choice& ch,
                   hipStream_t st) {
   if (value_dim == 512) return go<F16, NARROW, 512>(p, a, pl, ch, st);
   return go<F16, NARROW, 256>(p, a, pl, ch, st);
@@ -855,22 +1072,18 @@ hipError_t go_dim(const pp_kv_pages& p, int32_t value_dim, const pp_attention_ar
 }  // namespace
 
 int64_t latent_workspace(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a) {
-  Plan pl{};
-  const Choice ch = choose(p, value_dim, a, pl);
-  const PartRows n = part_rows(a, pl, ch);
-  return (n.tiles + n.rows) * (value_dim + 1) * 4;
+  Split pl{};
+  const Choice ch = choose(p, a, pl);
+  return regions(value_dim, a, ch, pl);
 }
 
 hipError_t launch_latent(const pp_kv_pages& p, int32_t value_dim, const pp_attention_args& a, hipStream_t st) {
-  Plan pl{};
-  const Choice ch = choose(p, value_dim, a, pl);
+  Split pl{};
+  const Choice ch = choose(p, a, pl);
+  regions(value_dim, a, ch, pl);
   pl.negative = a.scale < 0;
-  pl.c = (a.scale < 0 ? -a.scale : a.scale) * kLog2e;
-  pl.part = (float*)a.workspace;
-  const PartRows n = part_rows(a, pl, ch);
-  pl.row_part = pl.part + n.tiles * value_dim;
-  pl.part_lse = pl.row_part + n.rows * value_dim;
-  pl.row_lse = pl.part_lse + n.tiles;
+  // a scale of 0 is held above it, so that -infinity times it is still that
+  pl.c = std::fmax(std::fabs(a.scale) * kLog2e, 0x1p-126f);
   const bool narrow = p.dtype == PP_E4M3;
   if (a.dtype == PP_F16) return narrow ? go_dim<true, true>(p, value_dim, a, pl, ch, st) : go_dim<true, false>(p, value_dim, a, pl, ch, st);
   return narrow ? go_dim<false, true>(p, value_dim, a, pl, ch, st) : go_dim<false, false>(p, value_dim, a, pl, ch, st);
