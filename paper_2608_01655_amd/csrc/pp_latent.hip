@@ -19,10 +19,10 @@ namespace pp {
 namespace {
 
 constexpr int kFew = 16;             // rows k_latent_rows takes
-constexpr int kRowsStart = 4;        // what a request's start and end cost it, in stages, and the least a block takes
+constexpr int kRowsStart = 16;        // what a request's start and end cost it, in stages, and the least a block takes
 constexpr int kRowsShare = 8;
-constexpr int kTilesStart = 8;       // the same of k_latent_tiles, in steps of 32 keys
-constexpr int kTilesShare = 12;
+constexpr int kTilesStart = 16;       // the same of k_latent_tiles, in steps of 32 keys
+constexpr int kTilesShare = 8;
 constexpr int kBlocks = 256;         // resident ones: one a CU
 constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into equal shares, and requests
 
@@ -302,14 +302,18 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         i32x4 y = *(const i32x4*)(src + ks * 32);
-        if (pl.negative) y ^= (int)0x80008000;
+        y ^= pl.negative;
         qf[ks] = __builtin_bit_cast(s16x8, y);
       }
     }
     f32x4 acc[DB];
     float m = -INFINITY, l = 0;
+    s16x8 nothing = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int d = 0; d < DB; ++d) acc[d] = f32x4{0, 0, 0, 0};
+    for (int d = 0; d < DB; ++d) {
+      asm volatile("" : "+v"(nothing));     // cleared one by one, not copied
+      acc[d] = mfma16<F16>(nothing, nothing, f32x4{0, 0, 0, 0});
+    }
     const int32_t pos_lo = q.start;   // the first row's; rows of -1 see nothing in any case
     const int32_t pos_hi = q.start + q.count - 1;
 
@@ -368,8 +372,10 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
         const float n = fmaxf(m, mx);
         const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
         l *= al;
+        if (__any(m != -INFINITY)) {      // else there is nothing yet
 #pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] *= al;
+          for (int d = 0; d < DB; ++d) acc[d] *= al;
+        }
         m = n;
       }
       const float mc = top_of<F16>(m, c);
@@ -700,18 +706,24 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       i32x4 x = *(const i32x4*)(src + ks * 16);
-      if (pl.negative) x ^= (int)0x80008000;
+      x ^= pl.negative;
       qf[ks] = __builtin_bit_cast(s16x8, x);
     }
   }
 
-  f32x16 acc[DB][4];
+  // cleared by the matrix cores: 16 instructions instead of 256
+  f32x16 acc[DB][4], zeros;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) zeros[i] = 0;
+  s16x8 nothing = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[d][e][i] = 0;
+    for (int e = 0; e < 4; ++e) {
+      asm volatile("" : "+v"(nothing));     // else the compiler clears one and copies it
+      acc[d][e] = mfma32<F16>(nothing, nothing, zeros);
+      if constexpr (C == 512) asm volatile("" : "+a"(acc[d][e]));
+    }
   float m = -INFINITY, l = 0;
 
   // reads along a row: key l32, its units half + 2 ks (8 bits: the half of unit ks); transposed ones of
@@ -751,14 +763,16 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   auto peak = [&](float mx, int b) {
     mx = over_halves(mx, Max());
     const bool grows = __any(mx > m && (m == -INFINITY || (mx - m) * c > kLag<F16>));
+    bool scaled = false;
     if (grows) {
       const float n = fmaxf(m, mx);
       const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
-      l *= al;
-      m = n;
       if (half == 0) alphas[b * 128 + wave * 32 + l32] = al;
+      l *= al;
+      scaled = __any(m != -INFINITY);     // else there is nothing yet
+      m = n;
     }
-    if (lane == 0) grown[b * 4 + wave] = grows;
+    if (lane == 0) grown[b * 4 + wave] = scaled;
   };
   auto rescale = [&](int b) {
     const i32x4 any = *(const i32x4*)&grown[b * 4];
@@ -910,16 +924,38 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       });
     });
     barrier();
-#pragma unroll 4
-    for (int i = 0; i < C / 32; ++i) {
-      const int lane_row = (i * 256 + threadIdx.x) / (C / 4), d = threadIdx.x % (C / 4) * 4, at = e * 32 + lane_row;
-      const float inv = inverse[at];
-      const int64_t put = goes[at] + d;
-      f32x4 o = *LDS_PTR(f32x4, lds + (lane_row * kRow + d) * 4);
-      o = inv == 0 ? f32x4{0, 0, 0, 0} : o * inv;   // where nothing is seen the products may hold 0 times an infinity
-      if (at >= count) continue;
-      if (parts) *(f32x4*)&pl.slot_part[put] = o;
-      else *(i32x2*)((uint16_t*)a.out + put) = i32x2{pack2<F16>(o[0], o[1]), pack2<F16>(o[2], o[3])};
+    // a wave takes every fourth row, four of them at a time so that their reads are in flight together
+#pragma unroll 1
+    for (int i = 0; i < 8; i += 4) {
+      f32x4 o[4][C / 256];
+      float inv[4];
+      int64_t put[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = (i + j) * 4 + wave;
+        inv[j] = inverse[e * 32 + at];
+        put[j] = goes[e * 32 + at];
+#pragma unroll
+        for (int h = 0; h < C / 256; ++h) o[j][h] = *LDS_PTR(f32x4, lds + (at * kRow + h * 256 + lane * 4) * 4);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int h = 0; h < C / 256; ++h) {
+          asm volatile("" : "+v"(o[j][h]));
+          o[j][h] *= inv[j];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][h][x] = inv[j] == 0 ? 0.f : o[j][h][x];   // of no keys: 0 times an infinity, it may be
+        }
+        if (e * 32 + (i + j) * 4 + wave >= count) continue;
+        const int64_t to_row = uniform(put[j]);
+#pragma unroll
+        for (int h = 0; h < C / 256; ++h) {
+          const int d = h * 256 + lane * 4;
+          if (parts) *(f32x4*)(pl.slot_part + to_row + d) = o[j][h];
+          else *(i32x2*)((uint16_t*)a.out + to_row + d) = i32x2{pack2<F16>(o[j][h][0], o[j][h][1]), pack2<F16>(o[j][h][2], o[j][h][3])};
+        }
+      }
     }
     barrier();
   }
@@ -935,51 +971,79 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
 // --------------------------------------------------------- k_latent_join ---
 
-// Rows in several parts: a wave takes 256 elements of one of the `each` rows at most of a block's cut.  Bound by the
-// chain of its loads, so eight parts are read at a time, their log sums with them.
-template <bool F16, int C, int ROWS>
+// Rows in several parts, of the `each` rows at most of a block's cut.  Bound by the chain of its loads: a wave reads
+// eight parts at a time, their log sums with them, and WAVES waves share a row's parts where they are many.
+template <bool F16, int C, int ROWS, int WAVES>
 __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split pl, int32_t each) {
   constexpr int kTurn = 8, kHalves = C / 256;
-  const int lane = threadIdx.x % kWave;
-  const int32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int32_t first = id / kHalves / each, row = id / kHalves % each, d = id % kHalves * 256 + lane * 4;
-  const int32_t G = pl.group;
-  if (first >= kBlocks) return;
+  __shared__ float tops[4], totals[4];
+  __shared__ f32x4 outs[4][C / 4];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t id = blockIdx.x * (4 / WAVES) + wave / WAVES, share = wave % WAVES;
+  const int32_t first = id / each, row = id % each;
   const Cut at = (ROWS == kFew ? pl.row_cut : pl.slot_cut)[first];
-  if (row >= at.rows) return;
+  if (row >= at.rows) return;         // all waves of the row
   const float* const from = ROWS == kFew ? pl.row_part : pl.slot_part;
   const float* const sums = ROWS == kFew ? pl.row_lse : pl.slot_lse;
   float m = -INFINITY, sum = 0;
-  f32x4 o = {0, 0, 0, 0};
-  for (int32_t base = first; base <= at.last; base += kTurn) {
+  f32x4 o[kHalves];
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) o[h] = f32x4{0, 0, 0, 0};
+  const int32_t count = at.last - first + 1, mine = (count + WAVES - 1) / WAVES;
+  const int32_t p0 = first + share * mine, p1 = p0 + mine <= at.last ? p0 + mine : at.last + 1;
+  for (int32_t base = p0; base < p1; base += kTurn) {
     float x[kTurn];
-    f32x4 y[kTurn];
+    f32x4 y[kTurn][kHalves];
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) {
-      const int32_t i = base + j < at.last ? base + j : at.last;
+      const int32_t i = base + j < p1 ? base + j : p1 - 1;
       const int64_t part = (2 * (int64_t)i + (i == first)) * ROWS + row;
       x[j] = sums[part];
-      y[j] = *(const f32x4*)(from + part * C + d);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) y[j][h] = *(const f32x4*)(from + part * C + h * 256 + lane * 4);
     }
     float n = m;
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) n = fmaxf(n, x[j]);
     const float al = m == -INFINITY ? 0.f : exp2_(m - n);
-    o *= al;
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) o[h] *= al;
     sum *= al;
     m = n;
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) {
-      if (base + j > at.last || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
+      if (base + j >= p1 || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
       const float w = x[j] == n ? 1.f : exp2_(x[j] - n);
       sum += w;
-      o += w * y[j];
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) o[h] += w * y[j][h];
     }
   }
-  o *= sum == 0 ? 0.f : 1.f / sum;
-  const int32_t t = at.first + (at.row + row) / G, g = (at.row + row) % G;
-  store4<F16>(a, t, g, d, o);
-  if (a.lse && d == 0) a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
+  if constexpr (WAVES > 1) {
+    if (lane == 0) {
+      tops[wave] = m;
+      totals[wave] = sum;
+    }
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) outs[wave][h * 64 + lane] = o[h];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v) {
+      if (totals[v] == 0) continue;
+      const float n = fmaxf(m, tops[v]);
+      const float al = m == -INFINITY ? 0.f : exp2_(m - n), be = tops[v] == n ? 1.f : exp2_(tops[v] - n);
+      sum = sum * al + totals[v] * be;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) o[h] = o[h] * al + outs[v][h * 64 + lane] * be;
+      m = n;
+    }
+  }
+  const float inv = sum == 0 ? 0.f : 1.f / sum;
+  const int32_t t = at.first + (at.row + row) / pl.group, g = (at.row + row) % pl.group;
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) store4<F16>(a, t, g, h * 256 + lane * 4, o[h] * inv);
+  if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }
 
 // -------------------------------------------------------------- dispatch ---
@@ -1030,6 +1094,7 @@ int64_t regions(int32_t value_dim, const pp_attention_args& a, const Choice& ch,
 
 template <bool F16, bool NARROW, int C>
 hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl, const Choice& ch, hipStream_t st) {
+  const int64_t most = (int64_t)a.max_new * pl.group;      // rows of a request
   if (ch.tiles) {
     constexpr int lds = LatentTiles<NARROW, C>::kLds;
     static OnEachGpu once;
@@ -1039,9 +1104,10 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl,
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (pl.even) {
-      const int64_t most = (int64_t)a.max_new * pl.group, each = most < 128 ? most : 128;
-      const int64_t waves = kBlocks * each * (C / 256);
-      k_latent_join<F16, C, 128><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)each);
+      const int32_t each = (int32_t)(most < 128 ? most : 128);
+      // few slots are in many parts
+      if (pl.slots <= 64) k_latent_join<F16, C, 128, 4><<<kBlocks * each, 256, 0, st>>>(a, pl, each);
+      else k_latent_join<F16, C, 128, 1><<<kBlocks * each / 4, 256, 0, st>>>(a, pl, each);
       const hipError_t e2 = hipGetLastError();
       if (e2 != hipSuccess) return e2;
     }
@@ -1054,9 +1120,8 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl,
     k_latent_rows<F16, NARROW, C><<<kBlocks, 256, lds, st>>>(p, a, pl);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t most = (int64_t)a.max_new * pl.group, each = most < kFew ? most : kFew;
-    const int64_t waves = kBlocks * each * (C / 256);
-    k_latent_join<F16, C, kFew><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)each);
+    const int32_t each = (int32_t)(most < kFew ? most : kFew);
+    k_latent_join<F16, C, kFew, 4><<<kBlocks * each, 256, 0, st>>>(a, pl, each);
     return hipGetLastError();
   }
   return hipSuccess;
@@ -1081,7 +1146,7 @@ hipError_t launch_latent(const pp_kv_pages& p, int32_t value_dim, const pp_atten
   Split pl{};
   const Choice ch = choose(p, a, pl);
   regions(value_dim, a, ch, pl);
-  pl.negative = a.scale < 0;
+  pl.negative = a.scale < 0 ? (int32_t)0x80008000 : 0;     // the queries' signs
   // a scale of 0 is held above it, so that -infinity times it is still that
   pl.c = std::fmax(std::fabs(a.scale) * kLog2e, 0x1p-126f);
   const bool narrow = p.dtype == PP_E4M3;
