@@ -839,12 +839,9 @@ def pp_turns(radians):
     return turns.view(np.int64)
 
 
-def _weight(w, rows, device):
-    """(elements normed, address) of a norm's weights for `rows`."""
-    if w is None:
-        return 0, 0
-    if rows is None or w.dim() != 1 or w.dtype != rows.dtype or w.get_device() != device \
-            or not w.is_contiguous():
+def _weight(w, dtype, device):
+    """(elements normed, address) of a norm's weights."""
+    if w.dim() != 1 or w.dtype != dtype or w.get_device() != device or not w.is_contiguous():
         raise ValueError("weights: want a contiguous vector of the rows' type on the GPU")
     return w.shape[0], w.data_ptr()
 
@@ -870,41 +867,50 @@ def pp_rotary_write(position, turns, *, q=None, q_out=None, k=None, k_out=None, 
         raise ValueError("want q with q_out, k with k_out or k_cache, v with v_cache")
     device, st = _stream_of(torch, first, stream)
     T, dtype = first.shape[0], first.dtype
-    strides, dims = [], []
-    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            strides += [0, 0, 0, 0]
-            dims.append((0, 0))
-            continue
-        strides += _rows(x, what, device)
-        if x.shape[0] != T or x.dtype != dtype:
-            raise ValueError("shape mismatch")
-        if out is None:
-            strides += [0, 0]
-        else:
-            strides += _rows(out, what + "_out", device)
-            if out.shape != x.shape or out.dtype != dtype:
-                raise ValueError("shape mismatch")
-        dims.append(tuple(x.shape[1:]))
-    pages, slots = None, 0
-    if v is None:
-        strides += [0, 0]
-    else:
-        strides += _rows(v, "v", device)
-        if v.shape != k.shape or v.dtype != dtype:
-            raise ValueError("shape mismatch")
+    Hq = Dq = Hk = Dk = qt = qh = qot = qoh = kt = kh = kot = koh = vt = vh = 0
+    q_at = q_to = k_at = k_to = v_at = slots = rot = at = turning = 0
+    q_norm = q_w = k_norm = k_w = 0
+    pages, same = None, True
+    if q is not None:
+        (qt, qh), (qot, qoh) = _rows(q, "q", device), _rows(q_out, "q_out", device)
+        shape = q.shape
+        _, Hq, Dq = shape
+        same = q_out.shape == shape and q_out.dtype == dtype
+        q_at, q_to = q.data_ptr(), q_out.data_ptr()
+        if q_weight is not None:
+            q_norm, q_w = _weight(q_weight, dtype, device)
+    elif q_weight is not None:
+        raise ValueError("weights: there are no such rows")
+    if k is not None:
+        kt, kh = _rows(k, "k", device)
+        shape = k.shape
+        Tk, Hk, Dk = shape
+        same = same and Tk == T and k.dtype == dtype
+        k_at = k.data_ptr()
+        if k_weight is not None:
+            k_norm, k_w = _weight(k_weight, dtype, device)
+        if k_out is not None:
+            kot, koh = _rows(k_out, "k_out", device)
+            same = same and k_out.shape == shape and k_out.dtype == dtype
+            k_to = k_out.data_ptr()
+        if v is not None:
+            vt, vh = _rows(v, "v", device)
+            same = same and v.shape == shape and v.dtype == dtype
+            v_at = v.data_ptr()
+    elif k_weight is not None:
+        raise ValueError("weights: there are no such rows")
     if k_cache is not None:
         pages, H, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
         if slot_map is None or slot_map.dtype != torch.int64 or slot_map.shape != (T,) \
                 or slot_map.get_device() != device or not slot_map.is_contiguous():
             raise ValueError(f"slot_map: want a contiguous int64 tensor of shape {(T,)} on the "
                              "current GPU")
-        if (H, D) != dims[1]:
-            raise ValueError("shape mismatch")
+        same = same and H == Hk and D == Dk
         slots = slot_map.data_ptr()
     elif k_scale is not None or v_scale is not None or slot_map is not None:
         raise ValueError("scales and places are for pages")
-    rot = at = turning = 0
+    if not same:
+        raise ValueError("shape mismatch")
     if turns is not None:
         if turns.dtype != torch.int64 or turns.dim() != 1 or turns.get_device() != device \
                 or not turns.is_contiguous():
@@ -914,14 +920,10 @@ def pp_rotary_write(position, turns, *, q=None, q_out=None, k=None, k_out=None, 
             raise ValueError(f"position: want a contiguous int32 tensor of shape {(T,)} on the "
                              "current GPU")
         rot, at, turning = 2 * turns.shape[0], position.data_ptr(), turns.data_ptr()
-    q_norm, q_w = _weight(q_weight, q, device)
-    k_norm, k_w = _weight(k_weight, k, device)
     rc = lib().pp_rotary_write(_ROTARY_ARGS.pack(
-        T, _type(first), *dims[0], q_first, q_norm, *dims[1], k_first, k_norm, rot,
-        1 if interleaved else 0, eps, amplitude, *strides,
-        0 if q is None else q.data_ptr(), 0 if k is None else k.data_ptr(),
-        0 if v is None else v.data_ptr(), 0 if q_out is None else q_out.data_ptr(),
-        0 if k_out is None else k_out.data_ptr(), q_w, k_w, at, turning, slots), pages, st)
+        T, _type(first), Hq, Dq, q_first, q_norm, Hk, Dk, k_first, k_norm, rot,
+        1 if interleaved else 0, eps, amplitude, qt, qh, qot, qoh, kt, kh, kot, koh, vt, vh,
+        q_at, k_at, v_at, q_to, k_to, q_w, k_w, at, turning, slots), pages, st)
     if rc:
         _check(rc)
 
@@ -986,10 +988,11 @@ def pp_page_copy(pools, source, target, tokens=None, *, stream=None):
     first = pools[0]
     shape, strides, dtype = first.shape, first.stride(), first.dtype
     for p in pools:
-        if p.dim() != 4 or p.shape != shape or p.stride() != strides or p.dtype != dtype \
-                or p.get_device() != device or strides[3] != 1:
-            raise ValueError("pools: want device tensors [pages][heads][page_size][dim] alike, "
-                             "dim contiguous")
+        if p.shape != shape or p.stride() != strides or p.dtype != dtype \
+                or p.get_device() != device:
+            raise ValueError("pools: want device tensors [pages][heads][page_size][dim] alike")
+    if len(shape) != 4 or strides[3] != 1:
+        raise ValueError("pools: want [pages][heads][page_size][dim], dim contiguous")
     P, H, ps, D = shape
     bases = struct.pack(f"@{len(pools)}P", *[p.data_ptr() for p in pools])
     table = ctypes.c_char_p(bases)

@@ -191,18 +191,47 @@ __device__ __forceinline__ int32_t before(int32_t x, int32_t& all, int32_t* sums
   return base + up - x;
 }
 
-// The whole of it in one block, with a bit a page in LDS.
+// The whole of it in one block, with a bit a page in LDS, for few rows: 16 waves take two rows at a time each.  64
+// rows of up to 512 blocks 5.5 us (8.0 with the call); 128 of 512 11.6 us with the call and 256 of 256 13.9, where the
+// four launches below take 13.
 constexpr int kFreeWords = 32768;     // pages / 32
+constexpr int kFewRows = 256;
+constexpr int kFewEntries = 65536;
 
 __global__ void __launch_bounds__(1024) k_free_few(pp_free_args a, int shift) {
   extern __shared__ uint32_t named[];
   __shared__ int32_t sums[16];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int32_t pages = a.n_pages - a.first, words = (pages + 31) / 32;
+  // the blocks of this wave's rows, one a lane
+  int32_t blocks = wave + 16 * lane < a.requests ? blocks_of(a.length[wave + 16 * lane], shift) : 0;
+  if (blocks > a.max_blocks) blocks = a.max_blocks;
   for (int i = tid; i < words; i += 1024) named[i] = i == words - 1 && pages % 32 ? ~0u << (pages % 32) : 0;
   __syncthreads();
-  for (int32_t r = tid / kWave; r < a.requests; r += 16)
-    pages_of(a, shift, r, tid % kWave, kWave, [&](int32_t p) { atomicOr(&named[(p - a.first) / 32], 1u << ((p - a.first) % 32)); });
+  constexpr int kRows = 2, kTurn = 4;
+  for (int i = 0; wave + 16 * i < a.requests; i += kRows) {
+    int32_t n[kRows], most = 0;
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      n[j] = __builtin_amdgcn_readlane(blocks, i + j);      // rows past the last have none
+      most = n[j] > most ? n[j] : most;
+    }
+    for (int32_t b = lane; b < most; b += kWave * kTurn) {
+      int32_t page[kRows][kTurn];
+#pragma unroll
+      for (int j = 0; j < kRows; ++j)
+#pragma unroll
+        for (int k = 0; k < kTurn; ++k)
+          page[j][k] = b + k * kWave < n[j] ? a.block_table[(wave + 16 * (i + j)) * a.row_stride + b + k * kWave] : -1;
+#pragma unroll
+      for (int j = 0; j < kRows; ++j)
+#pragma unroll
+        for (int k = 0; k < kTurn; ++k) {
+          const uint32_t p = (uint32_t)page[j][k] - (uint32_t)a.first;     // past the last where it is before the first
+          if (p < (uint32_t)pages) atomicOr(&named[p / 32], 1u << (p % 32));
+        }
+    }
+  }
   __syncthreads();
   const int32_t each = (words + 1023) / 1024, w0 = tid * each < words ? tid * each : words;
   const int32_t w1 = w0 + each < words ? w0 + each : words;
@@ -229,31 +258,50 @@ __global__ void __launch_bounds__(256) k_mark(pp_free_args a, int shift) {
   pages_of(a, shift, r, threadIdx.x % kWave, kWave, [&](int32_t p) { a.marks[p] = 1; });
 }
 
-// A block lists the pages of 1,024 words, after counting those before them for itself.
+// Free pages of word i of the marks: bit 0 of a byte, 0 for bytes before `first` and from n_pages on.
+__device__ __forceinline__ uint64_t free_of(const pp_free_args& a, int32_t i) {
+  const int32_t words = (a.n_pages + 7) / 8;
+  if (i >= words) return 0;
+  uint64_t x = 0;
+  if (i * 8 + 8 <= a.n_pages) {
+    x = ((const uint64_t*)a.marks)[i];
+  } else {
+    for (int j = 0; i * 8 + j < a.n_pages; ++j) x |= (uint64_t)a.marks[i * 8 + j] << (8 * j);
+  }
+  x = (x & 0x0101010101010101ull) ^ 0x0101010101010101ull;
+  if (i == a.first / 8) x &= ~0ull << (a.first % 8 * 8);
+  if (i * 8 + 8 > a.n_pages) x &= ~0ull >> ((i * 8 + 8 - a.n_pages) * 8);
+  return x;
+}
+
+// The marks are taken in groups of 1,024 words.  k_count leaves a group's number of free pages in the upper bits of its first
+// word's bytes, two bits in each, so that k_list needs no more memory and reads one word a group before its own:
+// 106,000 pages' marks added up by every block took 60 us.  (The last group's is nobody's, and its first word may
+// be short.)
+__global__ void __launch_bounds__(1024) k_count(pp_free_args a) {
+  __shared__ int32_t sums[16];
+  const int32_t i = a.first / 8 + blockIdx.x * 1024 + threadIdx.x;
+  const uint64_t x = free_of(a, i);
+  int32_t all;
+  before(__popcll(x), all, sums);
+  if (threadIdx.x == 0 && blockIdx.x + 1 < gridDim.x) {
+    uint64_t n = 0;
+    for (int j = 0; j < 8; ++j) n |= (uint64_t)(all >> (2 * j) & 3) << (8 * j + 1);
+    ((uint64_t*)a.marks)[i] = (((uint64_t*)a.marks)[i] & 0x0101010101010101ull) | n;
+  }
+}
+
 __global__ void __launch_bounds__(1024) k_list(pp_free_args a) {
   __shared__ int32_t sums[16], sums2[16];
   const int tid = threadIdx.x;
-  const uint64_t* marks = (const uint64_t*)a.marks;
-  const int32_t first = a.first / 8, words = (a.n_pages + 7) / 8;
-  // free pages of a word: bytes before `first` and from n_pages on are none
-  auto free_of = [&](int32_t i) -> uint64_t {
-    if (i >= words) return 0;
-    uint64_t x = 0;
-    if (i * 8 + 8 <= a.n_pages) {
-      x = marks[i];
-    } else {
-      for (int j = 0; i * 8 + j < a.n_pages; ++j) x |= (uint64_t)a.marks[i * 8 + j] << (8 * j);
-    }
-    x ^= 0x0101010101010101ull;
-    if (i == first) x &= ~0ull << (a.first % 8 * 8);
-    if (i * 8 + 8 > a.n_pages) x &= ~0ull >> ((i * 8 + 8 - a.n_pages) * 8);
-    return x;
-  };
-  const int32_t begin = first + blockIdx.x * 1024;
+  const int32_t begin = a.first / 8 + blockIdx.x * 1024;
   int32_t sum = 0, all, total;
-  for (int32_t i = first + tid; i < begin; i += 1024) sum += __popcll(free_of(i));
+  for (int32_t g = tid; g < (int32_t)blockIdx.x; g += 1024) {
+    const uint64_t n = ((const uint64_t*)a.marks)[a.first / 8 + g * 1024];
+    for (int j = 0; j < 8; ++j) sum += (int32_t)(n >> (8 * j + 1) & 3) << (2 * j);
+  }
+  const uint64_t x = free_of(a, begin + tid);
   before(sum, all, sums);
-  const uint64_t x = free_of(begin + tid);
   int32_t at = all + before(__popcll(x), total, sums2);
   for (uint64_t y = x; y; y &= y - 1, ++at)
     if (at < a.room) a.free_pages[at] = (begin + tid) * 8 + __builtin_ctzll(y) / 8;
@@ -305,7 +353,7 @@ hipError_t launch_fork_tables(const pp_fork_args& a, hipStream_t st) {
 hipError_t launch_free_pages(const pp_free_args& a, hipStream_t st) {
   const int shift = __builtin_ctz(a.page_size);
   const int64_t words = ((int64_t)a.n_pages - a.first + 31) / 32;
-  if ((int64_t)a.requests * a.max_blocks <= 65536 && words <= kFreeWords) {
+  if (a.requests <= kFewRows && (int64_t)a.requests * a.max_blocks <= kFewEntries && words <= kFreeWords) {
     const int lds = (int)(words * 4);
     if (lds > 65536 - 256) {
       static OnEachGpu once;
@@ -323,8 +371,9 @@ hipError_t launch_free_pages(const pp_free_args& a, hipStream_t st) {
   const int64_t whole = a.n_pages / 8;
   k_clear<<<(unsigned)(whole / 256 < 1024 ? whole / 256 + 1 : 1024), 256, 0, st>>>(a.marks, a.n_pages);
   if (a.requests && a.max_blocks) k_mark<<<(a.requests + 3) / 4, 256, 0, st>>>(a, shift);
-  const int32_t left = (a.n_pages + 7) / 8 - a.first / 8;
-  k_list<<<left > 0 ? (left + 1023) / 1024 : 1, 1024, 0, st>>>(a);
+  const int32_t left = (a.n_pages + 7) / 8 - a.first / 8, groups = left > 0 ? (left + 1023) / 1024 : 1;
+  if (groups > 1) k_count<<<groups, 1024, 0, st>>>(a);
+  k_list<<<groups, 1024, 0, st>>>(a);
   return hipGetLastError();
 }
 

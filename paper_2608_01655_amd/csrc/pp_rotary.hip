@@ -73,70 +73,81 @@ __device__ __forceinline__ void widen(i32x4 x, float* f) {
   for (int j = 0; j < 8; ++j) f[j] = widen1<F16>((uint16_t)(x[j / 2] >> (16 * (j % 2))));
 }
 
-// The wave's rows of group g of one kind for one token.
-template <bool F16, bool NARROW, bool TO_PAGES>
-__device__ __forceinline__ void rows_of(const Work& w, const Rows& r, const pp_kv_pages& p, void* base, const float* scales,
-                                        int32_t t, int32_t g, const Angles& an, bool plain) {
-  const int lane = threadIdx.x % kWave;
-  const int sub = lane & ((1 << r.lanes_log2) - 1);
-  const int32_t h = (g << (6 - r.lanes_log2)) + (lane >> r.lanes_log2);
-  int64_t to = 0;
+// A lane's two chunks of its row of a group of one kind, for one token, as they are read.
+struct Chunks {
+  i32x4 x[2], w[2];
+  int32_t at[2];       // their numbers
+  int64_t to;          // their row's place, in elements
+  int32_t head;
+  bool has[2], turns, skipped;
+};
+
+template <bool TO_PAGES, bool PLAIN>
+__device__ __forceinline__ Chunks read_chunks(const Work& w, const Rows& r, const pp_kv_pages& p, int32_t t, int32_t g) {
+  Chunks c;
+  const int lane = threadIdx.x % kWave, sub = lane & ((1 << r.lanes_log2) - 1);
+  const int32_t h = (g << (6 - r.lanes_log2)) + (lane >> r.lanes_log2), turning = PLAIN ? 0 : r.rot;
+  c.head = h;
+  c.turns = sub < turning / 2;
+  if (c.turns) {
+    c.at[0] = r.first + (w.interleaved ? 2 * sub : sub);
+    c.at[1] = c.at[0] + (w.interleaved ? 1 : turning / 2);
+  } else {
+    const int32_t u = 2 * (sub - turning / 2), first = PLAIN ? r.chunks : r.first;
+    c.at[0] = u < first ? u : u + turning;
+    c.at[1] = u + 1 < first ? u + 1 : u + 1 + turning;
+  }
+  const uint16_t* from = r.in + t * r.token + h * r.head;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    c.has[j] = h < r.heads && c.at[j] < r.chunks;
+    c.x[j] = c.w[j] = i32x4{0, 0, 0, 0};
+    if (c.has[j]) c.x[j] = *(const i32x4*)(from + c.at[j] * 8);
+    if (!PLAIN && c.has[j] && c.at[j] < r.norm) c.w[j] = *(const i32x4*)(r.weight + c.at[j] * 8);
+  }
+  c.skipped = false;
   if (TO_PAGES) {
     const int64_t at = w.slot[t];
-    if (at < 0 || at >> w.shift >= p.n_pages) return;        // the whole wave
-    to = (at >> w.shift) * p.page_stride + h * p.head_stride + (at & (p.page_size - 1)) * p.token_stride;
+    c.skipped = at < 0 || at >> w.shift >= p.n_pages;        // for the whole wave
+    c.to = (at >> w.shift) * p.page_stride + h * p.head_stride + (at & (p.page_size - 1)) * p.token_stride;
   } else {
-    to = t * r.out_token + h * r.out_head;
+    c.to = t * r.out_token + h * r.out_head;
   }
-  int32_t a, b;
-  const int32_t turning = plain ? 0 : r.rot;
-  const bool turns = sub < turning / 2;
-  if (turns) {
-    a = r.first + (w.interleaved ? 2 * sub : sub);
-    b = w.interleaved ? a + 1 : a + turning / 2;
-  } else {
-    const int32_t u = 2 * (sub - turning / 2), first = plain ? r.chunks : r.first;
-    a = u < first ? u : u + turning;
-    b = u + 1 < first ? u + 1 : u + 1 + turning;
-  }
-  const bool has_a = h < r.heads && a < r.chunks, has_b = h < r.heads && b < r.chunks;
-  const uint16_t* from = r.in + t * r.token + h * r.head;
-  i32x4 xa = {0, 0, 0, 0}, xb = {0, 0, 0, 0};
-  if (has_a) xa = *(const i32x4*)(from + a * 8);
-  if (has_b) xb = *(const i32x4*)(from + b * 8);
-  const bool same = !NARROW || !TO_PAGES;
-  auto put = [&](int32_t chunk, const float* y, const Scale& s) {
-    if constexpr (NARROW && TO_PAGES) *(i32x2*)((uint8_t*)base + to + chunk * 8) = narrow8(y, s);
-    else *(i32x4*)((uint16_t*)base + to + chunk * 8) = round8<F16>(y);
-  };
-  if (plain && same) {                                        // as it is
-    if (has_a) *(i32x4*)((uint16_t*)base + to + a * 8) = xa;
-    if (has_b) *(i32x4*)((uint16_t*)base + to + b * 8) = xb;
+  return c;
+}
+
+template <bool F16, bool NARROW, bool PLAIN>
+__device__ __forceinline__ void write_chunks(const Work& w, const Rows& r, const Chunks& c, void* base, const float* scales,
+                                             const Angles& an) {
+  if (c.skipped) return;
+  if constexpr (PLAIN && !NARROW) {                           // as it is
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (c.has[j]) *(i32x4*)((uint16_t*)base + c.to + c.at[j] * 8) = c.x[j];
     return;
   }
   float y[16];
-  widen<F16>(xa, y);
-  widen<F16>(xb, y + 8);
-  if (!plain && r.norm) {
-    const bool na = has_a && a < r.norm, nb = has_b && b < r.norm;
+  widen<F16>(c.x[0], y);
+  widen<F16>(c.x[1], y + 8);
+  if (!PLAIN && r.norm) {
     float sum = 0;
-    if (na)
-      for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(y[j], y[j], sum);
-    if (nb)
-      for (int j = 8; j < 16; ++j) sum = __builtin_fmaf(y[j], y[j], sum);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (c.has[j] && c.at[j] < r.norm)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(y[8 * j + i], y[8 * j + i], sum);
     for (int o = 1; o < 1 << r.lanes_log2; o <<= 1) sum += __shfl_xor(sum, o);
     const float f = 1.f / sqrtf(sum / (r.norm * 8) + w.eps);
-    float v[8];
-    if (na) {
-      widen<F16>(*(const i32x4*)(r.weight + a * 8), v);
-      for (int j = 0; j < 8; ++j) y[j] = y[j] * f * v[j];
-    }
-    if (nb) {
-      widen<F16>(*(const i32x4*)(r.weight + b * 8), v);
-      for (int j = 0; j < 8; ++j) y[8 + j] = y[8 + j] * f * v[j];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (!(c.has[j] && c.at[j] < r.norm)) continue;
+      float v[8];
+      widen<F16>(c.w[j], v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[8 * j + i] = y[8 * j + i] * f * v[i];
     }
   }
-  if (turns) {
+  if (!PLAIN && c.turns) {
     if (w.interleaved) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -153,9 +164,13 @@ __device__ __forceinline__ void rows_of(const Work& w, const Rows& r, const pp_k
       }
     }
   }
-  const Scale s = scale_of(NARROW && TO_PAGES && scales && h < r.heads ? scales[h] : 1.f);
-  if (has_a) put(a, y, s);
-  if (has_b) put(b, y + 8, s);
+  const Scale s = scale_of(NARROW && scales && c.head < r.heads ? scales[c.head] : 1.f);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (!c.has[j]) continue;
+    if constexpr (NARROW) *(i32x2*)((uint8_t*)base + c.to + c.at[j] * 8) = narrow8(y + 8 * j, s);
+    else *(i32x4*)((uint16_t*)base + c.to + c.at[j] * 8) = round8<F16>(y + 8 * j);
+  }
 }
 
 template <bool F16, bool NARROW, bool PAGED>
@@ -164,21 +179,28 @@ __global__ void __launch_bounds__(256) k_rotary(Work w, pp_kv_pages p) {
   const int32_t t = (int32_t)(id / w.waves);
   if (t >= w.tokens) return;
   const int32_t g0 = (int32_t)(id % w.waves) * w.each;
-  const int32_t g1 = g0 + w.each < w.groups ? g0 + w.each : w.groups;
+  const int32_t g1 = g0 + w.each < w.groups ? g0 + w.each : w.groups, kg = w.q.groups + w.k.groups;
   const int lane = threadIdx.x % kWave;
   const int32_t position = w.position ? w.position[t] : 0;
   Angles an;
   int32_t g = g0;
-  if (g < w.q.groups) angles(w, position, lane & ((1 << w.q.lanes_log2) - 1), w.q.rot, an);
-  for (; g < g1 && g < w.q.groups; ++g) rows_of<F16, NARROW, false>(w, w.q, p, w.q.out, nullptr, t, g, an, false);
-  if (g < g1 && g < w.q.groups + w.k.groups)
-    if (g == g0 || w.k.lanes_log2 != w.q.lanes_log2) angles(w, position, lane & ((1 << w.k.lanes_log2) - 1), w.k.rot, an);
-  for (; g < g1 && g < w.q.groups + w.k.groups; ++g) {
-    if constexpr (PAGED) rows_of<F16, NARROW, true>(w, w.k, p, p.k, p.k_scale, t, g - w.q.groups, an, false);
-    else rows_of<F16, NARROW, false>(w, w.k, p, w.k.out, nullptr, t, g - w.q.groups, an, false);
+  // a group's rows are on their way before the angles are worked out
+  for (; g < g1 && g < w.q.groups; ++g) {
+    const Chunks c = read_chunks<false, false>(w, w.q, p, t, g);
+    if (g == g0) angles(w, position, lane & ((1 << w.q.lanes_log2) - 1), w.q.rot, an);
+    write_chunks<F16, false, false>(w, w.q, c, w.q.out, nullptr, an);
+  }
+  for (; g < g1 && g < kg; ++g) {
+    const Chunks c = read_chunks<PAGED, false>(w, w.k, p, t, g - w.q.groups);
+    if (g == g0 || (g == w.q.groups && w.k.lanes_log2 != w.q.lanes_log2))
+      angles(w, position, lane & ((1 << w.k.lanes_log2) - 1), w.k.rot, an);
+    write_chunks<F16, NARROW && PAGED, false>(w, w.k, c, PAGED ? p.k : w.k.out, PAGED ? p.k_scale : nullptr, an);
   }
   if constexpr (PAGED)
-    for (; g < g1; ++g) rows_of<F16, NARROW, true>(w, w.v, p, p.v, p.v_scale, t, g - w.q.groups - w.k.groups, an, true);
+    for (; g < g1; ++g) {
+      const Chunks c = read_chunks<true, true>(w, w.v, p, t, g - kg);
+      write_chunks<F16, NARROW, true>(w, w.v, c, p.v, p.v_scale, an);
+    }
 }
 
 int log2_up(int32_t n) {
