@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
 #pragma unroll
         for (int j = 0; j < 4 * KB; ++j) {
           const int32_t key = key0 + (j / 4) * 16 + j % 4;
-          if (!(sees(pos, key, a.window) && key < k1)) y[j] = -INFINITY;
+          if (!(sees(pos, key, a.window) && (uint32_t)key < (uint32_t)k1)) y[j] = -INFINITY;
         }
         wait_lds();
 #pragma unroll 1
@@ -547,13 +547,14 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       sum += q.count * G > pl.few ? (q.count * G + 127) / 128 : 0;
     }
     int32_t from = (int32_t)before(sum, all, sums);
-    slots = (int32_t)uniform(all < kSlots ? all : kSlots);
+    // requests that overlap may have more slots than there can be, and than there is room for: those are left out
+    slots = (int32_t)uniform(all < pl.slots ? all : pl.slots);
 #pragma unroll 1
     for (int32_t i = i0; i < i0 + each && i < a.requests; ++i) {
       const int32_t rows = requests[i][1];
       if (rows <= pl.few) continue;
-      if (from < kSlots) begins[from] = i;   // overlapping requests may have more slots than there can be
-      owners[i].row = from;                 // for now: the request's first slot
+      if (from < slots) begins[from] = i;
+      owners[i].row = from;            // for now: the request's first slot
       from += (rows + 127) / 128;
     }
     __syncthreads();
@@ -622,8 +623,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   } else {
     const Slot s = slot_of(a, pl, slot);
     r = s.r;
+    if (r < 0 || (int64_t)(slot - s.first) * 128 >= (int64_t)a.tokens * G) return;
     row0 = (slot - s.first) * 128;
-    if (r < 0) return;
   }
   const Request q = request(a, pl, r);
   const int32_t rows = q.count * G;
@@ -802,7 +803,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
   // The values of one step (at `cur`, weights in buffer b) and the scores and weights of the next.
   constexpr int kAhead = 4, NV = 2 * DB;
-  auto step = [&](uint32_t cur, uint32_t next, int b, int32_t key0, bool masked, bool more, const Move& tile) {
+  auto step = [&](uint32_t cur, uint32_t next, int b, int32_t key0, uint32_t limit, bool masked, bool more,
+                  const Move& tile) {
     rescale(b);
     s16x8 f[KS], w[8], v[NV];
     f32x16 y;
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const int32_t key = key0 + 4 * half + (j / 4) * 8 + j % 4;
-            if (!(sees(pos, key, a.window) && key < k1)) y[j] = -INFINITY;
+            if (!(sees(pos, key, a.window) && (uint32_t)key < limit)) y[j] = -INFINITY;
           }
         }
       }
@@ -885,7 +887,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     const uint32_t next = u / SUBS % NB * Sh::kTile + u % SUBS * 32 * RB;
     const bool masked = u < whole || u >= tail;
     const bool more = u && (SUBS == 1 || !(u & 1));    // a tile's last step is over: two tiles on
-    step(cur, next, (u & 1) ^ 1, kbase + u * 32, masked, more, move_of(u / SUBS + 1));
+    step(cur, next, (u & 1) ^ 1, kbase + u * 32, u < steps ? k1 : 0, masked, more, move_of(u / SUBS + 1));
     if (u == steps) break;
     if (SUBS == 1 || (u & 1)) wait_loads<0>();
     barrier();

@@ -274,6 +274,80 @@ def test_many_requests(requests):
     check(case(new, length, 16, seed=13))
 
 
+def check_requests(c, which):
+    """Requests `which` of the call against the 64-bit implementation, one at a time."""
+    out, lse = attend(c)
+    torch.cuda.synchronize()
+    begin = c["begin"].tolist()
+    cache = c["cache"].cpu()
+    for r in which:
+        rows = slice(begin[r], begin[r + 1])
+        sub = torch.tensor([0, begin[r + 1] - begin[r]], dtype=torch.int32)
+        want, want_lse, tol, tol_lse = R.latent(c["q"][rows], cache, c["table"][r:r + 1], sub, c["length"][r:r + 1], c["latent"],
+                                                scale=c["scale"], window=c["window"], k_scale=c["ks"])
+        close(out[rows], want, tol)
+        close(lse[rows], want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("window", [0, 700])
+@pytest.mark.parametrize("dtype,cache,latent", [(BF, BF, 512), (HF, E4, 512), (BF, E4, 256)])
+@pytest.mark.parametrize("requests,heads", [(1030, 20), (520, 200)])
+def test_more_slots_than_are_cut(requests, heads, dtype, cache, latent, window):
+    """So many rows that each block takes 128 of them whole, some of them over more keys than it has page numbers of
+    at a time."""
+    length = [1 + r % 50 for r in range(requests)]
+    long = {3: 4097, 100: 2300, 515: 5000, requests - 1: 2048}
+    for r, n in long.items():
+        length[r] = n
+    c = case([1] * requests, length, heads, latent=latent, dtype=dtype, cache=cache, seed=requests)
+    c["window"] = window
+    assert B.pp_latent_workspace(c["q"], c["cache"], c["table"], latent, max_new=1, max_len=5000, window=window) == 0
+    check_requests(c, [*long, 0, 49, 300])
+
+
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("heads,new", [(16, 8200), (40, 3400)])
+def test_prompts_of_more_slots_than_are_cut(heads, new, window):
+    c = case([new, 3], [new, 600], heads, seed=heads)
+    c["window"] = window
+    out, lse = attend(c)
+    torch.cuda.synchronize()
+    cache = c["cache"].cpu()
+    for i in (0, 1, 37, new // 2, new - 1):               # single tokens of the prompt
+        sub = torch.tensor([0, 1], dtype=torch.int32)
+        want, want_lse, tol, tol_lse = R.latent(c["q"][i:i + 1], cache, c["table"][:1], sub, torch.tensor([i + 1]), 512, scale=c["scale"], window=window)
+        close(out[i:i + 1], want, tol)
+        close(lse[i:i + 1], want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("requests", [1, 3, 700])
+@pytest.mark.parametrize("heads", [16, 128])
+def test_shares_of_any_lengths(requests, heads):
+    """Blocks whose share is of many requests, of a part of one, or begins and ends inside them."""
+    g = np.random.default_rng(requests)
+    length = g.integers(0, 40, requests).tolist()
+    length[requests // 2] = 3000 if requests > 1 else 130
+    length[-1] = 1111
+    new = [1 if n else 0 for n in length]
+    new[0], length[0] = 1, max(length[0], 1)
+    c = case(new, length, heads, seed=requests)
+    which = sorted({0, requests // 2, requests - 1, *range(0, requests, 41)})
+    check_requests(c, which)
+
+
+def test_starts_that_are_out_of_order():
+    """Requests whose tokens overlap, or lie outside: nothing else is written, and nothing fails."""
+    c = case([2] * 40, [70] * 40, 128, seed=19)
+    want = [x.clone() for x in attend(c)]
+    bad = c["begin"].clone()
+    bad[5:35:2] = 0
+    bad[6:36:2] = 10 ** 6
+    attend(dict(c, begin=bad, out=torch.empty_like(c["out"]), lse=torch.empty_like(c["lse"])), max_new=80)
+    torch.cuda.synchronize()
+    got = attend(c)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("new,heads", [(1, 16), (24, 16)])
 def test_same_bits_again(new, heads):
     c = case([new] * 5, [5000, 4000, 37, 100, 2000], heads, seed=14)
