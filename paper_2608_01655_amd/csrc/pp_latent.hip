@@ -504,6 +504,10 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   constexpr int DB = C / 128;                               // blocks of 32 of a wave's quarter of the latent
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int G = pl.group;
+  // Blocks go to the eight XCDs in turn.  32 neighbouring shares or slots are one's, since their rows are most often of one
+  // request, whose keys its L2 then holds for all of them.
+  const int32_t block = (blockIdx.x | 255) < gridDim.x ? (int32_t)((blockIdx.x & ~255u) | (blockIdx.x & 7) << 5 | (blockIdx.x & 255) >> 3)
+                                                       : (int32_t)blockIdx.x;
 
   // keys that the 128 rows of a request from row0 on see (there are less than 2^31 rows in all)
   struct Item {
@@ -528,10 +532,10 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   int64_t* const places = (int64_t*)(g_lds + Sh::kTables);
   Owner* const owners = (Owner*)(places + kSlots);
   int64_t share = 1;
-  int32_t slot = blockIdx.x, slots = blockIdx.x + 1;
+  int32_t slot = block, slots = 0;
   constexpr int kStart = kTilesStart / SUBS;
   if (pl.even) {
-    if (threadIdx.x == 0) pl.slot_cut[blockIdx.x].rows = 0;
+    if (threadIdx.x == 0) pl.slot_cut[block].rows = 0;
     int64_t* const sums = (int64_t*)g_lds;                      // in the ring, as are
     int32_t* const begins = (int32_t*)(g_lds + 64);            // [kSlots]: the request that begins at a slot
     i32x4* const requests = (i32x4*)(g_lds + 64 + 4 * kSlots); // [kSlots]
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     __syncthreads();
     share = uniform((all + gridDim.x - 1) / gridDim.x);
     if (share < kTilesShare / SUBS) share = kTilesShare / SUBS;
-    const int64_t x0 = blockIdx.x * share;
+    const int64_t x0 = block * share;
     if (x0 >= all) return;
     int32_t lo = 0, hi = slots - 1;         // the last slot at or before x0
     while (lo < hi) {
@@ -611,16 +615,26 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   }
 
   const int half = lane / 32, l32 = lane % 32, i16 = lane % 16, dh = (lane / 16) % 2;
+  // A block's first slot, of which it may have the end only, comes last: so the blocks begin with the first keys of
+  // their requests together, and find in L2 what the others have read.
+  int32_t left = -1;
+  if (pl.even && slot + 1 < slots && places[slot] + kStart < block * share && places[slot + 1] < (block + 1) * share) left = slot++;
+  left = __builtin_amdgcn_readfirstlane(left);
 #pragma unroll 1
-  for (; slot < slots; ++slot) {
+  for (bool more_slots = true; more_slots; ++slot) {
   int32_t r, row0;
   int64_t place = 0;
   if (pl.even) {
+    if (slot >= slots || uniform(places[slot]) >= (block + 1) * share) {
+      if (left < 0) return;
+      slot = left;
+      more_slots = false;
+    }
     place = uniform(places[slot]);
-    if (place >= (blockIdx.x + 1) * share) return;
     r = __builtin_amdgcn_readfirstlane(owners[slot].r);
     row0 = __builtin_amdgcn_readfirstlane(owners[slot].row);
   } else {
+    more_slots = false;
     const Slot s = slot_of(a, pl, slot);
     r = s.r;
     if (r < 0 || (int64_t)(slot - s.first) * 128 >= (int64_t)a.tokens * G) return;
@@ -635,7 +649,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   int64_t to = 0;
   const int32_t count = rows - row0 < 128 ? rows - row0 : 128;
   if (pl.even) {
-    const int32_t b = blockIdx.x;
+    const int32_t b = block;
     const Piece piece = piece_of(place, kStart, x.tiles, share, b);
     if (!piece.here) continue;
     const int64_t end = (int64_t)k0 + (int64_t)piece.to * TK;
