@@ -816,7 +816,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   };
 
   // The values of one step (at `cur`, weights in buffer b) and the scores and weights of the next.
-  constexpr int kAhead = 4, NV = 2 * DB;
+  constexpr int kAhead = 2, NV = 2 * DB;
   auto step = [&](uint32_t cur, uint32_t next, int b, int32_t key0, uint32_t limit, bool masked, bool more,
                   const Move& tile) {
     rescale(b);
