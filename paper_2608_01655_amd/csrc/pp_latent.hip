@@ -52,12 +52,12 @@ struct Latent {
   static constexpr int kHalf = kLoads / 2;                  // those of kKeys / 2 keys
   static constexpr int kKS16 = (C + 64) / 32, kKS32 = (C + 64) / 16;   // steps of the scores
   static __device__ __forceinline__ int swizzle(int row) {
-    return NARROW ? (row >> 2) & 3 : (row & 2) << 1 | (row & 4) >> 1;
+    return NARROW ? (row >> 2) & 3 : (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3;
   }
-  // This lane's source of load i of kKeys / 2 rows, in bytes from the first.
-  static __device__ __forceinline__ uint32_t source(int i, int lane, uint32_t tok_b) {
+  // This lane's source of load i of kKeys / 2 rows from row `first` on (a multiple of that), in bytes from it.
+  static __device__ __forceinline__ uint32_t source(int i, int lane, uint32_t tok_b, int first) {
     const int u = i * 64 + lane, row = u / kUnits;
-    return row * tok_b + ((u % kUnits) ^ swizzle(row)) * 16;
+    return row * tok_b + ((u % kUnits) ^ swizzle(row + first)) * 16;
   }
 };
 
@@ -239,9 +239,12 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
   const uint32_t tok_b = (uint32_t)(p.token_stride * es);
   const char* rows_at = (const char*)p.k;
   const uint32_t ring = lds_base() + wave * (NS * Sh::kStage);
-  uint32_t off[Sh::kHalf];
+  uint32_t off[2][Sh::kHalf];
 #pragma unroll
-  for (int i = 0; i < Sh::kHalf; ++i) off[i] = Sh::source(i, lane, tok_b);
+  for (int i = 0; i < Sh::kHalf; ++i) {
+    off[0][i] = Sh::source(i, lane, tok_b, 0);
+    off[1][i] = Sh::source(i, lane, tok_b, KEYS / 2);
+  }
   // reads along a row: row i16, its units grp + 4 ks (16 bits) or grp / 2 + 2 ks; transposed ones: four
   // keys a 16-lane group, or eight.  The swizzle meets the steps' low bits only, the rest are offsets.
   const uint32_t kx = NARROW ? ((grp / 2) ^ Sh::swizzle(i16)) * 16 + (grp % 2) * 8 : (grp ^ Sh::swizzle(i16)) * 16;
@@ -286,7 +289,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
         const int32_t key = kbase + t * KEYS + half * (KEYS / 2);
         const int64_t page = __builtin_amdgcn_readlane(held, (t * KB + (KB - 1) * half) & 63);
         const char* from = rows_at + page * page_b + (int64_t)(key & (p.page_size - 1)) * tok_b;
-        each<Sh::kHalf>([&](auto i) { load_lds(into + (half * Sh::kHalf + i) * 1024, off[i], from); });
+        each<Sh::kHalf>([&](auto i) { load_lds(into + (half * Sh::kHalf + i) * 1024, off[half][i], from); });
       }
     };
     __syncthreads();                  // the ring was the last piece's join
@@ -474,7 +477,7 @@ struct LatentTiles : Latent<NARROW, C> {
   static constexpr int kNB = 3;                             // tiles in LDS
   static constexpr int kWeights = 4 * 2 * 1024;             // of 128 rows and 32 keys, as the products take them
   static constexpr int kOffsets = kNB * kTile + 2 * kWeights + 2 * 128 * 4 + 2 * 16;
-  static constexpr int kTables = kOffsets + (L::kHalf + 3) / 4 * 1024;   // of the even split
+  static constexpr int kTables = kOffsets + 2 * ((L::kHalf + 3) / 4) * 1024;   // of the even split
   static constexpr int kLds = kTables + kSlots * 16;
 };
 
@@ -698,15 +701,19 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     return {(const char*)uniform((int64_t)from), (uint32_t)__builtin_amdgcn_readfirstlane(to)};
   };
   // this lane's sources wait in LDS: registers are short
-  auto sources = [&](auto i) { return *LDS_PTR(u32x4, offsets + i * 1024 + lane * 16); };
+  constexpr int kTable = (Sh::kHalf + 3) / 4 * 1024;         // rows 0 .. and 8 .. of 16 lie differently
+  const uint32_t my_offsets = offsets + wave % 2 * kTable;
+  auto sources = [&](auto i) { return *LDS_PTR(u32x4, my_offsets + i * 1024 + lane * 16); };
   auto bring = [&](auto i, u32x4 off, const Move& x) { load_lds_at<i * 1024>(x.to, off[i % 4], x.from); };
 
   // the first tiles are on their way before the queries are read
   if (nt) {
-    if (threadIdx.x < kWave)
+    if (wave < 2)
       each<(Sh::kHalf + 3) / 4>([&](auto i) {
-        *LDS_PTR(u32x4, offsets + i * 1024 + lane * 16) = u32x4{Sh::source(i * 4, lane, tok_b), Sh::source(i * 4 + 1, lane, tok_b),
-                                                                Sh::source(i * 4 + 2, lane, tok_b), Sh::source(i * 4 + 3, lane, tok_b)};
+        u32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = Sh::source(i * 4 + j, lane, tok_b, wave * kMine);
+        *LDS_PTR(u32x4, my_offsets + i * 1024 + lane * 16) = x;
       });
     barrier();
 #pragma unroll 1
@@ -747,11 +754,14 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   const int vrow = NARROW ? ((i16 / 2) / 4) * 8 + 4 * half + (i16 / 2) % 4 : 4 * half + i16 / 4;
   const uint32_t vx = NARROW ? (dh ^ Sh::swizzle(vrow)) * 16 + (i16 % 2) * 8
                              : ((dh * 2 + (i16 % 4) / 2) ^ Sh::swizzle(vrow)) * 16 + (i16 % 2) * 8;
-  uint32_t k_at[4], v_at[2];
+  uint32_t k_at[4], v_at[2], v_up[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) k_at[i] = lds + l32 * RB + (kx ^ (i * (NARROW ? 16 : 32)));
 #pragma unroll
-  for (int i = 0; i < 2; ++i) v_at[i] = lds + vrow * RB + (vx ^ (i * (NARROW ? 32 : 64))) + wave * (RB - 64 * (int)es) / 4;
+  for (int i = 0; i < 2; ++i) {
+    v_at[i] = lds + vrow * RB + (vx ^ (i * (NARROW ? 32 : 64))) + wave * (RB - 64 * (int)es) / 4;
+    v_up[i] = (v_at[i] ^ 16) + 8 * RB;      // eight rows on, where the swizzle's lowest bit is another
+  }
   auto k_frag = [&](uint32_t at, int ks) -> s16x8 {
     const uint32_t from = at + k_at[ks % 4] + ks / 4 * (NARROW ? 64 : 128);
     if constexpr (NARROW) return widen8<F16>(*LDS_PTR(i32x2, from));
@@ -764,7 +774,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, from))));
     } else {
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, from));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, from + 8 * RB));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + v_up[db % 2] + db / 2 * 128));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   };
@@ -828,7 +838,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     each<kAhead>([&](auto i) { f[i] = k_frag(next, i); });
     each<KS>([&](auto i) {
       if constexpr (i + kAhead < KS) f[i + kAhead] = k_frag(next, i + kAhead);
-      else read_w(std::integral_constant<int, i + kAhead - KS>());
+      if constexpr (i >= KS - 4) read_w(std::integral_constant<int, i - (KS - 4)>());
       if constexpr (i == KS - 2) read_v(std::integral_constant<int, 0>());
       mfma32_vector<F16, i == 0>(y, f[i], qf[i]);
       if constexpr (i % 8 == 0 && i / 8 < (Sh::kHalf + 3) / 4) off[i / 8] = sources(std::integral_constant<int, i / 8>());
