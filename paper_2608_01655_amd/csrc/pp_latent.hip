@@ -496,8 +496,8 @@ __device__ __forceinline__ void mfma32_vector(f32x16& x, s16x8 a, s16x8 b) {
   }
 }
 
-// 16 passes of the last instruction that wrote x are over after 19 wait states.
-__device__ __forceinline__ void settle(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x)); }
+// x may be read 12 wait states after the last instruction that wrote it: the number that the compiler leaves where it sees one.
+__device__ __forceinline__ void settle(f32x16& x) { asm volatile("s_nop 11" : "+v"(x)); }
 
 // 128 rows of one request and one part of its keys a block.
 template <bool F16, bool NARROW, int C>
@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   if (!pl.even && (rows <= pl.few || row0 >= rows)) return;
   const Item x = item(q.start, rows, q.lo, q.hi, row0);
   int32_t k0 = x.k0, k1 = x.k1;
-  bool parts = false;
+  bool parts = false, cuts = false;
   int64_t to = 0;
   const int32_t count = rows - row0 < 128 ? rows - row0 : 128;
   if (pl.even) {
@@ -660,8 +660,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     k0 += piece.from * TK;
     parts = !piece.first || !piece.last;
     to = 2 * b + piece.first;
-    if (piece.first && parts && threadIdx.x == 0)
-      pl.slot_cut[b] = {(int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, count};
+    cuts = piece.first && parts;      // the request is cut from here on
   }
   k0 = __builtin_amdgcn_readfirstlane(k0);
   k1 = __builtin_amdgcn_readfirstlane(k1);
@@ -686,7 +685,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   constexpr int kMine = TK / 4;
   const uint32_t own = __builtin_amdgcn_readfirstlane(lds + wave * kMine * RB);
   const int32_t* blocks = a.block_table + r * a.row_stride;
-  int32_t held = 0;
+  int32_t held = nt ? page_of(p, a, pl, blocks, (int64_t)kbase + (int64_t)lane * TK + wave * kMine) : 0;   // of 64 tiles
   // where tile t comes from and goes to, or the last one again where there are no more
   struct Move {
     const char* from;
@@ -694,7 +693,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   };
   auto move_of = [&](int32_t t) -> Move {
     const uint32_t to = own + t % NB * Sh::kTile;
-    if (t < nt && (t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (int64_t)(t + lane) * TK + wave * kMine);
+    if (t && t < nt && (t & 63) == 0) held = page_of(p, a, pl, blocks, (int64_t)kbase + (int64_t)(t + lane) * TK + wave * kMine);
     if (t >= nt) t = nt - 1;
     const int64_t page = __builtin_amdgcn_readlane(held, t & 63);
     const char* from = (const char*)p.k + page * page_b + (int64_t)((kbase + t * TK + wave * kMine) & (p.page_size - 1)) * tok_b;
@@ -706,7 +705,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   auto sources = [&](auto i) { return *LDS_PTR(u32x4, my_offsets + i * 1024 + lane * 16); };
   auto bring = [&](auto i, u32x4 off, const Move& x) { load_lds_at<i * 1024>(x.to, off[i % 4], x.from); };
 
-  // the first tiles are on their way before the queries are read
+  // The queries and the first tiles are on their way together, and what follows up to the first step beside them.
+  s16x8 qf[KS];
+  {
+    const uint16_t* src = (const uint16_t*)a.q + (q.first + tok) * a.q_token_stride + g * a.q_head_stride + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const s16x8*)(src + ks * 16);
+  }
   if (nt) {
     if (wave < 2)
       each<(Sh::kHalf + 3) / 4>([&](auto i) {
@@ -722,16 +727,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       each<Sh::kHalf>([&](auto i) { bring(i, sources(std::integral_constant<int, i / 4>()), x); });
     }
   }
-  s16x8 qf[KS];
-  {
-    const uint16_t* src = (const uint16_t*)a.q + (q.first + tok) * a.q_token_stride + g * a.q_head_stride + half * 8;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      i32x4 x = *(const i32x4*)(src + ks * 16);
-      x ^= pl.negative;
-      qf[ks] = __builtin_bit_cast(s16x8, x);
-    }
-  }
+  if (cuts && threadIdx.x == 0)
+    pl.slot_cut[block] = {(int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, count};
 
   // cleared by the matrix cores: 16 instructions instead of 256
   f32x16 acc[DB][4], zeros;
@@ -902,6 +899,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 #pragma unroll 1
   for (uint32_t i = threadIdx.x * 16; i < Sh::kWeights; i += 4096) *LDS_PTR(i32x4, weights + Sh::kWeights + i) = i32x4{0, 0, 0, 0};
   if (threadIdx.x < 4) grown[4 + threadIdx.x] = 0;
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    i32x4 y = __builtin_bit_cast(i32x4, qf[ks]);
+    y ^= pl.negative;
+    qf[ks] = __builtin_bit_cast(s16x8, y);
+  }
   wait_loads<0>();
   barrier();
   const int32_t steps = nt * SUBS, whole = sp.whole * SUBS, tail = sp.tail * SUBS;
