@@ -26,15 +26,17 @@ constexpr int kTilesShare = 8;
 constexpr int kBlocks = 256;         // resident ones: one a CU
 constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into equal shares, and requests
 
-// Rows that begin in a block and go on in the next ones up to `last`: `rows` of them from row `row` on of the request whose
-// tokens begin at `first` (rows 0: none).
+// Rows that begin in block `block` and go on in the next ones up to `last`: `rows` of them from row `row` on of the
+// request whose tokens begin at `first` (rows 0: none).
 struct Cut {
-  int32_t last, first, row, rows;
+  int32_t block, last, first, row, rows;
 };
 
-// A call's plan, and its parts in the workspace: [2 kBlocks][rows][C], their log sums, and each block's cut.
+// A call's plan, and its parts in the workspace: [2 kBlocks][rows][C] (those of k_latent_tiles in its registers'
+// order, part_at), their log sums, and the cuts.
 struct Split : Plan {
   int32_t even;                      // k_latent_tiles cuts its slots
+  int32_t by_slot;                   // its cuts are numbered by slots, which are fewer than blocks, else by the block they begin in
   float *slot_part, *slot_lse;
   Cut *row_cut, *slot_cut;
 };
@@ -270,7 +272,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
     const bool parts = !piece.first || !piece.last;
     const int64_t to = 2 * b + piece.first;
     if (piece.first && parts && threadIdx.x == 0)
-      pl.row_cut[b] = {(int32_t)((place + x.cost - 1) / share), q.first, 0, rows};
+      pl.row_cut[b] = {b, (int32_t)((place + x.cost - 1) / share), q.first, 0, rows};
     const int32_t k0 = q.lo + piece.from * KEYS;
     const int64_t end = (int64_t)q.lo + (int64_t)piece.to * KEYS;
     const int32_t k1 = end < q.hi ? (int32_t)end : q.hi;
@@ -499,6 +501,20 @@ __device__ __forceinline__ void mfma32_vector(f32x16& x, s16x8 a, s16x8 b) {
 // x may be read 12 wait states after the last instruction that wrote it: the number that the compiler leaves where it sees one.
 __device__ __forceinline__ void settle(f32x16& x) { asm volatile("s_nop 11" : "+v"(x)); }
 
+// Where element d of row `row` of part `part` lies: runs of 256 floats have eight elements of 32 rows, as the
+// accumulators' registers do.
+template <int C>
+__device__ __forceinline__ int64_t part_at(int64_t part, int32_t row, int32_t d) {
+  return (part * 128 + row / 32 * 32) * C + d / 8 * 256 + (d / 4 % 2) * 128 + row % 32 * 4 + d % 4;
+}
+
+// This lane's number, without a register that keeps it.
+__device__ __forceinline__ int this_lane() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
+  return x;
+}
+
 // 128 rows of one request and one part of its keys a block.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Split pl) {
@@ -538,7 +554,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   int32_t slot = block, slots = 0;
   constexpr int kStart = kTilesStart / SUBS;
   if (pl.even) {
-    if (threadIdx.x == 0) pl.slot_cut[block].rows = 0;
+    if (!pl.by_slot && threadIdx.x == 0) pl.slot_cut[block].rows = 0;
     int64_t* const sums = (int64_t*)g_lds;                      // in the ring, as are
     int32_t* const begins = (int32_t*)(g_lds + 64);            // [kSlots]: the request that begins at a slot
     i32x4* const requests = (i32x4*)(g_lds + 64 + 4 * kSlots); // [kSlots]
@@ -556,6 +572,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     int32_t from = (int32_t)before(sum, all, sums);
     // requests that overlap may have more slots than there can be, and than there is room for: those are left out
     slots = (int32_t)uniform(all < pl.slots ? all : pl.slots);
+    if (pl.by_slot && block == 0)       // the others are written where they begin
+      for (int32_t i = slots + threadIdx.x; i < pl.slots; i += 256) pl.slot_cut[i].rows = 0;
 #pragma unroll 1
     for (int32_t i = i0; i < i0 + each && i < a.requests; ++i) {
       const int32_t rows = requests[i][1];
@@ -660,7 +678,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     k0 += piece.from * TK;
     parts = !piece.first || !piece.last;
     to = 2 * b + piece.first;
-    cuts = piece.first && parts;      // the request is cut from here on
+    cuts = piece.first && (parts || pl.by_slot);
   }
   k0 = __builtin_amdgcn_readfirstlane(k0);
   k1 = __builtin_amdgcn_readfirstlane(k1);
@@ -701,8 +719,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   };
   // this lane's sources wait in LDS: registers are short
   constexpr int kTable = (Sh::kHalf + 3) / 4 * 1024;         // rows 0 .. and 8 .. of 16 lie differently
-  const uint32_t my_offsets = offsets + wave % 2 * kTable;
-  auto sources = [&](auto i) { return *LDS_PTR(u32x4, my_offsets + i * 1024 + lane * 16); };
+  uint32_t my_offsets = offsets + wave % 2 * kTable + lane * 16;
+  asm volatile("" : "+v"(my_offsets));
+  auto sources = [&](auto i) {
+    uint32_t x = my_offsets;
+    asm volatile("" : "+v"(x));       // one register, and i as an offset
+    return *LDS_PTR(u32x4, x + i * 1024);
+  };
   auto bring = [&](auto i, u32x4 off, const Move& x) { load_lds_at<i * 1024>(x.to, off[i % 4], x.from); };
 
   // The queries and the first tiles are on their way together, and what follows up to the first step beside them.
@@ -718,7 +741,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
         u32x4 x;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = Sh::source(i * 4 + j, lane, tok_b, wave * kMine);
-        *LDS_PTR(u32x4, my_offsets + i * 1024 + lane * 16) = x;
+        *LDS_PTR(u32x4, my_offsets + i * 1024) = x;
       });
     barrier();
 #pragma unroll 1
@@ -728,7 +751,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     }
   }
   if (cuts && threadIdx.x == 0)
-    pl.slot_cut[block] = {(int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, count};
+    pl.slot_cut[pl.by_slot ? slot : block] = {block, (int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, parts ? count : 0};
 
   // cleared by the matrix cores: 16 instructions instead of 256
   f32x16 acc[DB][4], zeros;
@@ -751,35 +774,34 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   const int vrow = NARROW ? ((i16 / 2) / 4) * 8 + 4 * half + (i16 / 2) % 4 : 4 * half + i16 / 4;
   const uint32_t vx = NARROW ? (dh ^ Sh::swizzle(vrow)) * 16 + (i16 % 2) * 8
                              : ((dh * 2 + (i16 % 4) / 2) ^ Sh::swizzle(vrow)) * 16 + (i16 % 2) * 8;
-  uint32_t k_at[4], v_at[2], v_up[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = lds + l32 * RB + (kx ^ (i * (NARROW ? 16 : 32)));
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    v_at[i] = lds + vrow * RB + (vx ^ (i * (NARROW ? 32 : 64))) + wave * (RB - 64 * (int)es) / 4;
-    v_up[i] = (v_at[i] ^ 16) + 8 * RB;      // eight rows on, where the swizzle's lowest bit is another
-  }
+  // Rows and tiles begin at multiples of 128 bytes (64 of 8-bit rows), so the steps' low bits are exchanged in the whole address.
+  static_assert(Sh::kTile % 128 == 0 && RB % (NARROW ? 64 : 128) == 0);
+  uint32_t k_at = lds + l32 * RB + kx, v_at = lds + vrow * RB + vx + wave * (C * (int)es / 4);
+  asm volatile("" : "+v"(k_at), "+v"(v_at));      // made for each slot: kept from one to the next they would go to memory
   auto k_frag = [&](uint32_t at, int ks) -> s16x8 {
-    const uint32_t from = at + k_at[ks % 4] + ks / 4 * (NARROW ? 64 : 128);
+    const uint32_t from = ((at + k_at) ^ (ks % 4 * (NARROW ? 16 : 32))) + ks / 4 * (NARROW ? 64 : 128);
     if constexpr (NARROW) return widen8<F16>(*LDS_PTR(i32x2, from));
     else return *LDS_PTR(s16x8, from);
   };
   // keys 8 (j / 4) + 4 half + j % 4 of 16, as the weights' registers have them
   auto v_frag = [&](uint32_t at, int db) -> s16x8 {
-    const uint32_t from = at + v_at[db % 2] + db / 2 * (NARROW ? 64 : 128);
+    const uint32_t from = (at + v_at) ^ (db % 2 * (NARROW ? 32 : 64));
     if constexpr (NARROW) {
-      return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, from))));
-    } else {
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, from));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + v_up[db % 2] + db / 2 * 128));
+      return widen8<F16>(__builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, from + db / 2 * 64))));
+    } else {                          // eight rows on the swizzle's lowest bit is another
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, from + db / 2 * 128));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, (from ^ 16) + 8 * RB + db / 2 * 128));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   };
-  auto p_frag = [&](int b, int i) -> s16x8 {       // weights of rows 32 (i / 2) .., keys 16 (i % 2) ..
-    return *LDS_PTR(s16x8, weights + b * Sh::kWeights + i * 1024 + lane * 16);
-  };
-  auto put_weights = [&](int b, int k, s16x8 w) {
-    *LDS_PTR(s16x8, weights + b * Sh::kWeights + (wave * 2 + k) * 1024 + lane * 16) = w;
+  // Weights of rows 32 (i / 2) .., keys 16 (i % 2) .. lie at i * 1024 from where a buffer's begin for this lane.
+  // The compiler is kept from a register for each i.
+  uint32_t w_at = weights + lane * 16;
+  asm volatile("" : "+v"(w_at));
+  auto weights_of = [&](int b) -> uint32_t {
+    uint32_t x = w_at + b * Sh::kWeights;
+    asm volatile("" : "+v"(x));
+    return x;
   };
   // The rows' maximum with that of 32 scores; where one grows too far, all waves have to know.
   auto peak = [&](float mx, int b) {
@@ -789,12 +811,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     if (grows) {
       const float n = fmaxf(m, mx);
       const float al = m == -INFINITY ? 0.f : exp2_((m - n) * c);
-      if (half == 0) alphas[b * 128 + wave * 32 + l32] = al;
+      const int i = this_lane();
+      if (i < 32) alphas[b * 128 + wave * 32 + i] = al;
       l *= al;
       scaled = __any(m != -INFINITY);     // else there is nothing yet
       m = n;
     }
-    if (lane == 0) grown[b * 4 + wave] = scaled;
+    if (this_lane() == 0) grown[b * 4 + wave] = scaled;
   };
   auto rescale = [&](int b) {
     const i32x4 any = *(const i32x4*)&grown[b * 4];
@@ -802,7 +825,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (!__builtin_amdgcn_readfirstlane(any[e])) continue;
-      const float al = alphas[b * 128 + e * 32 + l32];
+      const float al = alphas[b * 128 + e * 32 + this_lane() % 32];
       each<DB>([&](auto d) {
         if constexpr (C == 512) asm volatile("" : "+a"(acc[d][e]));
         acc[d][e] *= al;
@@ -817,7 +840,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   bool odd = false;
   auto clean = [&](uint32_t at) {
 #pragma unroll 1
-    for (int i = lane; i < 32 * kQuarter; i += kWave)
+    for (int i = this_lane(); i < 32 * kQuarter; i += kWave)
       odd |= clean16<F16, NARROW>(lds + at + i / kQuarter * RB + (wave * kQuarter + i % kQuarter) * 16);
     wait_lds();
   };
@@ -831,7 +854,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     f32x16 y;
     u32x4 off[(Sh::kHalf + 3) / 4];
     auto read_v = [&](auto i) { v[i] = v_frag(cur + i / DB * 16 * RB, i % DB); };
-    auto read_w = [&](auto i) { w[i] = p_frag(b, i % 4 * 2 + i / 4); };
+    const uint32_t w_from = weights_of(b);
+    auto read_w = [&](auto i) { w[i] = *LDS_PTR(s16x8, w_from + (i % 4 * 2 + i / 4) * 1024); };
     each<kAhead>([&](auto i) { f[i] = k_frag(next, i); });
     each<KS>([&](auto i) {
       if constexpr (i + kAhead < KS) f[i + kAhead] = k_frag(next, i + kAhead);
@@ -844,13 +868,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       __builtin_amdgcn_sched_barrier(0);
     });
     float mx = -INFINITY, mc = 0, sum = 0, x[16];
+    uint32_t w_to = 0;
     constexpr int NM = NV * 4;
     each<NM>([&](auto at) {
       constexpr int i = decltype(at)::value, g = i / 4, e = i % 4;
       if constexpr (e == 0 && g + 1 < NV) read_v(std::integral_constant<int, g + 1>());
-      if constexpr (g >= 1 && g <= 2 && (e == 1 || e == 2) && DB > 2) read_w(std::integral_constant<int, 4 + (g - 1) * 2 + e - 1>());
-      if constexpr (DB == 2 && g == 1) read_w(std::integral_constant<int, 4 + e>());
       acc[g % DB][e] = mfma32<F16>(v[g], w[g / DB * 4 + e], acc[g % DB][e]);
+      if constexpr (g == DB - 1) read_w(std::integral_constant<int, 4 + e>());      // in place of the one just used
       // the next step's weights, a few instructions beside each product
       constexpr int kWait = 4, kMax = NM / 8, kPeak = kWait + kMax, kExp = kPeak + 1, kEnd = NM - NM / 8;
       if constexpr (i == kWait - 1) {
@@ -882,8 +906,9 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
         }
         asm volatile("" : "+v"(sum));
       }
-      if constexpr (i == kEnd) put_weights(b ^ 1, 0, pack8<F16>(x));
-      if constexpr (i == kEnd + 1) put_weights(b ^ 1, 1, pack8<F16>(x + 8));
+      if constexpr (i == kEnd) w_to = weights_of(b ^ 1) + wave * 2048;
+      if constexpr (i == kEnd) *LDS_PTR(s16x8, w_to) = pack8<F16>(x);
+      if constexpr (i == kEnd + 1) *LDS_PTR(s16x8, w_to + 1024) = pack8<F16>(x + 8);
       __builtin_amdgcn_sched_barrier(0);
     });
     l += sum;
@@ -924,76 +949,69 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   }
   wait_loads<0>();
 
-  // The rows' sums and where they go, from their waves to all; then 32 rows at a time through LDS, so that
-  // whole lines are written.
+  // The rows' sums and where they go, from their waves to all.  What a lane holds goes out from its registers: parts
+  // as they lie, 1 KB a store, and rows in pieces of 32 bytes (32 rows at a time through LDS, in whole lines,
+  // took 20,000 cycles where this takes XXX).
+  // Numbers of lanes are made anew: what the loop would have to keep for here it has no registers for.
+  const int lane_ = this_lane(), half_ = lane_ / 32, l32_ = lane_ % 32;
   l = over_halves(l, Sum());
   const int any_odd = __syncthreads_or(odd);
   int64_t* const goes = (int64_t*)(g_lds + NB * Sh::kTile);          // [128], in place of the weights
   float* const inverse = (float*)(goes + 128);                       // [128]
-  if (half == 0) {
-    alphas[wave * 32 + l32] = l;
-    inverse[wave * 32 + l32] = l == 0 ? 0.f : vs / l;
-    goes[wave * 32 + l32] = parts ? (to * 128 + wave * 32 + l32) * C
-                                  : (q.first + tok) * a.out_token_stride + g * a.out_head_stride;
-    if (live) {
+  if (half_ == 0) {
+    const int32_t i = wave * 32 + l32_, row_ = row0 + i;
+    alphas[i] = l;
+    inverse[i] = l == 0 ? 0.f : vs / l;
+    if (row_ < rows) {
+      const int32_t tok_ = row_ / G, g_ = row_ % G;
+      goes[i] = (q.first + tok_) * a.out_token_stride + g_ * a.out_head_stride;
       const float lse = l == 0 ? -INFINITY : m * c + (__log2f(l) - kLift<F16>);
-      if (parts) pl.slot_lse[to * 128 + wave * 32 + l32] = lse;
-      else if (a.lse) a.lse[(int64_t)(q.first + tok) * a.q_heads + g] = lse / kLog2e;
+      if (parts) pl.slot_lse[to * 128 + i] = lse;
+      else if (a.lse) a.lse[(int64_t)(q.first + tok_) * a.q_heads + g_] = lse / kLog2e;
     }
   }
-  constexpr int kRow = C + 4;         // floats
+  barrier();
+  float inv = 0;
+  int64_t row_at = 0;
 #pragma unroll 1
-  for (int32_t e = 0; e < 4 && e * 32 < count; ++e) {
-    each<4>([&](auto i) {
-      if (i != e) return;
-      each<DB>([&](auto db) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-          *LDS_PTR(f32x4, lds + (l32 * kRow + (wave * DB + db) * 32 + b * 8 + half * 4) * 4) =
-              f32x4{acc[db][i][4 * b], acc[db][i][4 * b + 1], acc[db][i][4 * b + 2], acc[db][i][4 * b + 3]};
-      });
+  for (int32_t n = 0; n < 4 * DB && n / DB * 32 < count; ++n) {
+    const int32_t e = n / DB, db = n % DB;
+    if (db == 0) {
+      inv = inverse[e * 32 + l32_];
+      row_at = goes[e * 32 + l32_];
+    }
+    f32x16 o;
+    each<4 * DB>([&](auto i) {
+      if (i != n) return;
+      o = acc[i % DB][i / DB];
+      asm volatile("" : "+v"(o));
     });
-    barrier();
-    // a wave takes every fourth row, four of them at a time so that their reads are in flight together
-#pragma unroll 1
-    for (int i = 0; i < 8; i += 4) {
-      f32x4 o[4][C / 256];
-      float inv[4];
-      int64_t put[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = (i + j) * 4 + wave;
-        inv[j] = inverse[e * 32 + at];
-        put[j] = goes[e * 32 + at];
+    for (int j = 0; j < 16; ++j) o[j] *= inv;
+    if (__any(inv == 0)) {              // of no keys: 0 times an infinity, it may be
 #pragma unroll
-        for (int h = 0; h < C / 256; ++h) o[j][h] = *LDS_PTR(f32x4, lds + (at * kRow + h * 256 + lane * 4) * 4);
-      }
+      for (int j = 0; j < 16; ++j) o[j] = inv == 0 ? 0.f : o[j];
+    }
+    if (parts) {
+      float* const at = pl.slot_part + part_at<C>(to, e * 32, (wave * DB + db) * 32) + lane_ * 4;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int b = 0; b < 4; ++b) *(f32x4*)(at + b * 256) = f32x4{o[4 * b], o[4 * b + 1], o[4 * b + 2], o[4 * b + 3]};
+    } else if (e * 32 + l32_ < count) {
+      // halves of the wave have four elements each in turn; after the exchange eight
+      uint16_t* const at = (uint16_t*)a.out + row_at + (wave * DB + db) * 32 + half_ * 8;
 #pragma unroll
-        for (int h = 0; h < C / 256; ++h) {
-          asm volatile("" : "+v"(o[j][h]));
-          o[j][h] *= inv[j];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) o[j][h][x] = inv[j] == 0 ? 0.f : o[j][h][x];   // of no keys: 0 times an infinity, it may be
-        }
-        if (e * 32 + (i + j) * 4 + wave >= count) continue;
-        const int64_t to_row = uniform(put[j]);
-#pragma unroll
-        for (int h = 0; h < C / 256; ++h) {
-          const int d = h * 256 + lane * 4;
-          if (parts) *(f32x4*)(pl.slot_part + to_row + d) = o[j][h];
-          else *(i32x2*)((uint16_t*)a.out + to_row + d) = i32x2{pack2<F16>(o[j][h][0], o[j][h][1]), pack2<F16>(o[j][h][2], o[j][h][3])};
-        }
+      for (int b = 0; b < 4; b += 2) {
+        const auto x = __builtin_amdgcn_permlane32_swap(pack2<F16>(o[4 * b], o[4 * b + 1]), pack2<F16>(o[4 * b + 4], o[4 * b + 5]), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(pack2<F16>(o[4 * b + 2], o[4 * b + 3]), pack2<F16>(o[4 * b + 6], o[4 * b + 7]), false, false);
+        *(i32x4*)(at + b * 8) = i32x4{(int32_t)x[0], (int32_t)y[0], (int32_t)x[1], (int32_t)y[1]};
       }
     }
-    barrier();
   }
   if (!any_odd) continue;
   __threadfence_block();
   __syncthreads();
   mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, row0, count, kbase, k1, alphas, [&](int32_t i, int32_t d) {
-    if (parts) pl.slot_part[goes[i] + d] = __builtin_nanf("");
+    if (parts) pl.slot_part[part_at<C>(to, i, d)] = __builtin_nanf("");
     else ((uint16_t*)a.out)[goes[i] + d] = F16 ? 0x7e00 : 0x7fc0;
   });
   }
@@ -1001,36 +1019,40 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
 // --------------------------------------------------------- k_latent_join ---
 
-// Rows in several parts, of the `each` rows at most of a block's cut.  Bound by the chain of its loads: a wave reads
-// eight parts at a time, their log sums with them, and WAVES waves share a row's parts where they are many.
+// Cut rows, of the `each` at most of a cut.  Bound by the chain of its loads: a wave reads eight parts at a time, their
+// log sums with them, and WAVES waves share parts where they are many.  A wave has a row of k_latent_rows, or
+// a 32nd of 32 rows of k_latent_tiles, as they lie.
 template <bool F16, int C, int ROWS, int WAVES>
 __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split pl, int32_t each) {
+  constexpr bool kTiles = ROWS != kFew;
   constexpr int kTurn = 8, kHalves = C / 256;
-  __shared__ float tops[4], totals[4];
+  __shared__ float tops[4][kWave], totals[4][kWave];
   __shared__ f32x4 outs[4][C / 4];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int32_t id = blockIdx.x * (4 / WAVES) + wave / WAVES, share = wave % WAVES;
-  const int32_t first = id / each, row = id % each;
-  const Cut at = (ROWS == kFew ? pl.row_cut : pl.slot_cut)[first];
-  if (row >= at.rows) return;         // all waves of the row
-  const float* const from = ROWS == kFew ? pl.row_part : pl.slot_part;
-  const float* const sums = ROWS == kFew ? pl.row_lse : pl.slot_lse;
+  const int32_t cut = id / each, piece = id % each;
+  const Cut at = (kTiles ? pl.slot_cut : pl.row_cut)[cut];
+  if ((kTiles ? piece / 32 * 32 : piece) >= at.rows) return;         // all waves of the rows
+  const int32_t row = kTiles ? piece / 32 * 32 + lane % 32 : piece;
+  const float* const from = (kTiles ? pl.slot_part : pl.row_part) +
+                            (kTiles ? (int64_t)(piece / 32 * 32) * C + piece % 32 * (kHalves * 256) : (int64_t)piece * C) + lane * 4;
+  const float* const sums = (kTiles ? pl.slot_lse : pl.row_lse) + row;
   float m = -INFINITY, sum = 0;
   f32x4 o[kHalves];
 #pragma unroll
   for (int h = 0; h < kHalves; ++h) o[h] = f32x4{0, 0, 0, 0};
-  const int32_t count = at.last - first + 1, mine = (count + WAVES - 1) / WAVES;
-  const int32_t p0 = first + share * mine, p1 = p0 + mine <= at.last ? p0 + mine : at.last + 1;
+  const int32_t count = at.last - at.block + 1, mine = (count + WAVES - 1) / WAVES;
+  const int32_t p0 = at.block + share * mine, p1 = p0 + mine <= at.last ? p0 + mine : at.last + 1;
   for (int32_t base = p0; base < p1; base += kTurn) {
     float x[kTurn];
     f32x4 y[kTurn][kHalves];
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) {
       const int32_t i = base + j < p1 ? base + j : p1 - 1;
-      const int64_t part = (2 * (int64_t)i + (i == first)) * ROWS + row;
+      const int64_t part = (2 * (int64_t)i + (i == at.block)) * ROWS;
       x[j] = sums[part];
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) y[j][h] = *(const f32x4*)(from + part * C + h * 256 + lane * 4);
+      for (int h = 0; h < kHalves; ++h) y[j][h] = *(const f32x4*)(from + part * C + h * 256);
     }
     float n = m;
 #pragma unroll
@@ -1050,30 +1072,32 @@ __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split 
     }
   }
   if constexpr (WAVES > 1) {
-    if (lane == 0) {
-      tops[wave] = m;
-      totals[wave] = sum;
-    }
+    tops[wave][lane] = m;
+    totals[wave][lane] = sum;
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) outs[wave][h * 64 + lane] = o[h];
     __syncthreads();
     if (wave) return;
 #pragma unroll
     for (int v = 1; v < WAVES; ++v) {
-      if (totals[v] == 0) continue;
-      const float n = fmaxf(m, tops[v]);
-      const float al = m == -INFINITY ? 0.f : exp2_(m - n), be = tops[v] == n ? 1.f : exp2_(tops[v] - n);
-      sum = sum * al + totals[v] * be;
+      const float top = tops[v][lane], total = totals[v][lane];
+      if (total == 0) continue;
+      const float n = fmaxf(m, top);
+      const float al = m == -INFINITY ? 0.f : exp2_(m - n), be = top == n ? 1.f : exp2_(top - n);
+      sum = sum * al + total * be;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) o[h] = o[h] * al + outs[v][h * 64 + lane] * be;
       m = n;
     }
   }
+  if (row >= at.rows) return;
   const float inv = sum == 0 ? 0.f : 1.f / sum;
   const int32_t t = at.first + (at.row + row) / pl.group, g = (at.row + row) % pl.group;
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h) store4<F16>(a, t, g, h * 256 + lane * 4, o[h] * inv);
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
+  for (int h = 0; h < kHalves; ++h)
+    store4<F16>(a, t, g, kTiles ? (piece % 32 * kHalves + h) * 8 + lane / 32 * 4 : h * 256 + lane * 4, o[h] * inv);
+  if (a.lse && (kTiles ? piece % 32 == 0 && lane < 32 : lane == 0))
+    a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }
 
 // -------------------------------------------------------------- dispatch ---
@@ -1098,6 +1122,7 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Split& pl) {
   const int64_t slots = (int64_t)a.tokens * pl.group / 128 + a.requests;
   pl.slots = slots < INT32_MAX ? (int32_t)slots : INT32_MAX;
   pl.even = slots <= kSlots;
+  pl.by_slot = slots < kBlocks;
   return ch;
 }
 
@@ -1117,7 +1142,7 @@ int64_t regions(int32_t value_dim, const pp_attention_args& a, const Choice& ch,
   if (ch.tiles && pl.even) {
     pl.slot_part = (float*)take((int64_t)2 * kBlocks * 128 * value_dim * 4);
     pl.slot_lse = (float*)take((int64_t)2 * kBlocks * 128 * 4);
-    pl.slot_cut = (Cut*)take(kBlocks * sizeof(Cut));
+    pl.slot_cut = (Cut*)take(kBlocks * sizeof(Cut));    // or one a slot, fewer
   }
   return at;
 }
@@ -1134,10 +1159,10 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl,
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (pl.even) {
-      const int32_t each = (int32_t)(most < 128 ? most : 128);
+      const int32_t each = most < 128 ? ((int32_t)most + 31) / 32 * 32 : 128, cuts = pl.by_slot ? pl.slots : kBlocks;
       // few slots are in many parts
-      if (pl.slots <= 64) k_latent_join<F16, C, 128, 4><<<kBlocks * each, 256, 0, st>>>(a, pl, each);
-      else k_latent_join<F16, C, 128, 1><<<kBlocks * each / 4, 256, 0, st>>>(a, pl, each);
+      if (pl.slots <= 64) k_latent_join<F16, C, 128, 4><<<cuts * each, 256, 0, st>>>(a, pl, each);
+      else k_latent_join<F16, C, 128, 1><<<cuts * each / 4, 256, 0, st>>>(a, pl, each);
       const hipError_t e2 = hipGetLastError();
       if (e2 != hipSuccess) return e2;
     }
