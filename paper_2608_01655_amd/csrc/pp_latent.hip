@@ -14,17 +14,23 @@
 
 #include "pp_attend.h"
 
+#include <algorithm>
+
 namespace pp {
 
 namespace {
 
 constexpr int kFew = 16;             // rows k_latent_rows takes
-constexpr int kRowsStart = 16;        // what a request's start and end cost it, in stages, and the least a block takes
-constexpr int kRowsShare = 8;
-constexpr int kTilesStart = 16;       // the same of k_latent_tiles, in steps of 32 keys
-constexpr int kTilesShare = 8;
 constexpr int kBlocks = 256;         // resident ones: one a CU
 constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into equal shares, and requests
+// What an item's start and end cost it, in tiles (stages of 16 or 32 keys, steps of 32), and the least that a block takes
+// of them.  A start takes k_latent_rows some 11 us beside 1 us a tile of a wave, and k_latent_tiles 20 us beside 1.7 us a
+// step.  With 4 and 8 (rows), 8 and 12 (tiles): 64 requests of 16 heads, 8 bits, 73 us where this takes 60, 48 requests of
+// 128 heads 112 for 87, 512 short requests 89 for 70.
+constexpr int kRowsStart = 16, kRowsShare = 8, kTilesStart = 16, kTilesShare = 8;
+// Keys that requests of few rows may have beside prompts and still go with them through k_latent_tiles: 32 single tokens
+// of 2,048 keys beside 512 new ones 87 us, with launches of their own 104; 16 of 16,384 365 for 362.
+constexpr int kAlone = 131072;
 
 // Rows that begin in block `block` and go on in the next ones up to `last`: `rows` of them from row `row` on of the
 // request whose tokens begin at `first` (rows 0: none).
@@ -951,7 +957,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
   // The rows' sums and where they go, from their waves to all.  What a lane holds goes out from its registers: parts
   // as they lie, 1 KB a store, and rows in pieces of 32 bytes (32 rows at a time through LDS, in whole lines,
-  // took 20,000 cycles where this takes XXX).
+  // took 20,000 cycles where this takes 14,000).
   // Numbers of lanes are made anew: what the loop would have to keep for here it has no registers for.
   const int lane_ = this_lane(), half_ = lane_ / 32, l32_ = lane_ % 32;
   l = over_halves(l, Sum());
@@ -1115,8 +1121,13 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Split& pl) {
     ch.rows = true;
   } else {
     ch.tiles = true;
-    // single tokens apart, unless every request has max_new tokens
-    ch.rows = pl.group <= kFew && (int64_t)a.requests * a.max_new != a.tokens;
+    // requests of few rows apart, unless every request has max_new tokens, or those that can be of few rows have few keys
+    if (pl.group <= kFew && (int64_t)a.requests * a.max_new != a.tokens) {
+      const int64_t few = kFew / pl.group;      // tokens; max_new is above it
+      const int64_t others = ((int64_t)a.tokens - few * a.requests + a.max_new - few - 1) / (a.max_new - few);
+      const int64_t keys = std::min((int64_t)a.max_len, (int64_t)a.max_blocks << pl.shift);
+      ch.rows = (a.requests - std::max<int64_t>(others, 0)) * keys > kAlone;
+    }
   }
   pl.few = ch.rows ? kFew : 0;
   const int64_t slots = (int64_t)a.tokens * pl.group / 128 + a.requests;

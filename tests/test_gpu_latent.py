@@ -95,6 +95,21 @@ def test_mixed_batches(window, dtype, cache, page, latent):
     check(c)
 
 
+@pytest.mark.parametrize("dtype,cache,page,latent", [(BF, BF, 16, 512), (HF, E4, 32, 512), (BF, E4, 64, 256), (HF, HF, 1024, 256)])
+@pytest.mark.parametrize("window", [0, 1, 50, 200])
+@pytest.mark.parametrize("heads", [16, 7])
+def test_mixed_batches_that_may_be_long(heads, window, dtype, cache, page, latent):
+    """Where the requests of few rows may have many keys they have launches of their own."""
+    new = [1, 33, 1, 0, 5, 1, 80, 2, 1]
+    length = [400, 433, 1, 77, 205, 64, 80, 300, 900]
+    c = case(new, length, heads, latent=latent, dtype=dtype, cache=cache, page=page, seed=window)
+    c["window"] = window
+    wide = torch.full((len(new), 200_000 // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c["table"].shape[1]] = c["table"]
+    c["table"] = wide
+    check(c, max_len=200_000)
+
+
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("new,heads,n", [(1, 16, 9000), (1, 128, 5000), (2, 20, 6001), (30, 16, 5000)])
 def test_long_requests_in_parts(new, heads, n, dtype, cache):
