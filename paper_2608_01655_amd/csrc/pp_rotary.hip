@@ -1,4 +1,10 @@
 // pp_rotary.hip -- norms, rotary positions and page writes in one pass (gfx950).
+//
+// y = x / sqrt(mean x^2 + eps) * weight, (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t), in 32 bits from
+// the rows' read to their one rounding.  Bound by memory: a row is read once and written once, 16 bytes a lane, whatever
+// is done to it between.  65,536 tokens of 32 query and 8 key heads of 128, half of each rotated, into 8-bit pages take
+// 283 us, 1.48 GB at 5.2 TB/s, what a large copy reaches; rotation and write in torch operations 4,350.  61 tokens of
+// 28 and 4 normed heads take 4.4 us, a chain of slot, row and store behind the launch, and 9.3 with the call's checks.
 
 #include "pp_rows.h"
 
@@ -251,7 +257,8 @@ hipError_t launch_rotary(const pp_rotary_args& a, const pp_kv_pages* pages, hipS
   w.amplitude = a.amplitude;
   w.groups = w.q.groups + w.k.groups + w.v.groups;
   const int64_t most = (int64_t)a.tokens * w.groups;
-  // a wave a group while there are few, so that a token's rows are not taken one after the other
+  // A wave a group while there are few, so that a token's rows are not taken one after the other; else 8,192 waves at least,
+  // and angles are worked out once a wave.
   int64_t each = most / 8192;
   w.each = (int32_t)(each < 1 ? 1 : each > w.groups ? w.groups : each);
   w.waves = (w.groups + w.each - 1) / w.each;
