@@ -117,6 +117,16 @@ __device__ __forceinline__ void mark_odd(const pp_kv_pages& p, const pp_attentio
   }
 }
 
+// The last block of an item that begins in block b and whose costs end before `end`.  At most 255 are between them, so the
+// quotient of floats is one off at most; a division of 64 bits takes a thousand cycles where its code is run once.
+__device__ __forceinline__ int32_t last_block(int64_t end, int64_t share, int32_t b) {
+  const int64_t behind = end - 1 - b * share;
+  int32_t n = (int32_t)((float)behind / (float)share);
+  if (n * share > behind) --n;
+  if ((n + 1) * share <= behind) ++n;
+  return b + n;
+}
+
 // -------------------------------------------------------- k_latent_rows ---
 
 template <bool NARROW, int C>
@@ -225,7 +235,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
     int64_t mine = 0, all;
     for (int32_t i = r0; i < r1; ++i) mine += item(i).cost;
     int64_t from = before(mine, all, sums);
-    share = uniform((all + gridDim.x - 1) / gridDim.x);
+    share = uniform((all + kBlocks - 1) / kBlocks);
     if (share < kRowsShare) share = kRowsShare;
     const int64_t x0 = blockIdx.x * share;
     if (x0 >= all) return;
@@ -282,7 +292,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
     const bool parts = !piece.first || !piece.last;
     const int64_t to = 2 * b + piece.first;
     if (piece.first && parts && threadIdx.x == 0)
-      pl.row_cut[b] = {b, (int32_t)((place + x.cost - 1) / share), q.first, 0, rows};
+      pl.row_cut[b] = {b, last_block(place + x.cost, share, b), q.first, 0, rows};
     const int32_t k0 = q.lo + piece.from * KEYS;
     const int64_t end = (int64_t)q.lo + (int64_t)piece.to * KEYS;
     const int32_t k1 = end < q.hi ? (int32_t)end : q.hi;
@@ -639,7 +649,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
       at += cost[e];
     }
     __syncthreads();
-    share = uniform((all + gridDim.x - 1) / gridDim.x);
+    share = uniform((all + kBlocks - 1) / kBlocks);
     if (share < kTilesShare / SUBS) share = kTilesShare / SUBS;
     const int64_t x0 = block * share;
     if (x0 >= all) return;
@@ -768,7 +778,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     }
   }
   if (cuts && threadIdx.x == 0)
-    pl.slot_cut[pl.by_slot ? slot : block] = {block, (int32_t)((place + x.tiles + kStart - 1) / share), q.first, row0, parts ? count : 0};
+    pl.slot_cut[pl.by_slot ? slot : block] = {block, last_block(place + x.tiles + kStart, share, block), q.first, row0, parts ? count : 0};
 
   // cleared by the matrix cores: 16 instructions instead of 256
   f32x16 acc[DB][4], zeros;
@@ -942,12 +952,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   for (uint32_t i = threadIdx.x * 16; i < Sh::kWeights; i += 4096) *LDS_PTR(i32x4, weights + Sh::kWeights + i) = i32x4{0, 0, 0, 0};
   if (threadIdx.x < 4) grown[4 + threadIdx.x] = 0;
   __builtin_amdgcn_sched_barrier(0);
+  if (pl.negative)
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    i32x4 y = __builtin_bit_cast(i32x4, qf[ks]);
-    y ^= pl.negative;
-    qf[ks] = __builtin_bit_cast(s16x8, y);
-  }
+    for (int ks = 0; ks < KS; ++ks) {
+      i32x4 y = __builtin_bit_cast(i32x4, qf[ks]);
+      y ^= pl.negative;
+      qf[ks] = __builtin_bit_cast(s16x8, y);
+    }
   wait_loads<0>();
   barrier();
   const int32_t steps = nt * SUBS, whole = sp.whole * SUBS, tail = sp.tail * SUBS;
