@@ -27,6 +27,7 @@ constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into 
 // of them.  A start takes k_latent_rows some 11 us beside 1 us a tile of a wave, and k_latent_tiles 20 us beside 1.7 us a
 // step.  With 4 and 8 (rows), 8 and 12 (tiles): 64 requests of 16 heads, 8 bits, 73 us where this takes 60, 48 requests of
 // 128 heads 112 for 87, 512 short requests 89 for 70.
+// A least share of 4 stages: lone requests of 4,097 and 16,384 keys 20.5 and 30.2 us, of 8 21.2 and 26.1 (fewer parts).
 constexpr int kRowsStart = 16, kRowsShare = 8, kTilesStart = 16, kTilesShare = 8;
 // Keys that requests of few rows may have beside prompts and still go with them through k_latent_tiles: 32 single tokens
 // of 2,048 keys beside 512 new ones 87 us, with launches of their own 104; 16 of 16,384 365 for 362.
