@@ -674,7 +674,10 @@ int pp_rotary_write(const pp_rotary_args *args, const pp_kv_pages *pages, void *
  * multiplied in, and out is yet to be multiplied by the values' expansion.
  * Pages: k the rows, v NULL, heads 1, k_scale [1] (PP_E4M3 pages);
  * value_dim 512 or 256, dim = value_dim + 64.  Everything else is as in
- * pp_paged_attention; out rows are [tokens][q_heads][value_dim]. */
+ * pp_paged_attention; out rows are [tokens][q_heads][value_dim].  A key of
+ * s_j = -infinity makes elements of out NaN where its own are not finite (0
+ * times them), unless the row sees no other keys, wherever the call cuts
+ * requests. */
 int64_t pp_latent_workspace(const pp_kv_pages *pages, int32_t value_dim,
                             const pp_attention_args *args);
 int pp_latent_attention(const pp_kv_pages *pages, int32_t value_dim,

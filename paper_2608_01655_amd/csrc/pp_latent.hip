@@ -73,7 +73,10 @@ struct Latent {
 // What a row does not see does not touch it, whatever it holds.  In tiles that some row does not see whole, elements
 // that are not finite are set to 0 in LDS between the scores and the values.  A row that sees one has a score of
 // NaN or +infinity from it, and is NaN whole by its sum, or of -infinity, and then that element's weight of 0
-// times an infinity makes it NaN: so mark_odd sets the row's element to NaN once it is stored.
+// times an infinity makes it NaN: so mark_odd sets the row's element to NaN once it is stored.  In tiles seen whole
+// the product itself does.  A row of which a wave or a block has seen nothing but scores of -infinity leaves 0 or such NaN
+// there, which is added up with a factor of 0, so that where the batch is cut does not matter; the row is 0 only where that is
+// all it has seen.
 template <bool F16, bool NARROW>
 __device__ __forceinline__ bool clean16(uint32_t at) {
   u32x4 x = *LDS_PTR(u32x4, at);
@@ -94,7 +97,8 @@ __device__ __forceinline__ bool clean16(uint32_t at) {
   return any != 0;
 }
 
-// Rows row0 .. row0 + count - 1 of request r, keys k0 .. k1 - 1; sums: the rows' sums, 0 where nothing is seen.
+// Rows row0 .. row0 + count - 1 of request r, keys k0 .. k1 - 1; sums: 0 for rows that stay as they are (of nothing but
+// scores of -infinity, where that is known).
 // `put` sets a row's element d to NaN.  All threads of the block, behind the rows' stores.
 template <bool F16, bool NARROW, int C, class Put>
 __device__ __forceinline__ void mark_odd(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, int32_t r, int32_t start,
@@ -137,7 +141,7 @@ struct LatentRows : Latent<NARROW, C> {
   static constexpr int kNS = C == 512 ? 2 : 3;              // stages of a wave's ring
   static constexpr int kRing = kNW * kNS * L::kStage;
   static constexpr int kRow = C + 4;                        // floats of a joined row
-  static constexpr int kJoin = kNW * 16 * (kRow + 3) * 4;
+  static constexpr int kJoin = (kNW * 16 * (kRow + 3) + 16) * 4;
   static constexpr int kLds = kRing > kJoin ? kRing : kJoin;
 };
 
@@ -439,8 +443,9 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
 #pragma unroll
     for (int db = 0; db < DB; ++db) *(f32x4*)&js[(wave * 16 + i16) * Sh::kRow + db * 16 + grp * 4] = acc[db];
     __syncthreads();
-    // a factor for each wave's part of each row, 0 where it saw nothing
+    // a factor for each wave's part of each row, 0 where it saw nothing, and the rows' sums
     float* const jf = jl + NW * 16;                  // [16][NW]
+    float* const jt = jf + NW * 16;                  // [16]
     if (threadIdx.x < NW * 16) {
       const int w = threadIdx.x / 16, row = i16;
       float mm = -INFINITY, ll = 0;
@@ -453,6 +458,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
       }
       const float mw = jm[w * 16 + row];
       jf[row * NW + w] = jl[w * 16 + row] == 0 ? 0.f : (mw == mm ? 1.f : exp2_((mw - mm) * c)) * (vs / ll);
+      if (w == 0) jt[row] = parts ? 1.f : ll;        // what is 0 in a part need not be 0
       if (w == 0 && row < rows) {
         const float lse = ll == 0 ? -INFINITY : mm * c + (__log2f(ll) - kLift<F16>);
         if (parts) pl.row_lse[to * kFew + row] = lse;
@@ -466,24 +472,15 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
       const f32x4 f = *(const f32x4*)&jf[row * NW];
       f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        // a wave that saw nothing may hold anything
-        const f32x4 y = *(const f32x4*)&js[(w * 16 + row) * Sh::kRow + d];
-        o += f[w] == 0 ? f32x4{0, 0, 0, 0} : f[w] * y;
-      }
+      for (int w = 0; w < NW; ++w) o += f[w] * *(const f32x4*)&js[(w * 16 + row) * Sh::kRow + d];
+      if (jt[row] == 0) o = f32x4{0, 0, 0, 0};
       if (parts) *(f32x4*)&pl.row_part[(to * kFew + row) * C + d] = o;
       else store4<F16>(a, q.first + row / G, row % G, d, o);
     }
     if (!any_odd) continue;
-    __syncthreads();
-    if (threadIdx.x < 16) {
-      float sum = 0;
-      for (int w = 0; w < NW; ++w) sum += jl[w * 16 + threadIdx.x];
-      js[threadIdx.x] = sum;
-    }
     __threadfence_block();
     __syncthreads();
-    mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, 0, rows, k0, k1, js, [&](int32_t i, int32_t d) {
+    mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, 0, rows, k0, k1, jt, [&](int32_t i, int32_t d) {
       if (parts) pl.row_part[(to * kFew + i) * C + d] = __builtin_nanf("");
       else ((uint16_t*)a.out)[(q.first + i / G) * a.out_token_stride + i % G * a.out_head_stride + d] = F16 ? 0x7e00 : 0x7fc0;
     });
@@ -989,7 +986,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   float* const inverse = (float*)(goes + 128);                       // [128]
   if (half_ == 0) {
     const int32_t i = wave * 32 + l32_, row_ = row0 + i;
-    alphas[i] = l;
+    alphas[i] = parts ? 1.f : l;           // what is 0 in a part need not be 0
     inverse[i] = l == 0 ? 0.f : vs / l;
     if (row_ < rows) {
       const int32_t tok_ = row_ / G, g_ = row_ % G;
@@ -1017,7 +1014,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     });
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[j] *= inv;
-    if (__any(inv == 0)) {              // of no keys: 0 times an infinity, it may be
+    if (!parts && __any(inv == 0)) {    // of nothing but scores of -infinity: NaN, it may be
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[j] = inv == 0 ? 0.f : o[j];
     }
@@ -1094,8 +1091,8 @@ __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split 
     m = n;
 #pragma unroll
     for (int j = 0; j < kTurn; ++j) {
-      if (base + j >= p1 || x[j] == -INFINITY) continue;   // a part that saw nothing may hold anything
-      const float w = x[j] == n ? 1.f : exp2_(x[j] - n);
+      if (base + j >= p1) continue;
+      const float w = x[j] == -INFINITY ? 0.f : x[j] == n ? 1.f : exp2_(x[j] - n);   // a part that saw nothing is 0 or NaN
       sum += w;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) o[h] += w * y[j][h];
@@ -1111,9 +1108,8 @@ __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split 
 #pragma unroll
     for (int v = 1; v < WAVES; ++v) {
       const float top = tops[v][lane], total = totals[v][lane];
-      if (total == 0) continue;
       const float n = fmaxf(m, top);
-      const float al = m == -INFINITY ? 0.f : exp2_(m - n), be = top == n ? 1.f : exp2_(top - n);
+      const float al = m == -INFINITY ? 0.f : exp2_(m - n), be = total == 0 ? 0.f : top == n ? 1.f : exp2_(top - n);
       sum = sum * al + total * be;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) o[h] = o[h] * al + outs[v][h * 64 + lane] * be;
@@ -1125,7 +1121,8 @@ __global__ void __launch_bounds__(256) k_latent_join(pp_attention_args a, Split 
   const int32_t t = at.first + (at.row + row) / pl.group, g = (at.row + row) % pl.group;
 #pragma unroll
   for (int h = 0; h < kHalves; ++h)
-    store4<F16>(a, t, g, kTiles ? (piece % 32 * kHalves + h) * 8 + lane / 32 * 4 : h * 256 + lane * 4, o[h] * inv);
+    store4<F16>(a, t, g, kTiles ? (piece % 32 * kHalves + h) * 8 + lane / 32 * 4 : h * 256 + lane * 4,
+                sum == 0 ? f32x4{0, 0, 0, 0} : o[h] * inv);
   if (a.lse && (kTiles ? piece % 32 == 0 && lane < 32 : lane == 0))
     a.lse[(int64_t)t * a.q_heads + g] = sum == 0 ? -INFINITY : (m + __log2f(sum)) / kLog2e;
 }

@@ -1,0 +1,48 @@
+"""Attention over pages of latent rows where keys that are not finite meet the cuts of a batch."""
+
+import math
+
+import pytest
+import torch
+
+from tests import rows_ref as R
+from tests.test_gpu_latent import attend, case, check, close, put
+
+pytestmark = pytest.mark.gpu
+BF, HF, E4 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+@pytest.fixture(autouse=True)
+def _say_case(request):
+    print(f"\n[case] {request.node.name}", flush=True)
+    yield
+
+
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("others", [0, 5])
+@pytest.mark.parametrize("new,heads,n,first,dead", [
+    (1, 16, 128, 0, 32), (1, 16, 128, 96, 32), (1, 16, 100, 96, 4), (1, 16, 9000, 0, 128), (1, 16, 9000, 512, 16), (3, 5, 60, 0, 48),
+    (1, 128, 3000, 0, 256), (1, 128, 3000, 300, 900), (1, 128, 3000, 2990, 10), (40, 16, 6000, 0, 700), (40, 16, 6000, 5950, 20),
+    (100, 16, 100, 0, 40), (100, 16, 700, 600, 70)])
+def test_runs_of_minus_infinity(new, heads, n, first, dead, others, dtype, latent):
+    """Keys that score -infinity from an infinite element, whole tiles, waves' shares and parts of them: the element
+    is 0 times an infinity and so NaN in every row that sees one and another key, wherever the batch is cut; rows that
+    see no other key are 0."""
+    c = case([new] + [1] * others, [n] + [400] * others, heads, latent=latent, dtype=dtype, cache=dtype, seed=20)
+    c["q"].abs_().add_(0.01)
+    put(c, 0, range(first, first + dead), -math.inf, slice(5, 6))
+    want = R.latent(c["q"], c["cache"], c["table"], c["begin"], c["length"], latent, scale=c["scale"])[0]
+    assert bool(torch.isnan(want[new - 1, :, 5]).all()) and int(torch.isnan(want).sum()) <= new * heads
+    check(c)
+
+
+@pytest.mark.parametrize("new,heads,n,window", [(1, 16, 9000, 300), (2, 128, 3000, 700), (40, 16, 6000, 500)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_runs_of_minus_infinity_in_a_window(dtype, new, heads, n, window):
+    """The same at a window's edge: rows whose window is past them are finite."""
+    c = case([new], [n], heads, dtype=dtype, cache=dtype, seed=21)
+    c["q"].abs_().add_(0.01)
+    c["window"] = window
+    put(c, 0, range(n - window - 200, n - window + 1), -math.inf, slice(5, 6))
+    check(c)
