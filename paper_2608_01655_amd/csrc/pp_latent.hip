@@ -132,6 +132,9 @@ __device__ __forceinline__ int32_t last_block(int64_t end, int64_t share, int32_
   return b + n;
 }
 
+// What scores are multiplied by in the exponent: above 0 whatever the scales, so that -infinity times it is still that.
+__device__ __forceinline__ float exponent_of(const Plan& pl, float k_scale) { return fmaxf(pl.c * k_scale, 0x1p-126f); }
+
 // -------------------------------------------------------- k_latent_rows ---
 
 template <bool NARROW, int C>
@@ -260,7 +263,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
   }
 
   const float vs = NARROW && p.k_scale ? p.k_scale[0] : 1.f;
-  const float c = pl.c * vs;
+  const float c = exponent_of(pl, vs);
   const int64_t es = NARROW ? 1 : 2;
   const int64_t page_b = p.page_stride * es;
   const uint32_t tok_b = (uint32_t)(p.token_stride * es);
@@ -716,7 +719,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   barrier();                          // the last piece's sums are read
 
   const float vs = NARROW && p.k_scale ? p.k_scale[0] : 1.f;
-  const float c = pl.c * vs;
+  const float c = exponent_of(pl, vs);
 
   const int64_t es = NARROW ? 1 : 2;
   const int64_t page_b = p.page_stride * es;
@@ -1234,8 +1237,7 @@ hipError_t launch_latent(const pp_kv_pages& p, int32_t value_dim, const pp_atten
   const Choice ch = choose(p, a, pl);
   regions(value_dim, a, ch, pl);
   pl.negative = a.scale < 0 ? (int32_t)0x80008000 : 0;     // the queries' signs
-  // a scale of 0 is held above it, so that -infinity times it is still that
-  pl.c = std::fmax(std::fabs(a.scale) * kLog2e, 0x1p-126f);
+  pl.c = std::fabs(a.scale) * kLog2e;
   const bool narrow = p.dtype == PP_E4M3;
   if (a.dtype == PP_F16) return narrow ? go_dim<true, true>(p, value_dim, a, pl, ch, st) : go_dim<true, false>(p, value_dim, a, pl, ch, st);
   return narrow ? go_dim<false, true>(p, value_dim, a, pl, ch, st) : go_dim<false, false>(p, value_dim, a, pl, ch, st);

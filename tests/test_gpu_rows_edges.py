@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+from paper_2608_01655_amd import binding as B
 from tests import rows_ref as R
 from tests.test_gpu_latent import attend, case, check, close, put
 
@@ -45,4 +46,14 @@ def test_runs_of_minus_infinity_in_a_window(dtype, new, heads, n, window):
     c["q"].abs_().add_(0.01)
     c["window"] = window
     put(c, 0, range(n - window - 200, n - window + 1), -math.inf, slice(5, 6))
+    check(c)
+
+
+@pytest.mark.parametrize("scale,k_scale", [(0.0, 1e-8), (0.0, 1e-38), (1e-30, 1e-20), (-1e-36, 1e-9)])
+@pytest.mark.parametrize("new,heads", [(1, 16), (30, 16)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_scales_whose_product_vanishes(dtype, new, heads, scale, k_scale):
+    """Scores of next to nothing: every key that is seen has the same weight, others none."""
+    c = case([new] * 2, [200, 3000], heads, dtype=dtype, cache=E4, seed=22)
+    c["scale"], c["ks"] = scale, torch.full((1,), k_scale, device="cuda")
     check(c)
