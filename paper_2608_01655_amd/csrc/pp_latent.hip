@@ -97,16 +97,28 @@ __device__ __forceinline__ bool clean16(uint32_t at) {
   return any != 0;
 }
 
-// Rows row0 .. row0 + count - 1 of request r, keys k0 .. k1 - 1; sums: 0 for rows that stay as they are (of nothing but
-// scores of -infinity, where that is known).
-// `put` sets a row's element d to NaN.  All threads of the block, behind the rows' stores.
-template <bool F16, bool NARROW, int C, class Put>
+// Whether some row sees a key of a tile that not all of them see: only such keys are odd, so that what lies behind the
+// last token, or before a window, costs no time.
+__device__ __forceinline__ bool seen_at_all(int32_t key, int32_t pos_lo, int32_t k1, int32_t window) {
+  return (uint32_t)key < (uint32_t)k1 && (window == 0 || (int64_t)key > (int64_t)pos_lo - window);
+}
+
+// Rows row0 .. row0 + count - 1 of request r, keys k0 .. k1 - 1 of tiles of N, of which all rows see tiles sp.whole .. sp.tail - 1;
+// sums: 0 for rows that stay as they are (of nothing but scores of -infinity, where that is known).
+// `put` sets a row's element d to NaN.  All threads of the block, behind the rows' stores.  A walk over all of the keys took a batch
+// of 64 requests of 16,001 keys and NaN behind each from 225 us to 5 ms.
+template <bool F16, bool NARROW, int C, int N, class Put>
 __device__ __forceinline__ void mark_odd(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, int32_t r, int32_t start,
-                                         int32_t row0, int32_t count, int32_t k0, int32_t k1, const float* sums, Put&& put) {
+                                         int32_t row0, int32_t count, int32_t k0, int32_t k1, const Span3& sp, const float* sums, Put&& put) {
   const int32_t* blocks = a.block_table + r * a.row_stride;
   const int64_t es = NARROW ? 1 : 2;
 #pragma unroll 1
   for (int32_t key = k0; key < k1; ++key) {
+    const int32_t tile = (key - k0) / N;
+    if (tile >= sp.whole && tile < sp.tail) {      // to the last key of the tiles seen whole
+      key = k0 + (sp.tail * N - 1);
+      continue;
+    }
     const char* from = (const char*)p.k + page_of(p, a, pl, blocks, key) * p.page_stride * es +
                        (int64_t)(key & (p.page_size - 1)) * p.token_stride * es;
 #pragma unroll 1
@@ -392,8 +404,11 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
         }
         wait_lds();
 #pragma unroll 1
-        for (int i = lane; i < KEYS * (C * (int)es / 16); i += kWave)
-          odd |= clean16<F16, NARROW>(in + i / (C * (int)es / 16) * RB + i % (C * (int)es / 16) * 16);
+        for (int i = lane; i < KEYS * (C * (int)es / 16); i += kWave) {
+          const int row = i / (C * (int)es / 16);
+          odd |= clean16<F16, NARROW>(in + row * RB + i % (C * (int)es / 16) * 16) &&
+                 seen_at_all(kbase + t * KEYS + row, pos_lo, k1, a.window);
+        }
         wait_lds();
       }
       float mx = y[0];
@@ -483,7 +498,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attent
     if (!any_odd) continue;
     __threadfence_block();
     __syncthreads();
-    mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, 0, rows, k0, k1, jt, [&](int32_t i, int32_t d) {
+    const Span3 all = spans<KEYS>(k0, tiles, pos_lo, pos_hi, k1, a.window);
+    mark_odd<F16, NARROW, C, KEYS>(p, a, pl, r, q.start, 0, rows, k0, k1, all, jt, [&](int32_t i, int32_t d) {
       if (parts) pl.row_part[(to * kFew + i) * C + d] = __builtin_nanf("");
       else ((uint16_t*)a.out)[(q.first + i / G) * a.out_token_stride + i % G * a.out_head_stride + d] = F16 ? 0x7e00 : 0x7fc0;
     });
@@ -866,10 +882,13 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   // Between a step's scores and its values, this wave's quarter of keys that some row does not see whole.
   constexpr int kQuarter = C / 4 * (NARROW ? 1 : 2) / 16;      // units
   bool odd = false;
-  auto clean = [&](uint32_t at) {
+  auto clean = [&](uint32_t at, int32_t key0) {
 #pragma unroll 1
-    for (int i = this_lane(); i < 32 * kQuarter; i += kWave)
-      odd |= clean16<F16, NARROW>(lds + at + i / kQuarter * RB + (wave * kQuarter + i % kQuarter) * 16);
+    for (int i = this_lane(); i < 32 * kQuarter; i += kWave) {
+      const int row = i / kQuarter;
+      odd |= clean16<F16, NARROW>(lds + at + row * RB + (wave * kQuarter + i % kQuarter) * 16) &&
+             seen_at_all(key0 + row, pos_lo, k1, a.window);
+    }
     wait_lds();
   };
 
@@ -973,7 +992,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
     if (u == steps) break;
     if (SUBS == 1 || (u & 1)) wait_loads<0>();
     barrier();
-    if (masked) clean(next);
+    if (masked) clean(next, kbase + u * 32);
     cur = next;
   }
   wait_loads<0>();
@@ -1039,7 +1058,7 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
   if (!any_odd) continue;
   __threadfence_block();
   __syncthreads();
-  mark_odd<F16, NARROW, C>(p, a, pl, r, q.start, row0, count, kbase, k1, alphas, [&](int32_t i, int32_t d) {
+  mark_odd<F16, NARROW, C, TK>(p, a, pl, r, q.start, row0, count, kbase, k1, spans<TK>(kbase, nt, pos_lo, pos_hi, k1, a.window), alphas, [&](int32_t i, int32_t d) {
     if (parts) pl.slot_part[part_at<C>(to, i, d)] = __builtin_nanf("");
     else ((uint16_t*)a.out)[goes[i] + d] = F16 ? 0x7e00 : 0x7fc0;
   });

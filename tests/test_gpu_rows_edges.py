@@ -57,3 +57,41 @@ def test_scales_whose_product_vanishes(dtype, new, heads, scale, k_scale):
     c = case([new] * 2, [200, 3000], heads, dtype=dtype, cache=E4, seed=22)
     c["scale"], c["ks"] = scale, torch.full((1,), k_scale, device="cuda")
     check(c)
+
+
+def least_time(c, calls=10):
+    """Microseconds of a call, the least of a few turns."""
+    ws = torch.empty(B.pp_latent_workspace(c["q"], c["cache"], c["table"], c["latent"], max_new=c["max_new"], max_len=c["max_len"],
+                                           window=c["window"]), dtype=torch.uint8, device="cuda")
+    least = math.inf
+    for _ in range(6):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(calls):
+            attend(c, workspace=ws)
+        b.record()
+        torch.cuda.synchronize()
+        least = min(least, a.elapsed_time(b) / calls * 1e3)
+    return least
+
+
+@pytest.mark.parametrize("cache", [BF, E4])
+@pytest.mark.parametrize("new,heads,n,requests,window", [(1, 16, 16_001, 64, 0), (1, 128, 6001, 48, 0), (200, 16, 8_203, 6, 0),
+                                                         (1, 16, 16_001, 64, 9_000), (200, 16, 8_203, 6, 3_000)])
+def test_what_is_not_seen_costs_no_time(new, heads, n, requests, window, cache):
+    """NaN behind the last token and before a window is not looked at key by key: a call takes what it takes
+    without (a walk over all keys of a share took many times as long)."""
+    c = case([new] * requests, [n] * requests, heads, cache=cache, seed=23)
+    c["window"] = window
+    clean = least_time(c)
+    want = [x.clone() for x in attend(c)]
+    for r in range(requests):
+        hidden = list(range(n, -(-n // 16) * 16))
+        if window:
+            hidden += range(n - new - window - 100, n - new - window + 1)
+        put(c, r, hidden, math.nan)
+    spoilt = least_time(c)
+    got = attend(c)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    print(f"{clean:.1f} us, {spoilt:.1f} with NaN", flush=True)
+    assert spoilt < 2 * clean + 20
