@@ -262,8 +262,6 @@ hipError_t launch_rotary(const pp_rotary_args& a, const pp_kv_pages* pages, hipS
   int64_t each = most / 8192;
   w.each = (int32_t)(each < 1 ? 1 : each > w.groups ? w.groups : each);
   w.waves = (w.groups + w.each - 1) / w.each;
-  const int64_t grid = ((int64_t)a.tokens * w.waves + 3) / 4;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   pp_kv_pages p{};
   if (pages) {
     p = *pages;
@@ -273,8 +271,21 @@ hipError_t launch_rotary(const pp_rotary_args& a, const pp_kv_pages* pages, hipS
   auto kern = !pages ? (f16 ? k_rotary<true, false, false> : k_rotary<false, false, false>)
               : narrow ? (f16 ? k_rotary<true, true, true> : k_rotary<false, true, true>)
                        : (f16 ? k_rotary<true, false, true> : k_rotary<false, false, true>);
-  kern<<<(unsigned)grid, 256, 0, st>>>(w, p);
-  return hipGetLastError();
+  // as many tokens at a time as a launch takes (waves are few where there are more)
+  const int64_t turn = most_blocks(256) * 4 / w.waves;
+  for (int64_t t = 0; t < a.tokens; t += turn) {
+    w.tokens = (int32_t)(a.tokens - t < turn ? a.tokens - t : turn);
+    kern<<<(unsigned)(((int64_t)w.tokens * w.waves + 3) / 4), 256, 0, st>>>(w, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    for (Rows* r : {&w.q, &w.k, &w.v}) {
+      if (r->in) r->in += turn * r->token;
+      if (r->out) r->out += turn * r->out_token;
+    }
+    if (w.position) w.position += turn;
+    if (w.slot) w.slot += turn;
+  }
+  return hipSuccess;
 }
 
 }  // namespace pp

@@ -18,6 +18,9 @@ namespace pp {
 constexpr int kLine = 16;
 constexpr int kHop = 14;
 
+// Blocks that one launch takes: threads past 2^32 are left out, and no error says so.
+constexpr int64_t most_blocks(int threads) { return 0xffffffff / threads; }
+
 // What has to succeed once on each GPU.  A failure is tried again by the next call; two threads may
 // both come through the first time.
 class OnEachGpu {

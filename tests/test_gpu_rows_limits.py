@@ -1,0 +1,43 @@
+"""The operators around the pages at sizes past what one launch takes (2^32 threads)."""
+
+import pytest
+import torch
+
+from paper_2608_01655_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def _say_case(request):
+    print(f"\n[case] {request.node.name}", flush=True)
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_more_tokens_than_a_launch_takes(paged):
+    """2^26 tokens and a few: the bits of a call a piece of them."""
+    T, D = 2 ** 26 + 5, 16
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=BF)  # noqa: E731
+    q, k, v = rand(T, 1, D), rand(T, 1, D), rand(T, 1, D)
+    weight, turns = 1 + rand(D) / 8, torch.from_numpy(B.pp_rotary_turns(D)).cuda()
+    position = torch.randint(0, 10 ** 6, (T,), generator=g, device="cuda", dtype=torch.int32)
+    pages = -(-T // 16)
+    place = pages * 16 - 1 - torch.arange(T, device="cuda")
+
+    def call(pieces):
+        out = torch.zeros_like(q)
+        to = torch.zeros((2, pages, 1, 16, D), device="cuda", dtype=BF) if paged else torch.zeros_like(k)
+        for i in range(pieces):
+            s = slice(i * T // pieces, (i + 1) * T // pieces)
+            kw = dict(v=v[s], slot_map=place[s], k_cache=to[0], v_cache=to[1]) if paged else dict(k_out=to[s])
+            B.pp_rotary_write(position[s], turns, q=q[s], q_out=out[s], k=k[s], q_weight=weight, k_weight=weight, **kw)
+        torch.cuda.synchronize()
+        return out, to
+
+    for a, b in zip(call(1), call(3)):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+        assert bool((a[-1] != 0).any())
