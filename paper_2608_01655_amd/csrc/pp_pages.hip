@@ -317,11 +317,7 @@ __global__ void __launch_bounds__(1024) k_list(pp_free_args a) {
 hipError_t launch_page_copy(const pp_copy_args& a, hipStream_t st) {
   const int32_t size = a.dtype == PP_E4M3 ? 1 : 2;
   Copy c{};
-  c.source = a.source;
-  c.target = a.target;
-  c.tokens = a.tokens;
   c.page = a.page_stride * size;
-  c.moves = a.moves;
   c.n_pages = a.n_pages;
   c.page_size = a.page_size;
   c.units = a.dim * size / 16;
@@ -334,14 +330,21 @@ hipError_t launch_page_copy(const pp_copy_args& a, hipStream_t st) {
   c.dense = (c.inners == 1 || c.inner == c.units * 16) && (c.outers == 1 || c.outer == (int64_t)c.inners * c.units * 16);
   const int64_t all = (int64_t)c.outers * c.inners * c.units;
   c.blocks = (int32_t)((all + kCopyUnits - 1) / kCopyUnits);
-  for (int32_t at = 0; at < a.n_pools; at += kPools) {
-    const int32_t n = a.n_pools - at < kPools ? a.n_pools - at : kPools;
-    for (int32_t i = 0; i < n; ++i) c.pools[i] = (char*)a.pools[at + i];
-    const int64_t grid = (int64_t)c.blocks * a.moves * n;
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    k_copy<<<(unsigned)grid, 256, 0, st>>>(c);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  // as many moves, and then pools, at a time as a launch takes (a page has 2^16 blocks at most)
+  const int64_t most = most_blocks(256) / c.blocks;
+  for (int64_t move = 0; move < a.moves; move += most) {
+    c.moves = (int32_t)(a.moves - move < most ? a.moves - move : most);
+    c.source = a.source + move;
+    c.target = a.target + move;
+    c.tokens = a.tokens ? a.tokens + move : nullptr;
+    const int32_t turn = most / c.moves < kPools ? (int32_t)(most / c.moves) : kPools;
+    for (int32_t at = 0; at < a.n_pools; at += turn) {
+      const int32_t n = a.n_pools - at < turn ? a.n_pools - at : turn;
+      for (int32_t i = 0; i < n; ++i) c.pools[i] = (char*)a.pools[at + i];
+      k_copy<<<(unsigned)((int64_t)c.blocks * c.moves * n), 256, 0, st>>>(c);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   return hipSuccess;
 }

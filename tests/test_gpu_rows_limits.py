@@ -6,7 +6,7 @@ import torch
 from paper_2608_01655_amd import binding as B
 
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+BF, E4 = torch.bfloat16, torch.float8_e4m3fn
 
 
 @pytest.fixture(autouse=True)
@@ -41,3 +41,17 @@ def test_more_tokens_than_a_launch_takes(paged):
     for a, b in zip(call(1), call(3)):
         assert torch.equal(a.view(torch.int16), b.view(torch.int16))
         assert bool((a[-1] != 0).any())
+
+
+@pytest.mark.parametrize("pools,moves", [(129, 131_073), (1, 2 ** 24 + 3)])
+def test_more_moves_than_a_launch_takes(pools, moves):
+    """Past 2^24 pages in all pools, and in one."""
+    n_pages = 2 * moves + 1
+    g = torch.Generator(device="cuda").manual_seed(2)
+    pool = torch.randint(0, 120, (pools, n_pages, 1, 16, 16), generator=g, device="cuda", dtype=torch.uint8)
+    source = 2 * torch.arange(moves, device="cuda", dtype=torch.int32)
+    want = pool.clone()
+    want[:, 1:2 * moves:2] = pool[:, 0:2 * moves:2]
+    B.pp_page_copy(list(pool.view(E4)), source, source + 1)
+    torch.cuda.synchronize()
+    assert torch.equal(pool, want)
