@@ -934,8 +934,9 @@ hipError_t go_rows(const pp_kv_pages& p, const pp_attention_args& a, const Plan&
   const hipError_t ok = allow_lds(once, &k_rows<F16, NARROW, D, RT>, lds);
   if (ok != hipSuccess) return ok;
   const int64_t grid = (int64_t)a.requests * pl.parts_rows * p.heads;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_rows<F16, NARROW, D, RT><<<(unsigned)grid, kWave * RowsShape<NARROW, D, RT>::kNW, lds, st>>>(p, a, pl);
+  constexpr int threads = kWave * RowsShape<NARROW, D, RT>::kNW;
+  if (grid > most_blocks(threads)) return hipErrorInvalidConfiguration;
+  k_rows<F16, NARROW, D, RT><<<(unsigned)grid, threads, lds, st>>>(p, a, pl);
   return hipGetLastError();
 }
 
@@ -947,7 +948,7 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, 
     const hipError_t ok = allow_lds(once, &k_tiles<F16, NARROW, D>, lds);
     if (ok != hipSuccess) return ok;
     const int64_t grid = (int64_t)pl.slots * pl.parts_tiles * p.heads;
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (grid > most_blocks(256)) return hipErrorInvalidConfiguration;
     k_tiles<F16, NARROW, D><<<(unsigned)grid, 256, lds, st>>>(p, a, pl);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -965,6 +966,7 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Plan& pl, 
       few_rows = (int64_t)a.max_new * pl.group < pl.few ? (int64_t)a.max_new * pl.group : pl.few;
       waves = (int64_t)a.requests * p.heads * ((few_rows + kRows - 1) / kRows);
     }
+    if ((waves + 3) / 4 > most_blocks(256)) return hipErrorInvalidConfiguration;
     k_join<F16, D><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, pl, (int32_t)few_rows, p.heads);
     e = hipGetLastError();
   }

@@ -1209,6 +1209,7 @@ hipError_t go(const pp_kv_pages& p, const pp_attention_args& a, const Split& pl,
     static OnEachGpu once;
     const hipError_t ok = allow_lds(once, &k_latent_tiles<F16, NARROW, C>, lds);
     if (ok != hipSuccess) return ok;
+    if (!pl.even && pl.slots > most_blocks(256)) return hipErrorInvalidConfiguration;
     k_latent_tiles<F16, NARROW, C><<<pl.even ? kBlocks : pl.slots, 256, lds, st>>>(p, a, pl);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

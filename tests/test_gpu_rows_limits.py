@@ -55,3 +55,19 @@ def test_more_moves_than_a_launch_takes(pools, moves):
     B.pp_page_copy(list(pool.view(E4)), source, source + 1)
     torch.cuda.synchronize()
     assert torch.equal(pool, want)
+
+
+@pytest.mark.parametrize("max_new,heads", [(1, 272), (100, 272)])
+def test_attention_of_more_blocks_than_a_launch_takes(max_new, heads):
+    """65,536 requests of 272 key heads are refused, not done in part."""
+    R, D = 65_536, 64
+    q = torch.zeros((R, heads, D), device="cuda", dtype=BF)
+    out = torch.full_like(q, 7)
+    pages = torch.zeros((1, heads, 16, D), device="cuda", dtype=BF)
+    table, length = (torch.zeros(s, device="cuda", dtype=torch.int32) for s in ((R, 1), (R,)))
+    with pytest.raises(B.PPError) as e:
+        B.pp_paged_attention(q, pages, pages, table, torch.arange(R + 1, device="cuda", dtype=torch.int32), length + 1, out,
+                             scale=0.1, max_new=max_new, max_len=16)
+    assert e.value.code == B.PP_E_DEVICE
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
