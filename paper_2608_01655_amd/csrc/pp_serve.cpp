@@ -147,6 +147,24 @@ int check_rotary_rows(int32_t tokens, int32_t heads, int32_t dim, int32_t first,
   return PP_OK;
 }
 
+// Whether rows of out_table and of block_table have entries in common.  Rows of one may lie between the other's.
+bool tables_meet(const pp_fork_args& a) {
+  const __int128 n = (__int128)4 * a.max_blocks, in_step = (__int128)4 * a.row_stride, out_step = (__int128)4 * a.out_row_stride;
+  const __int128 first = (__int128)(uintptr_t)a.out_table - (uintptr_t)a.block_table, last = in_step * (a.parents - 1);
+  if (first >= last + n || first + out_step * (a.rows - 1) + n <= 0) return false;
+  if (in_step == out_step && in_step) {                      // all rows alike, so one tells
+    const __int128 at = (first % in_step + in_step) % in_step;
+    if (at >= n && at + n <= in_step) return false;
+  }
+  for (int32_t r = 0; r < a.rows; ++r) {
+    const __int128 at = first + out_step * r;               // from the first row of block_table
+    const __int128 below = at <= 0 || in_step == 0 ? 0 : at >= last ? last : at / in_step * in_step;   // the nearest rows
+    const __int128 above = below + in_step < last ? below + in_step : last;
+    if ((at > below - n && at < below + n) || (at > above - n && at < above + n)) return true;
+  }
+  return false;
+}
+
 // Nothing to do: no rows.
 bool empty(const pp_attention_args& a) { return a.requests == 0 || a.tokens == 0 || a.max_new == 0; }
 
@@ -435,13 +453,7 @@ int pp_fork_tables(const pp_fork_args* a, void* hip_stream) {
     return report(PP_E_ARG, "null pointer");
   if (a->rows > 1 && a->out_row_stride < a->max_blocks)
     return report(PP_E_ARG, "rows of out_table overlap");
-  // the tables from their first entry to their last
-  if (a->rows && a->parents && a->max_blocks) {
-    const uintptr_t in = (uintptr_t)a->block_table, out = (uintptr_t)a->out_table;
-    const uintptr_t in_end = in + 4 * ((uint64_t)(a->parents - 1) * a->row_stride + a->max_blocks);
-    const uintptr_t out_end = out + 4 * ((uint64_t)(a->rows - 1) * a->out_row_stride + a->max_blocks);
-    if (in < out_end && out < in_end) return report(PP_E_ARG, "out_table overlaps block_table");
-  }
+  if (a->rows && a->parents && tables_meet(*a)) return report(PP_E_ARG, "out_table overlaps block_table");
   return launched(launch_fork_tables(*a, (hipStream_t)hip_stream));
 }
 

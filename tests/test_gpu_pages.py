@@ -286,3 +286,21 @@ def test_refusals_of_the_binding():
     for kw in (dict(page_size=8), dict(page_size=16, first=101), dict(page_size=16, first=-1)):
         with pytest.raises(B.PPError):
             B.pp_free_pages(table, length, free, count, marks, **kw)
+
+
+@pytest.mark.parametrize("rows,parents", [(40, 40), (70, 40), (40, 70), (1, 1)])
+def test_fork_tables_side_by_side(rows, parents):
+    """Both tables in one tensor, a row of one beside the other's: no entry is in both."""
+    parent, length, table, free = fork_case(rows, rows, parents)
+    want = R.fork(parent, length, table, free, np.full((rows, 9), -5, np.int32), 16)
+    most = max(rows, parents)
+    for shape, pick in (((most, 2, 9), lambda x, i: x[:, i]), ((most, 23), lambda x, i: x[:, 14 * i:14 * i + 9])):
+        for i in range(2):
+            both = torch.full(shape, -5, dtype=torch.int32, device="cuda")
+            t, out = pick(both, i)[:parents], pick(both, 1 - i)[:rows]
+            t.copy_(dev(table))
+            got = dict(out_table=out, **{k: dev(np.full(rows, -7)) for k in ("out_length", "source", "target", "tokens")}, taken=dev([-7]))
+            B.pp_fork_tables(dev(parent), dev(length), t, dev(free), *got.values(), page_size=16)
+            torch.cuda.synchronize()
+            assert all(np.array_equal(got[k].cpu().numpy(), want[k]) for k in got)
+            assert np.array_equal(t.cpu().numpy(), table)

@@ -246,3 +246,10 @@ def test_layouts_agree():
     """The binding packs arguments by itself: as long as the structures of the C interface."""
     for packed, args in ((B._ROTARY_ARGS, B.pp_rotary_args), (B._COPY_ARGS, B.pp_copy_args), (B._FORK_ARGS, B.pp_fork_args), (B._FREE_ARGS, B.pp_free_args)):
         assert packed.size == ctypes.sizeof(args)
+
+
+@pytest.mark.parametrize("row,out_row,at", [(16, 16, 7), (16, 16, -7), (16, 16, 9), (16, 24, 8), (24, 16, 8), (0, 16, 7), (16, 16, 16 + 9), (0, 8, -8), (20, 8, -8)])
+def test_fork_refuses_tables_that_meet(L, row, out_row, at):
+    """Rows of 8 entries of one table that lie among the other's and have entries in common with them."""
+    a = _fork(row_stride=row, out_row_stride=out_row, out_table=AT + 4 * at)
+    assert L.pp_fork_tables(ctypes.byref(a), None) == B.PP_E_ARG and B.pp_last_error()
