@@ -253,3 +253,36 @@ def test_fork_refuses_tables_that_meet(L, row, out_row, at):
     """Rows of 8 entries of one table that lie among the other's and have entries in common with them."""
     a = _fork(row_stride=row, out_row_stride=out_row, out_table=AT + 4 * at)
     assert L.pp_fork_tables(ctypes.byref(a), None) == B.PP_E_ARG and B.pp_last_error()
+
+
+# Bytes of the two regions of pp_latent_attention's workspace: 512 parts of 16 or of 128 rows with a log sum each,
+# and 256 cuts of 20 bytes.
+def _regions(value_dim):
+    return tuple(512 * n * (value_dim + 1) * 4 + 5120 for n in (16, 128))
+
+
+@pytest.mark.parametrize("value_dim", [256, 512])
+@pytest.mark.parametrize("requests,tokens,q_heads,max_new,few,tiles", [
+    (1, 1, 16, 1, True, False), (65_536, 65_536, 16, 1, True, False), (8, 16, 8, 2, True, False),       # 16 rows at most
+    (1, 1, 17, 1, False, True), (1, 2, 16, 2, False, True), (33, 16_384, 7, 4096, True, True),
+    (4, 4096, 16, 1024, False, True), (6, 4096, 16, 1024, True, True),                                   # apart unless all have max_new tokens
+    (512, 512, 128, 1, False, True), (513, 513, 128, 1, False, False), (8, 8128, 16, 2048, True, True),  # up to 1,024 slots of 128 rows,
+    (8, 8136, 16, 2048, True, False), (4, 8192, 16, 2048, False, False), (1, 131_073, 128, 131_073, False, False)])  # a request one more
+def test_latent_workspace_sizes(L, requests, tokens, q_heads, max_new, few, tiles, value_dim):
+    dim = value_dim + 64
+    pages = _latent_pages(dim=dim, page_stride=16 * dim, head_stride=16 * dim, token_stride=dim)
+    a = _call(requests=requests, tokens=tokens, q_heads=q_heads, max_new=max_new, max_len=100_000, max_blocks=100_000)
+    row, slot = _regions(value_dim)
+    assert L.pp_latent_workspace(ctypes.byref(pages), value_dim, ctypes.byref(a)) == few * row + tiles * slot
+
+
+@pytest.mark.parametrize("blocks,apart", [(1, False), (132, False), (133, True), (10_000, True)])
+def test_latent_keys_of_single_tokens_end_with_the_block_table(L, blocks, apart):
+    """64 requests of 600 tokens, up to 512 each: two at least have more than one (536 beside one each), so 62 may be single
+    tokens, which go apart where they may have more than 131,072 keys (2,114 each).  Keys end with the block
+    table whatever the bound on the lengths."""
+    row, slot = _regions(512)
+    kw = dict(requests=64, tokens=600, max_new=512, q_heads=16, max_blocks=blocks)
+    for n in (blocks * 16, blocks * 16 + 1, 1 << 20, (1 << 31) - 1):
+        a = _call(max_len=n, **kw)
+        assert L.pp_latent_workspace(ctypes.byref(_latent_pages()), 512, ctypes.byref(a)) == apart * row + slot
