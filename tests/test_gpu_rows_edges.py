@@ -7,7 +7,7 @@ import torch
 
 from paper_2608_01655_amd import binding as B
 from tests import rows_ref as R
-from tests.test_gpu_latent import attend, case, check, close, put
+from tests.test_gpu_latent import attend, case, check, check_requests, put
 
 pytestmark = pytest.mark.gpu
 BF, HF, E4 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
@@ -95,3 +95,46 @@ def test_what_is_not_seen_costs_no_time(new, heads, n, requests, window, cache):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     print(f"{clean:.1f} us, {spoilt:.1f} with NaN", flush=True)
     assert spoilt < 2 * clean + 20
+
+
+def many(seed, requests, lo, hi, heads, *, latent, dtype, cache, window=0, page=16, pages=2048):
+    """Single tokens of long requests, whose rows of the block table share a pool that is much smaller."""
+    c = case([1] * 4, [pages * page // 4] * 4, heads, latent=latent, dtype=dtype, cache=cache, page=page, seed=seed, spare=0)
+    g = torch.Generator().manual_seed(seed)
+    length = torch.randint(lo, hi + 1, (requests,), generator=g)
+    c["table"] = torch.randint(0, pages, (requests, -(-hi // page)), generator=g).int().cuda()
+    c["length"], c["begin"] = length.int().cuda(), torch.arange(requests + 1, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c["q"] = torch.randn((requests, heads, latent + 64), generator=g, device="cuda", dtype=dtype)
+    c["out"] = torch.full((requests, heads, latent), 7.0, dtype=dtype, device="cuda")
+    c["lse"] = torch.full((requests, heads), 7.0, device="cuda")
+    return dict(c, max_new=1, max_len=hi, window=window), length.tolist()
+
+
+def share(length, window, tile, start, least):
+    """Tiles of a block's share: all requests' tiles and starts over 256 blocks."""
+    tiles = [-(-(n - (max(0, n - window) & ~63 if window else 0)) // tile) for n in length]
+    return max(least, -(-sum(t + start for t in tiles) // 256))
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF, BF), (HF, HF), (BF, E4), (HF, E4)])
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("requests,lo,hi,window,page", [(140, 8000, 16_384, 0, 16), (200, 9000, 12_000, 7001, 64)])
+def test_waves_of_many_tiles(requests, lo, hi, window, page, latent, dtype, cache):
+    """Each wave goes through more tiles than it has page numbers of at a time (64 of 16 keys, 32 of 32), and its ring
+    comes round many times."""
+    c, length = many(requests, requests, lo, hi, 16, latent=latent, dtype=dtype, cache=cache, window=window, page=page)
+    tile = 32 if cache == E4 else 16
+    assert share(length, window, tile, 16, 8) / 4 > 1.2 * 1024 / tile
+    check_requests(c, [0, 1, requests // 2, requests - 1])
+
+
+@pytest.mark.parametrize("dtype,cache,latent", [(BF, BF, 512), (HF, HF, 256), (HF, E4, 512), (BF, E4, 256)])
+@pytest.mark.parametrize("window", [0, 11_003])
+def test_blocks_of_many_tiles(window, dtype, cache, latent):
+    """The same of blocks of 128 rows whose shares begin and end inside requests: 64 tiles of 32 keys, or of 64."""
+    requests = 130 if cache == E4 else 70
+    c, length = many(requests, requests, 12_000, 16_384, 128, latent=latent, dtype=dtype, cache=cache, window=window)
+    tile, start = (64, 8) if cache == E4 else (32, 16)
+    assert share(length, window, tile, start, start // 2) > 1.2 * 64
+    check_requests(c, [0, 1, requests // 2])
