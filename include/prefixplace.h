@@ -677,7 +677,8 @@ int pp_rotary_write(const pp_rotary_args *args, const pp_kv_pages *pages, void *
  * pp_paged_attention; out rows are [tokens][q_heads][value_dim].  A key of
  * s_j = -infinity makes elements of out NaN where its own are not finite (0
  * times them), unless the row sees no other keys, wherever the call cuts
- * requests. */
+ * requests.  Where query_start is not in order, so that requests overlap,
+ * some may be left unwritten. */
 int64_t pp_latent_workspace(const pp_kv_pages *pages, int32_t value_dim,
                             const pp_attention_args *args);
 int pp_latent_attention(const pp_kv_pages *pages, int32_t value_dim,

@@ -7,7 +7,7 @@ import torch
 
 from paper_2608_01655_amd import binding as B
 from tests import rows_ref as R
-from tests.test_gpu_latent import attend, case, check, check_requests, put
+from tests.test_gpu_latent import attend, case, check, check_requests, close, put
 
 pytestmark = pytest.mark.gpu
 BF, HF, E4 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
@@ -138,3 +138,48 @@ def test_blocks_of_many_tiles(window, dtype, cache, latent):
     tile, start = (64, 8) if cache == E4 else (32, 16)
     assert share(length, window, tile, start, start // 2) > 1.2 * 64
     check_requests(c, [0, 1, requests // 2])
+
+
+@pytest.mark.parametrize("wild", [False, True])
+@pytest.mark.parametrize("requests,heads,overlap", [(40, 128, range(5, 35)), (40, 128, range(5, 9)), (40, 16, range(5, 9)), (1100, 20, range(50, 900))])
+def test_requests_that_overlap_write_nothing_else(requests, heads, overlap, wild):
+    """Starts out of order or outside: what stands around out, lse and the workspace and the rows that no request names stay as
+    they are, and requests that overlap no other have their rows, or are left out whole where all requests together have more
+    tiles of 128 rows than starts in order can have."""
+    c = case([2] * requests, [70] * requests, heads, seed=24)
+    T = 2 * requests
+    begin = c["begin"].tolist()
+    for r in overlap:
+        begin[r] = [0, 10 ** 6, -7, 2 * r][r % 4] if wild else 2 * r + [-8, 6, -3, 0][r % 4]
+    begin[0] = 1                                      # a row of nobody, but where a request begins at 0
+    named = [0] * (T + 1)
+    clip = lambda x: min(max(x, 0), T)  # noqa: E731
+    ranges = [(clip(a), max(clip(a), clip(b))) for a, b in zip(begin, begin[1:])]
+    for a, b in ranges:
+        for t in range(a, b):
+            named[t] += 1
+    alone = [t for r, (a, b) in enumerate(ranges) if (a, b) == (2 * r, 2 * r + 2) and named[a] == named[a + 1] == 1 for t in (a, a + 1)]
+    assert max(named) > 1 and (wild or len(alone) > 4 and not named[0])
+    bad = dict(c, begin=torch.tensor(begin, dtype=torch.int32, device="cuda"))
+    need = B.pp_latent_workspace(c["q"], c["cache"], c["table"], c["latent"], max_new=T, max_len=c["max_len"])
+    guard = 1 << 20
+    space = torch.full((need + 2 * guard,), 0x5a, dtype=torch.uint8, device="cuda")
+    outs = torch.full((T + 64, heads, c["latent"]), 7.0, dtype=BF, device="cuda")
+    lses = torch.full((T + 64, heads), 7.0, device="cuda")
+    got = attend(dict(bad, out=outs[32:-32], lse=lses[32:-32]), max_new=T, workspace=space[guard:guard + need])
+    torch.cuda.synchronize()
+    assert bool((space[:guard] == 0x5a).all()) and bool((space[guard + need:] == 0x5a).all())
+    for x in (outs, lses):
+        assert bool((x[:32] == 7).all()) and bool((x[-32:] == 7).all())
+    nobody = [t for t in range(T) if not named[t]]
+    for x in got:
+        assert bool((x[nobody] == 7).all())
+    if wild:
+        return
+    if sum(-(-(b - a) * heads // 128) for a, b in ranges) > T * heads // 128 + requests:
+        out = [t for t in alone if bool((got[0][t] == 7).all()) and bool((got[1][t] == 7).all())]
+        assert len(out) < len(alone)
+        alone = [t for t in alone if t not in out]
+    wanted, want_lse, tol, tol_lse = R.latent(c["q"], c["cache"], c["table"], c["begin"], c["length"], c["latent"], scale=c["scale"])
+    close(got[0][alone], wanted[alone], tol[alone])
+    close(got[1][alone], want_lse[alone], tol_lse[alone])
