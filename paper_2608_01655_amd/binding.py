@@ -765,20 +765,19 @@ def pp_paged_attention(q, k_cache, v_cache, block_table, query_start, length, ou
     device, st = _stream_of(torch, q, stream)
     L = lib()
     pages, _, D = _pages(torch, k_cache, v_cache, k_scale, v_scale, device)
-    if q.dim() == 3 and (q.shape[2] != D or out.shape != q.shape):
-        raise ValueError("shape mismatch")
-    _attend(torch, device, st, stream, L.pp_attention_workspace, L.pp_paged_attention, (pages,), q,
-            block_table, query_start, length, out, lse, scale, max_new, max_len, window, workspace)
+    _attend(torch, device, st, stream, L.pp_attention_workspace, L.pp_paged_attention, pages, D,
+            None, q, block_table, query_start, length, out, lse, scale, max_new, max_len, window,
+            workspace)
 
 
-def _attend(torch, device, st, stream, work, call, head, q, block_table, query_start, length, out,
-            lse, scale, max_new, max_len, window, workspace):
+def _attend(torch, device, st, stream, work, call, pages, D, latent, q, block_table, query_start,
+            length, out, lse, scale, max_new, max_len, window, workspace):
     """The checks and the call that attention over pages of any kind has: work and call are the C
-    entries, head their arguments before pp_attention_args."""
+    entries, D the pages' dim, and latent that of out's rows where it is another (and an argument)."""
     (qt, qh), (ot, oh) = _rows(q, "q", device), _rows(out, "out", device)
-    T, Hq, _ = q.shape
+    T, Hq, d = shape = q.shape
     R = length.shape[0]
-    if out.shape[:2] != q.shape[:2] or out.dtype != q.dtype:
+    if d != D or out.shape != (shape if latent is None else (T, Hq, latent)) or out.dtype != q.dtype:
         raise ValueError("shape mismatch")
     i32 = torch.int32
     if length.dtype != i32 or length.dim() != 1 or length.get_device() != device \
@@ -801,7 +800,7 @@ def _attend(torch, device, st, stream, work, call, head, q, block_table, query_s
 
     if workspace is None:
         a = args(0, 0)
-        need = work(*head, a)
+        need = work(pages, a) if latent is None else work(pages, latent, a)
         if need < 0:
             _check(need)
         if need:
@@ -815,7 +814,7 @@ def _attend(torch, device, st, stream, work, call, head, q, block_table, query_s
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace: want a contiguous tensor on the current GPU")
         a = args(workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = call(*head, a, st)
+    rc = call(pages, a, st) if latent is None else call(pages, latent, a, st)
     if rc:
         _check(rc)
 
@@ -939,12 +938,12 @@ def pp_latent_attention(q, cache, block_table, query_start, length, out, lse=Non
     if cache.dim() != 4 or cache.shape[1] != 1:
         raise ValueError("cache: want [pages][1][page_size][dim]")
     pages, _, D = _pages(torch, cache, None, k_scale, None, device)
-    if q.dim() != 3 or q.shape[2] != D or out.dim() != 3:
+    if out.dim() != 3:
         raise ValueError("shape mismatch")
     L = lib()
-    _attend(torch, device, st, stream, L.pp_latent_workspace, L.pp_latent_attention,
-            (pages, out.shape[2]), q, block_table, query_start, length, out, lse, scale, max_new,
-            max_len, window, workspace)
+    _attend(torch, device, st, stream, L.pp_latent_workspace, L.pp_latent_attention, pages, D,
+            out.shape[2], q, block_table, query_start, length, out, lse, scale, max_new, max_len,
+            window, workspace)
 
 
 def pp_latent_workspace(q, cache, block_table, value_dim, *, max_new, max_len, window=0) -> int:
