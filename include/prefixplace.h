@@ -534,7 +534,8 @@ int pp_block_tables(const pp_block_args *args, void *hip_stream);
 
 /* One layer's pages: element (page, head, token, i) of k and of v lies at
  * page * page_stride + head * head_stride + token * token_stride + i
- * elements (any order of the three).  PP_E4M3 pages hold value / scale of
+ * elements (any order of the three).  dim is what the call takes: 64, 128 or
+ * 256 in pp_kv_write and pp_paged_attention.  PP_E4M3 pages hold value / scale of
  * their head, k_scale and v_scale [heads] (device; NULL = 1; finite and
  * above 0, which the host cannot see); other types have no scales. */
 typedef struct {
@@ -543,7 +544,7 @@ typedef struct {
     int32_t dtype;
     int32_t n_pages, page_size;    /* page_size a power of two, 16 .. 1,024 */
     int32_t heads;
-    int32_t dim;                   /* 64, 128 or 256 */
+    int32_t dim;
     int64_t page_stride, head_stride, token_stride;
 } pp_kv_pages;
 
@@ -643,7 +644,8 @@ int pp_turns(int32_t n, const double *radians, uint64_t *turns);
  * NULL) hold one row a token and head, latent rows with heads = 1 say.
  * q_heads or k_heads = 0: no such rows.  Rows are [tokens][heads][dim];
  * dims, firsts and norms are multiples of 8, dims at most 1,024, rot_dim is
- * a multiple of 16 (0 = no rotation); weights are of the rows' type.
+ * a multiple of 16 (0 = no rotation); weights are of the rows' type.  Tokens
+ * times heads are 2^31 - 1 at most.
  * An output may be its input (the same pointer and strides). */
 typedef struct {
     int32_t tokens;
@@ -674,7 +676,10 @@ int pp_rotary_write(const pp_rotary_args *args, const pp_kv_pages *pages, void *
  * multiplied in, and out is yet to be multiplied by the values' expansion.
  * Pages: k the rows, v NULL, heads 1, k_scale [1] (PP_E4M3 pages);
  * value_dim 512 or 256, dim = value_dim + 64.  Everything else is as in
- * pp_paged_attention; out rows are [tokens][q_heads][value_dim].  A key of
+ * pp_paged_attention; out rows are [tokens][q_heads][value_dim].  Requests
+ * are cut by their lengths, not by max_len, so one far above costs no time
+ * (it says whether requests of few tokens beside prompts may be long enough for
+ * launches of their own).  A key of
  * s_j = -infinity makes elements of out NaN where its own are not finite (0
  * times them), unless the row sees no other keys, wherever the call cuts
  * requests.  Where query_start is not in order, so that requests overlap,
@@ -739,7 +744,7 @@ int pp_fork_tables(const pp_fork_args *args, void *hip_stream);
  * many; the first `room` of them are written to free_pages, whose other
  * entries stay as they are.  marks [n_pages] is scratch memory (8-byte
  * aligned), written before it is read.  Numbers out of range in rows name
- * no page. */
+ * no page.  n_pages is 2^24 at most. */
 typedef struct {
     int32_t requests;              /* >= 0, at most 65,536 */
     int32_t max_blocks;

@@ -11,6 +11,11 @@
 // a wave has the scores of 32 rows, and then of all 128 rows the values of a quarter of the latent, so that the
 // accumulators (128 x 512 floats, half the CU's registers) are there once.  Weights go from wave to wave
 // through LDS.  Both cut the batch into equal shares for 256 blocks, and k_latent_join puts cut rows together.
+//
+// Weights are rounded to the queries' type for the second product, as in pp_attend.hip and for its reason; scores, sums
+// and accumulators are 32 bits.  It costs less than a tenth of the output's own rounding (error against 64 bits 1.7e-3 in bf16
+// and 2.1e-4 in f16, with it and without), but outputs near the middle of two values of their type go to the other one: they
+// differ by 6e-4 to 1.2e-3 (f16 9e-5 to 1.8e-4) in all from those of weights in 32 bits.
 
 #include "pp_attend.h"
 
@@ -25,12 +30,12 @@ constexpr int kBlocks = 256;         // resident ones: one a CU
 constexpr int kSlots = 1024;         // row tiles that k_latent_tiles cuts into equal shares, and requests
 // What an item's start and end cost it, in tiles (stages of 16 or 32 keys, steps of 32), and the least that a block takes
 // of them.  A start takes k_latent_rows some 11 us beside 1 us a tile of a wave, and k_latent_tiles 20 us beside 1.7 us a
-// step.  With 4 and 8 (rows), 8 and 12 (tiles): 64 requests of 16 heads, 8 bits, 73 us where this takes 60, 48 requests of
-// 128 heads 112 for 87, 512 short requests 89 for 70.
-// A least share of 4 stages: lone requests of 4,097 and 16,384 keys 20.5 and 30.2 us, of 8 21.2 and 26.1 (fewer parts).
+// step.  With 4 and 8 (rows), 8 and 12 (tiles): 64 requests of 16 heads, 8 bits, 68.7 us where this takes 59.9, 48 requests of
+// 128 heads 88.6 for 80.4, 512 short requests 78.4 for 65.3.
+// A least share of 4 stages: lone requests of 4,097 and 16,384 keys 20.0 and 28.6 us, of 8 19.9 and 24.8 (fewer parts).
 constexpr int kRowsStart = 16, kRowsShare = 8, kTilesStart = 16, kTilesShare = 8;
 // Keys that requests of few rows may have beside prompts and still go with them through k_latent_tiles: 32 single tokens
-// of 2,048 keys beside 512 new ones 87 us, with launches of their own 104; 16 of 16,384 365 for 362.
+// of 2,048 keys beside 512 new ones 89 us, with launches of their own 104; 16 of 16,384 361.7 for 360.5.
 constexpr int kAlone = 131072;
 
 // Rows that begin in block `block` and go on in the next ones up to `last`: `rows` of them from row `row` on of the
@@ -220,7 +225,7 @@ __device__ __forceinline__ Piece piece_of(int64_t at, int32_t start, int32_t til
 // keeps a stage in flight while it works on another, without a barrier.
 // Bound by memory where there is much to read: 64 requests of 500 to 16,383 keys, 16 heads, 8 bits, 172 MB in 54 us, of
 // which the finding of the first share takes 2.5, the queries and the first tiles 3.5 and the joining of the waves and
-// the rows' stores 5; more keys go at 5.1 to 5.6 TB/s.  A lone request of 4,097 keys takes 14 us, 5 of them for two
+// the rows' stores 5; more keys go at 5.1 to 5.6 TB/s.  A lone request of 4,097 keys takes 15 us, 5 of them for two
 // tiles a wave, the rest as before.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_rows(pp_kv_pages p, pp_attention_args a, Split pl) {
@@ -554,12 +559,12 @@ __device__ __forceinline__ int this_lane() {
 
 // 128 rows of one request and one part of its keys a block: a key's row is read from memory once for 128 rows and
 // its values once from LDS (its scores four times, once a wave), where two blocks of 64 rows would need twice of both.
-// Bound by the matrix cores: prompts of 1,024 to 2,048 tokens of 16 heads behind up to 16,384 in f16 1,300 us, 1.06
-// PFLOP/s, of 2,048 behind 16,384 in bf16 1.16 (a product of 8,192 squared: 1.18 and 1.24).  A step takes 3,750 cycles
+// Bound by the matrix cores: prompts of 1,024 to 2,048 tokens of 16 heads behind up to 16,384 in f16 1,326 us, 1.05
+// PFLOP/s with the join, all behind 16,384 in bf16 1.19 (a product of 8,192 squared: 1.17 and 1.20).  A step takes 3,750 cycles
 // (f16 3,950, whose maxima are followed more closely), its products 2,176, at 2.2 GHz: products alone draw so much power that the
 // clock goes down to 1.7 GHz.  Without the reads of keys 6% less, without the loads of tiles 8%, without exponentials 1%;
 // products of scores and values in turn took as long.  8-bit rows are widened once for the scores and once for the values: 5,250
-// cycles, 0.9 PFLOP/s.
+// cycles, 0.99 PFLOP/s.
 template <bool F16, bool NARROW, int C>
 __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_attention_args a, Split pl) {
   using Sh = LatentTiles<NARROW, C>;
@@ -1067,8 +1072,8 @@ __global__ void __launch_bounds__(256, 1) k_latent_tiles(pp_kv_pages p, pp_atten
 
 // --------------------------------------------------------- k_latent_join ---
 
-// Cut rows, of the `each` at most of a cut.  Bound by the chain of its loads where parts are few (a lone request 4.7 us)
-// and by memory where they are many (48 requests of 128 heads, 77 MB, 13.8 us): a wave reads eight parts at a time, their
+// Cut rows, of the `each` at most of a cut.  Bound by the chain of its loads where parts are few (a lone request 4.3 us)
+// and by memory where they are many (48 requests of 128 heads, 77 MB, 13.0 us): a wave reads eight parts at a time, their
 // log sums with them, and WAVES waves share parts where they are many.  A wave has a row of k_latent_rows, or
 // a 32nd of 32 rows of k_latent_tiles, as they lie.
 template <bool F16, int C, int ROWS, int WAVES>
@@ -1176,7 +1181,7 @@ Choice choose(const pp_kv_pages& p, const pp_attention_args& a, Split& pl) {
   const int64_t slots = (int64_t)a.tokens * pl.group / 128 + a.requests;
   pl.slots = slots < INT32_MAX ? (int32_t)slots : INT32_MAX;
   pl.even = slots <= kSlots;
-  pl.by_slot = slots < kBlocks;     // fewer blocks of k_latent_join without rows: 32 requests of 4 new tokens 84 us for 89
+  pl.by_slot = slots < kBlocks;     // fewer blocks of k_latent_join without rows: 32 requests of 4 new tokens 78 us for 81
   return ch;
 }
 

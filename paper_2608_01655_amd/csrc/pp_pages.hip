@@ -25,8 +25,8 @@ struct Copy {
 };
 
 // A block copies kCopyUnits units (32 KB) of one page in one pool, four at a time a thread.  Bound by memory: 512
-// chunks of pages in all layers' pools, 537 MB read and written, 203 us, 5.3 TB/s, as a large copy.  29 open
-// pages take 3.5 us, two reads one after the other, and 8.4 with the call.
+// chunks of pages in all layers' pools, 537 MB read and written, 204 us, 5.3 TB/s, as a large copy.  29 open
+// pages take 3.4 us, two reads one after the other, and 8.5 with the call.
 constexpr int kCopyUnits = 2048;
 
 __global__ void __launch_bounds__(256) k_copy(Copy c) {
@@ -84,8 +84,9 @@ __device__ __forceinline__ bool is_open(const pp_fork_args& a, int32_t n) {
 
 // Rows need as many pages as rows before them have an open parent, less the different ones of
 // those parents.  Every block counts both for itself, with a bit for each parent seen, so that one launch
-// does.  Bound by the chain of its reads (parents, their lengths, rows): 64 new rows 4.2 us, 4,096 of up to 512
-// blocks 9.3 us, 9.5 MB; both take 9 us with the call.
+// does.  Bound by the chain of its reads (parents, their lengths, rows): 64 new rows 4.4 us, 4,096 of up to 512
+// blocks 9.5 us, 9.5 MB; 8.6 and 9.2 us a call among others.  The counting grows with the square of the rows and
+// shows from 8,192 on: 15 us, 16,384 43, 65,536 444.
 __global__ void __launch_bounds__(1024) k_fork(pp_fork_args a, int shift) {
   __shared__ uint32_t seen[kForkMost / 32];
   __shared__ int32_t sums[16];
@@ -195,8 +196,8 @@ __device__ __forceinline__ int32_t before(int32_t x, int32_t& all, int32_t* sums
 }
 
 // The whole of it in one block, with a bit a page in LDS, for few rows: 16 waves take two rows at a time each.  64
-// rows of up to 512 blocks 5.5 us (8.0 with the call); 128 of 512 11.6 us with the call and 256 of 256 13.9, where the
-// four launches below take 13.
+// rows of up to 512 blocks 7.2 us (7.4 a call among others); 128 of 512 10.8 us and 256 of 256 13.4, where the
+// four launches below take 12.5.
 constexpr int kFreeWords = 32768;     // pages / 32
 constexpr int kFewRows = 256;
 constexpr int kFewEntries = 65536;
@@ -248,8 +249,8 @@ __global__ void __launch_bounds__(1024) k_free_few(pp_free_args a, int shift) {
 }
 
 // Byte p of `marks` says whether page p is named: bytes because waves store them without waiting for each
-// other, where bits would take an atomic each.  4,096 rows that name 1.2 million pages take 18.5 us: k_clear 2.2, k_mark 9.5
-// (scattered bytes), k_count 2, k_list 4.2, each a launch behind the other.
+// other, where bits would take an atomic each.  4,096 rows that name 1.2 million pages take 18.9 us: k_clear 2.2, k_mark 9.7
+// (scattered bytes), k_count 1.9, k_list 3.7, each a launch behind the other.
 __global__ void __launch_bounds__(256) k_clear(uint8_t* marks, int32_t n_pages) {
   const int32_t whole = n_pages / 8, at = blockIdx.x * 256 + threadIdx.x;
   for (int64_t i = at; i < whole; i += (int64_t)gridDim.x * 256) ((uint64_t*)marks)[i] = 0;

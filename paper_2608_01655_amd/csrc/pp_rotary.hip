@@ -3,8 +3,8 @@
 // y = x / sqrt(mean x^2 + eps) * weight, (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t), in 32 bits from
 // the rows' read to their one rounding.  Bound by memory: a row is read once and written once, 16 bytes a lane, whatever
 // is done to it between.  65,536 tokens of 32 query and 8 key heads of 128, half of each rotated, into 8-bit pages take
-// 283 us, 1.48 GB at 5.2 TB/s, what a large copy reaches; rotation and write in torch operations 4,350.  61 tokens of
-// 28 and 4 normed heads take 4.4 us, a chain of slot, row and store behind the launch, and 9.3 with the call's checks.
+// 282 us, 1.48 GB at 5.2 TB/s, what a large copy reaches; rotation and write in torch operations 4,341.  61 tokens of
+// 28 and 4 normed heads take 4.2 us, a chain of slot, row and store behind the launch, and 9.5 with the call's checks.
 
 #include "pp_rows.h"
 
