@@ -578,7 +578,9 @@ int pp_kv_write(const pp_kv_pages *pages, int32_t tokens, int32_t dtype,
  * max_new and max_len bound every request's new tokens and length (parts of
  * long requests are cut by max_len, so one far above costs time); a request
  * of more than max_new new tokens may be left unwritten, and rows of tokens
- * that no request has are.  `workspace` is device memory
+ * that no request has are.  Calls that need more than 2^24 blocks (65,536
+ * requests of more than 256 key heads) fail with PP_E_DEVICE and write
+ * nothing, or the rows of a part of the requests.  `workspace` is device memory
  * of pp_attention_workspace bytes at least (256-byte aligned); the call
  * writes it before it reads it, so its contents need not be kept. */
 typedef struct {

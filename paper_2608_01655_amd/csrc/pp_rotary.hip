@@ -278,6 +278,7 @@ hipError_t launch_rotary(const pp_rotary_args& a, const pp_kv_pages* pages, hipS
     kern<<<(unsigned)(((int64_t)w.tokens * w.waves + 3) / 4), 256, 0, st>>>(w, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    if (t + turn >= a.tokens) break;
     for (Rows* r : {&w.q, &w.k, &w.v}) {
       if (r->in) r->in += turn * r->token;
       if (r->out) r->out += turn * r->out_token;
